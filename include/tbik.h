@@ -64,6 +64,7 @@ typedef enum {
     TBIK_FP6_E2M3 = 6,        /* OCP 6-bit float, 2 exponent / 3 fraction bits, bias 1, no infinities or NaN, max 7.5 */
     TBIK_FP6_E3M2 = 7         /* OCP 6-bit float, 3 exponent / 2 fraction bits, bias 3, no infinities or NaN, max 28  */
 } tbik_dtype;
+typedef enum { TBIK_ACT_NONE = 0, TBIK_ACT_RELU = 1, TBIK_ACT_SILU = 2, TBIK_ACT_GELU = 3, TBIK_ACT_GELU_TANH = 4 } tbik_activation;
 typedef enum { TBIK_SUM = 0, TBIK_MAX = 1, TBIK_LOGSOFTMAX = 2 } tbik_rowop;
 
 #define TBIK_MAX_SHARDS 64
@@ -495,6 +496,94 @@ int tbik_gemm_reference_mxfp6(const void *X, int64_t ldx, const void *Xs, int64_
 int tbik_rmsnorm_f16(const void *x, const void *weight, void *y, int M, int H, float eps, void *hip_stream);
 int tbik_combine_residual_rmsnorm_f16(const float *partials, int P, const void *residual, const void *weight, float eps,
                                       void *hidden, void *normed, int M, int H, void *hip_stream);
+
+/*
+ * Matrix products with an epilogue: what a layer does with each output element before it is stored.  With t the fp32 value that
+ * the product without an epilogue rounds (T over the whole K, Theorem 1), in this order, each step one fp32 operation,
+ *   Y[m,n] = round( act(t * row_scale[m] * col_scale[n] + bias[n]) + residual[m,n] )          absent parts are skipped
+ * and one rounding, to y_dtype.  The scales are those of a quantisation scheme (a scale per token and per output channel), which
+ * the 8-bit products leave to the caller.  act, in fp32:
+ *   RELU       v < 0 ? 0 : v                      SILU       v / (1 + e^-v)
+ *   GELU       v Phi(v), Phi the normal distribution function          GELU_TANH  v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) / 2
+ * with the hardware's exponential and reciprocal (about one fp32 ulp each): within 2^-20 |act(v)| + 2^-100 for |v| <= 12; the
+ * negative tails, which have their own exponent's rounding, keep a relative error below 2^-16.
+ * Determinism contract: the bits of row m depend on row m of X and residual, row_scale[m], and the weights, scales and biases of
+ * the columns only, and
+ *   tbik_gemm_*_epilogue(...) == tbik_tree_combine_epilogue(tbik_gemm_shard_partials_*(..., P), P, ...)      bit for bit, every legal P;
+ * partial sums of any operand format (fp32, MXFP4 and MXFP6 too) can be ended so.
+ *
+ *   epilogue     HOST pointer, read before the call returns; its pointers are device pointers
+ *     row_scale  fp32 [M] or NULL         col_scale  fp32 [N] or NULL            4-byte aligned
+ *     bias       [N] of bias_dtype (TBIK_F32, TBIK_BF16 or TBIK_F16) or NULL      aligned to its type
+ *     activation a tbik_activation
+ *     residual   [M, ldr] of y_dtype, ldr >= N, or NULL; aligned to its type (16 bytes and whole 16-byte rows take the vector
+ *                path); may be Y itself (ldr == ldy: updated in place), and must not overlap Y otherwise
+ *   y_dtype      tbik_gemm_epilogue: TBIK_F32 or x_dtype, which is TBIK_BF16 or TBIK_F16; the others: TBIK_F32, TBIK_BF16 or TBIK_F16
+ *   Everything else -- operands, alignment, tree parameters, workspace -- as for tbik_gemm (workspace: tbik_gemm_16bit_workspace_bytes),
+ *   tbik_gemm_fp8, tbik_gemm_mxfp8 and tbik_tree_combine.
+ * Errors: those of these calls; NULL without an epilogue, DTYPE for an unknown activation or bias type, SHAPE, ALIGN.
+ */
+typedef struct {
+    const float *row_scale;
+    const float *col_scale;
+    const void *bias;
+    tbik_dtype bias_dtype;
+    tbik_activation activation;
+    const void *residual;
+    int64_t ldr;
+} tbik_epilogue;
+int tbik_gemm_epilogue(const void *X, int64_t ldx, const void *W, int64_t ldw, const tbik_epilogue *epilogue, void *Y, int64_t ldy,
+                       tbik_dtype y_dtype, tbik_dtype x_dtype, int M, int N, int K, int leaf, int k_first,
+                       void *workspace, size_t workspace_bytes, void *hip_stream);
+int tbik_gemm_fp8_epilogue(const void *X, int64_t ldx, const void *Wt, int64_t ldwt, const tbik_epilogue *epilogue, void *Y, int64_t ldy,
+                           tbik_dtype y_dtype, tbik_dtype x_dtype, int M, int N, int K, int leaf, int k_first,
+                           void *workspace, size_t workspace_bytes, void *hip_stream);
+int tbik_gemm_mxfp8_epilogue(const void *X, int64_t ldx, const void *Xs, int64_t ldxs, const void *Wt, int64_t ldwt,
+                             const void *Ws, int64_t ldws, const tbik_epilogue *epilogue, void *Y, int64_t ldy, tbik_dtype y_dtype,
+                             tbik_dtype x_dtype, int M, int N, int K, int leaf, int k_first,
+                             void *workspace, size_t workspace_bytes, void *hip_stream);
+int tbik_tree_combine_epilogue(const float *partials, int P, const tbik_epilogue *epilogue, void *Y, int64_t ldy, tbik_dtype y_dtype,
+                               int M, int N, void *hip_stream);
+
+/*
+ * 8-bit outputs with scales: what makes the operand X of the 8-bit and microscaling products, in the kernel that has its values in fp32.
+ * v is the fp32 value that the 16-bit call rounds; every element takes one rounding (to nearest, ties to even) from v times a
+ * factor to q_dtype (TBIK_FP8_E4M3, largest = 448, emax = 8, or TBIK_FP8_E5M2, largest = 57344, emax = 15).
+ *   _fp8     one fp32 scale per row:  row_scale[m] = max_i |v[m,i]| / largest, at least 2^-126, 1 for a row of zeros;
+ *            q = r8(v * (1 / row_scale[m])), for tbik_gemm_fp8_epilogue (or tbik_gemm_fp8, whose output the caller scales)
+ *   _mxfp8   one byte s per 32 consecutive columns, the operand of tbik_gemm_mxfp8: 2^(s - 127) is the power of two that brings
+ *            the block's largest magnitude into (2^(emax - 1), 2^emax], s = 127 for a block of zeros, s >= 1;  q = r8(v / 2^(s - 127))
+ * Nothing saturates.  NaN does not count for a maximum and becomes NaN; an infinite v becomes NaN (infinity in E5M2 of _mxfp8), in
+ * _fp8 with an infinite scale, which makes the row's other elements zeros times infinity.
+ *
+ * tbik_rmsnorm_fp8 / _mxfp8: RMSNorm of the rows, after the residual's addition if there is one,
+ *   hidden = r16(x + residual) (stored; x itself without a residual),   v = (hidden * r) * weight   exactly as tbik_rmsnorm forms it
+ * tbik_combine_residual_rmsnorm_fp8 / _mxfp8: the same on shards' partial sums,
+ *   hidden = r16(r16(T(partials)) + residual)   exactly tbik_combine_residual_rmsnorm's
+ * tbik_silu_mul_fp8 / _mxfp8:  v = SiLU(gate) * up, the fp32 value that tbik_silu_mul rounds.
+ *
+ *   x, residual, hidden, gate, up   device, 16-bit of format `dtype` (TBIK_BF16 or TBIK_F16), [M, ld], 16-byte aligned, ld a multiple of 8;
+ *             residual and hidden both or neither; hidden may be x or residual itself (same ld), and must not overlap them otherwise
+ *   weight    device, `dtype`, [H], 16-byte aligned          partials   device, fp32, dense [P, M, H], 16-byte aligned, P a power of two <= 16
+ *   q         device, [M, ldq] bytes, 8-byte aligned, ldq a multiple of 8 (the products ask for 16); no overlap with an input
+ *   scales    device: row_scale fp32 [M]; _mxfp8: [M, lds] bytes, lds >= H / 32
+ *   H, I      up to 65536; a multiple of 8 (_fp8) or 32 (_mxfp8)
+ * Errors: NULL, SHAPE, DTYPE, ALIGN, HIP; combine_residual: SHARDS, UNSUPPORTED.
+ */
+int tbik_rmsnorm_fp8(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, float eps, void *hidden, int64_t ldh,
+                     void *q, int64_t ldq, float *row_scale, tbik_dtype dtype, tbik_dtype q_dtype, int M, int H, void *hip_stream);
+int tbik_rmsnorm_mxfp8(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, float eps, void *hidden, int64_t ldh,
+                       void *q, int64_t ldq, void *scales, int64_t lds, tbik_dtype dtype, tbik_dtype q_dtype, int M, int H, void *hip_stream);
+int tbik_combine_residual_rmsnorm_fp8(const float *partials, int P, const void *residual, int64_t ldr, const void *weight, float eps,
+                                      void *hidden, int64_t ldh, void *q, int64_t ldq, float *row_scale,
+                                      tbik_dtype dtype, tbik_dtype q_dtype, int M, int H, void *hip_stream);
+int tbik_combine_residual_rmsnorm_mxfp8(const float *partials, int P, const void *residual, int64_t ldr, const void *weight, float eps,
+                                        void *hidden, int64_t ldh, void *q, int64_t ldq, void *scales, int64_t lds,
+                                        tbik_dtype dtype, tbik_dtype q_dtype, int M, int H, void *hip_stream);
+int tbik_silu_mul_fp8(const void *gate, int64_t ldg, const void *up, int64_t ldu, void *q, int64_t ldq, float *row_scale,
+                      tbik_dtype dtype, tbik_dtype q_dtype, int M, int I, void *hip_stream);
+int tbik_silu_mul_mxfp8(const void *gate, int64_t ldg, const void *up, int64_t ldu, void *q, int64_t ldq, void *scales, int64_t lds,
+                        tbik_dtype dtype, tbik_dtype q_dtype, int M, int I, void *hip_stream);
 
 /* Forces an internal GEMM variant (testing and tuning only; the bits never depend on it).
  * 0 = choose from the shape (default); other values are listed in tbik_variant_name(). */

@@ -25,10 +25,37 @@ TBIK_MXFP4 = 5
 TBIK_SUM, TBIK_MAX, TBIK_LOGSOFTMAX = 0, 1, 2
 OK = 0
 
+_ACTIVATIONS = {None: 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
+
 VARIANT_AUTO, VARIANT_REFERENCE, VARIANT_T128, VARIANT_T32, VARIANT_T64 = 0, 1, 2, 3, 4
+
+class Epilogue(C.Structure):
+    """tbik_epilogue"""
+    _fields_ = [("row_scale", C.c_void_p), ("col_scale", C.c_void_p), ("bias", C.c_void_p), ("bias_dtype", C.c_int),
+                ("activation", C.c_int), ("residual", C.c_void_p), ("ldr", C.c_int64)]
+
+
+_RMS8 = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_float, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
+_TAIL8 = [C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_void_p, C.c_float, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
+_SILU8 = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
+_TYPES8 = [C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p]         # dtype, q_dtype, rows, columns, stream
 
 # name -> (restype, argtypes); mirrors include/tbik.h
 SIGNATURES = {
+    "tbik_gemm_epilogue": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.POINTER(Epilogue), C.c_void_p, C.c_int64, C.c_int, C.c_int,
+                                     C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "tbik_gemm_fp8_epilogue": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.POINTER(Epilogue), C.c_void_p, C.c_int64, C.c_int, C.c_int,
+                                         C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "tbik_gemm_mxfp8_epilogue": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                           C.POINTER(Epilogue), C.c_void_p, C.c_int64, C.c_int, C.c_int,
+                                           C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "tbik_tree_combine_epilogue": (C.c_int, [C.c_void_p, C.c_int, C.POINTER(Epilogue), C.c_void_p, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_void_p]),
+    "tbik_rmsnorm_fp8": (C.c_int, _RMS8 + _TYPES8),
+    "tbik_rmsnorm_mxfp8": (C.c_int, _RMS8 + [C.c_int64] + _TYPES8),
+    "tbik_combine_residual_rmsnorm_fp8": (C.c_int, _TAIL8 + _TYPES8),
+    "tbik_combine_residual_rmsnorm_mxfp8": (C.c_int, _TAIL8 + [C.c_int64] + _TYPES8),
+    "tbik_silu_mul_fp8": (C.c_int, _SILU8 + _TYPES8),
+    "tbik_silu_mul_mxfp8": (C.c_int, _SILU8 + [C.c_int64] + _TYPES8),
     "tbik_gemm": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int,
                             C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
     "tbik_gemm_shard_partials": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
@@ -731,6 +758,223 @@ def tbik_tree_combine(partials: torch.Tensor, out_dtype=torch.bfloat16, out: tor
     st = lib().tbik_tree_combine(partials.data_ptr(), P, out.data_ptr(), out.stride(0), _dt(out), M, N, _stream())
     _check(st, "tbik_tree_combine")
     return out
+
+
+def _on_current_device(*tensors):
+    """The kernels run on the current device's stream: a tensor that lives elsewhere is refused, not read."""
+    here = _current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError("a tensor on %s in a call on the current device cuda:%d" % (t.device, here))
+
+
+def _epilogue(M, N, out_dtype, row_scale, col_scale, bias, activation, residual) -> Epilogue:
+    """The parts of an epilogue, checked against an output [M, N]; what is not a GPU tensor of the right kind is refused here."""
+    if activation not in _ACTIVATIONS:
+        raise ValueError("activation is one of %s, got %r" % (", ".join(map(repr, _ACTIVATIONS)), activation))
+    e = Epilogue(activation=_ACTIVATIONS[activation])
+    for name, t, n in (("row_scale", row_scale, M), ("col_scale", col_scale, N), ("bias", bias, N)):
+        if t is None:
+            continue
+        if t.shape != (n,) or (t.stride(0) != 1 and n > 1):
+            raise ValueError("%s must be a contiguous tensor [%d]" % (name, n))
+        if name != "bias" and t.dtype != torch.float32:
+            raise TypeError("%s must be float32, got %s" % (name, t.dtype))
+        setattr(e, name, t.data_ptr())
+    if bias is not None:
+        e.bias_dtype = _dt(bias)
+    if residual is not None:
+        e.ldr = _rowmajor(residual, "residual")
+        if residual.shape != (M, N) or residual.dtype != out_dtype:
+            raise ValueError("residual must be [%d, %d] of the output's type %s" % (M, N, out_dtype))
+        e.residual = residual.data_ptr()
+    return e
+
+
+def tbik_gemm_epilogue(X: torch.Tensor, W: torch.Tensor, leaf: int, k_first: int = 1, bias: torch.Tensor | None = None,
+                       activation: str | None = None, residual: torch.Tensor | None = None, row_scale: torch.Tensor | None = None,
+                       col_scale: torch.Tensor | None = None, out_dtype=None, out: torch.Tensor | None = None,
+                       workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """act((X @ W) * row_scale[:, None] * col_scale + bias) + residual in the tree order, rounded once (bf16 or fp16 operands; the
+    output is of their type or float32).  `bias` float32, bfloat16 or float16; `activation` "relu", "silu", "gelu" or "gelu_tanh";
+    `residual` of the output's type, which may be `out` itself."""
+    ldx, ldw = _rowmajor(X, "X"), _rowmajor(W, "W")
+    assert X.dtype == W.dtype and X.dtype in (torch.bfloat16, torch.float16)
+    M, K = X.shape
+    assert W.shape[0] == K
+    N = W.shape[1]
+    if out is None:
+        out = X.new_empty((M, N), dtype=out_dtype or X.dtype)
+    ldo = _rowmajor(out, "out")
+    assert out.shape == (M, N)
+    _on_current_device(X, W, out, bias, residual, row_scale, col_scale, workspace)
+    e = _epilogue(M, N, out.dtype, row_scale, col_scale, bias, activation, residual)
+    L = lib()
+    if workspace is None:
+        need = L.tbik_gemm_16bit_workspace_bytes(M, N, K, leaf, k_first)
+        if need:
+            workspace = _workspace(need, X.device)
+    room, room_bytes = _room(workspace)
+    _check(L.tbik_gemm_epilogue(X.data_ptr(), ldx, W.data_ptr(), ldw, C.byref(e), out.data_ptr(), ldo, _dt(out), _dt(X), M, N, K, leaf, k_first,
+                                room, room_bytes, _stream()), "tbik_gemm_epilogue")
+    return out
+
+
+def tbik_gemm_fp8_epilogue(X: torch.Tensor, Wt: torch.Tensor, leaf: int, k_first: int = 1, fmt: str = "e4m3",
+                           row_scale: torch.Tensor | None = None, col_scale: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+                           activation: str | None = None, residual: torch.Tensor | None = None, out_dtype=torch.bfloat16,
+                           out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """The same on 8-bit operands (Wt is [N, K]), with the scales of their quantisation: row_scale float32 [M], as tbik_rmsnorm_fp8
+    and tbik_silu_mul_fp8 give it, col_scale float32 [N].  bfloat16, float16 or float32 output."""
+    X, Wt, dt = _fp8_operands(X, Wt, fmt)
+    M, K = X.shape
+    N = Wt.shape[0]
+    if out is None:
+        out = X.new_empty((M, N), dtype=out_dtype)
+    ldo = _rowmajor(out, "out")
+    assert out.shape == (M, N)
+    _on_current_device(X, Wt, out, bias, residual, row_scale, col_scale, workspace)
+    e = _epilogue(M, N, out.dtype, row_scale, col_scale, bias, activation, residual)
+    if workspace is None:
+        need = gemm_fp8_workspace_bytes(M, N, K, leaf, k_first)
+        if need:
+            workspace = _workspace(need, X.device)
+    room, room_bytes = _room(workspace)
+    _check(lib().tbik_gemm_fp8_epilogue(X.data_ptr(), X.stride(0), Wt.data_ptr(), Wt.stride(0), C.byref(e), out.data_ptr(), ldo, _dt(out), dt,
+                                        M, N, K, leaf, k_first, room, room_bytes, _stream()), "tbik_gemm_fp8_epilogue")
+    return out
+
+
+def tbik_gemm_mxfp8_epilogue(X, Xs, Wt, Ws, leaf: int, k_first: int = 1, fmt: str = "e4m3", row_scale: torch.Tensor | None = None,
+                             col_scale: torch.Tensor | None = None, bias: torch.Tensor | None = None, activation: str | None = None,
+                             residual: torch.Tensor | None = None, out_dtype=torch.bfloat16, out: torch.Tensor | None = None,
+                             workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """The same on MXFP8 operands (X and Xs as tbik_rmsnorm_mxfp8 and tbik_silu_mul_mxfp8 give them)."""
+    X, Wt, dt, M, N, K = _mx8_operands(X, Xs, Wt, Ws, fmt)
+    if out is None:
+        out = X.new_empty((M, N), dtype=out_dtype)
+    ldo = _rowmajor(out, "out")
+    assert out.shape == (M, N)
+    _on_current_device(X, Xs, Wt, Ws, out, bias, residual, row_scale, col_scale, workspace)
+    e = _epilogue(M, N, out.dtype, row_scale, col_scale, bias, activation, residual)
+    if workspace is None:
+        need = gemm_mxfp8_workspace_bytes(M, N, K, leaf, k_first)
+        if need:
+            workspace = _workspace(need, X.device)
+    room, room_bytes = _room(workspace)
+    _check(lib().tbik_gemm_mxfp8_epilogue(X.data_ptr(), X.stride(0), Xs.data_ptr(), Xs.stride(0), Wt.data_ptr(), Wt.stride(0), Ws.data_ptr(),
+                                          Ws.stride(0), C.byref(e), out.data_ptr(), ldo, _dt(out), dt, M, N, K, leaf, k_first, room, room_bytes,
+                                          _stream()), "tbik_gemm_mxfp8_epilogue")
+    return out
+
+
+def tbik_tree_combine_epilogue(partials: torch.Tensor, bias: torch.Tensor | None = None, activation: str | None = None,
+                               residual: torch.Tensor | None = None, row_scale: torch.Tensor | None = None,
+                               col_scale: torch.Tensor | None = None, out_dtype=torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
+    """act(T(partials[0..P)) * row_scale[:, None] * col_scale + bias) + residual, rounded once: partial sums of any operand format."""
+    assert partials.dim() == 3 and partials.is_contiguous() and partials.dtype == torch.float32
+    P, M, N = partials.shape
+    if out is None:
+        out = partials.new_empty((M, N), dtype=out_dtype)
+    ldo = _rowmajor(out, "out")
+    assert out.shape == (M, N)
+    _on_current_device(partials, out, bias, residual, row_scale, col_scale)
+    e = _epilogue(M, N, out.dtype, row_scale, col_scale, bias, activation, residual)
+    _check(lib().tbik_tree_combine_epilogue(partials.data_ptr(), P, C.byref(e), out.data_ptr(), ldo, _dt(out), M, N, _stream()),
+           "tbik_tree_combine_epilogue")
+    return out
+
+
+def _eight_bit_out(like, M, n, micro, fmt, out, scale):
+    """The patterns and scales of an 8-bit output: new tensors, or the caller's, checked."""
+    if fmt not in _FP8:
+        raise ValueError("fmt is 'e4m3' or 'e5m2', got %r" % (fmt,))
+    if out is None:
+        out = torch.empty((M, n), dtype=torch.uint8, device=like.device)
+    if scale is None:
+        scale = torch.empty((M, n // 32) if micro else (M,), dtype=torch.uint8 if micro else torch.float32, device=like.device)
+    _rowmajor(out, "out")
+    assert out.shape == (M, n) and out.dtype == torch.uint8
+    if micro:
+        _rowmajor(scale, "scale")
+        assert scale.shape == (M, n // 32) and scale.dtype == torch.uint8
+    else:
+        assert scale.shape == (M,) and scale.is_contiguous() and scale.dtype == torch.float32
+    return out, scale
+
+
+def _norm_8bit(name, micro, x, weight, eps, residual, fmt, hidden, out, scale):
+    M, H = x.shape[-2:]
+    if x.dim() == 3:                                  # shards' partial sums [P, M, H]
+        assert x.is_contiguous() and x.dtype == torch.float32
+        first, dtype = (x.data_ptr(), x.shape[0]), residual.dtype
+    else:
+        first, dtype = (x.data_ptr(), _rowmajor(x, "x")), x.dtype
+    assert dtype in (torch.bfloat16, torch.float16)
+    assert weight.shape == (H,) and weight.is_contiguous() and weight.dtype == dtype
+    stream = (None, 0, None, 0)                       # residual and hidden
+    if residual is not None:
+        if hidden is None:
+            hidden = torch.empty((M, H), dtype=dtype, device=x.device)
+        assert residual.shape == hidden.shape == (M, H) and residual.dtype == hidden.dtype == dtype
+        stream = (residual.data_ptr(), _rowmajor(residual, "residual"), hidden.data_ptr(), _rowmajor(hidden, "hidden"))
+    else:
+        assert hidden is None, "hidden is x itself without a residual"
+    out, scale = _eight_bit_out(x, M, H, micro, fmt, out, scale)
+    _on_current_device(x, weight, residual, hidden, out, scale)
+    types = ((scale.stride(0),) if micro else ()) + (_DTYPES[dtype], _FP8[fmt], M, H, _stream())
+    _check(getattr(lib(), name)(*first, *stream[:2], weight.data_ptr(), eps, *stream[2:], out.data_ptr(), out.stride(0), scale.data_ptr(), *types), name)
+    return hidden, out, scale
+
+
+def tbik_rmsnorm_fp8(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual: torch.Tensor | None = None, fmt: str = "e4m3",
+                     hidden: torch.Tensor | None = None, out: torch.Tensor | None = None, scale: torch.Tensor | None = None):
+    """(hidden, q, scale): hidden = x + residual rounded to their type (None without a residual), q the 8-bit patterns (uint8) of
+    RMSNorm(hidden) / scale, scale float32 [M] -- X and row_scale of tbik_gemm_fp8_epilogue.  `hidden` may be x or residual."""
+    assert x.dim() == 2
+    return _norm_8bit("tbik_rmsnorm_fp8", False, x, weight, eps, residual, fmt, hidden, out, scale)
+
+
+def tbik_rmsnorm_mxfp8(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual: torch.Tensor | None = None, fmt: str = "e4m3",
+                       hidden: torch.Tensor | None = None, out: torch.Tensor | None = None, scale: torch.Tensor | None = None):
+    """(hidden, q, scale): the same with a scale byte per 32 columns, uint8 [M, H / 32] -- X and Xs of tbik_gemm_mxfp8."""
+    assert x.dim() == 2
+    return _norm_8bit("tbik_rmsnorm_mxfp8", True, x, weight, eps, residual, fmt, hidden, out, scale)
+
+
+def tbik_combine_residual_rmsnorm_fp8(partials: torch.Tensor, residual: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, fmt: str = "e4m3",
+                                      hidden: torch.Tensor | None = None, out: torch.Tensor | None = None, scale: torch.Tensor | None = None):
+    """(hidden, q, scale) of shards' partial sums [P, M, H]: tbik_combine_residual_rmsnorm with tbik_rmsnorm_fp8's output."""
+    assert partials.dim() == 3
+    return _norm_8bit("tbik_combine_residual_rmsnorm_fp8", False, partials, weight, eps, residual, fmt, hidden, out, scale)
+
+
+def tbik_combine_residual_rmsnorm_mxfp8(partials: torch.Tensor, residual: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, fmt: str = "e4m3",
+                                        hidden: torch.Tensor | None = None, out: torch.Tensor | None = None, scale: torch.Tensor | None = None):
+    """(hidden, q, scale) of shards' partial sums [P, M, H]: tbik_combine_residual_rmsnorm with tbik_rmsnorm_mxfp8's output."""
+    assert partials.dim() == 3
+    return _norm_8bit("tbik_combine_residual_rmsnorm_mxfp8", True, partials, weight, eps, residual, fmt, hidden, out, scale)
+
+
+def _silu_mul_8bit(name, micro, gate, up, fmt, out, scale):
+    ldg, ldu = _rowmajor(gate, "gate"), _rowmajor(up, "up")
+    assert gate.dtype == up.dtype and gate.dtype in (torch.bfloat16, torch.float16) and gate.shape == up.shape
+    M, I = gate.shape
+    out, scale = _eight_bit_out(gate, M, I, micro, fmt, out, scale)
+    _on_current_device(gate, up, out, scale)
+    types = ((scale.stride(0),) if micro else ()) + (_dt(gate), _FP8[fmt], M, I, _stream())
+    _check(getattr(lib(), name)(gate.data_ptr(), ldg, up.data_ptr(), ldu, out.data_ptr(), out.stride(0), scale.data_ptr(), *types), name)
+    return out, scale
+
+
+def tbik_silu_mul_fp8(gate: torch.Tensor, up: torch.Tensor, fmt: str = "e4m3", out: torch.Tensor | None = None, scale: torch.Tensor | None = None):
+    """(q, scale): tbik_silu_mul with 8-bit patterns (uint8) and a float32 scale per row -- X and row_scale of tbik_gemm_fp8_epilogue."""
+    return _silu_mul_8bit("tbik_silu_mul_fp8", False, gate, up, fmt, out, scale)
+
+
+def tbik_silu_mul_mxfp8(gate: torch.Tensor, up: torch.Tensor, fmt: str = "e4m3", out: torch.Tensor | None = None, scale: torch.Tensor | None = None):
+    """(q, scale): the same with a scale byte per 32 columns, uint8 [M, I / 32] -- X and Xs of tbik_gemm_mxfp8."""
+    return _silu_mul_8bit("tbik_silu_mul_mxfp8", True, gate, up, fmt, out, scale)
 
 
 def _rmsnorm(name, dtype, x, weight, eps, out):

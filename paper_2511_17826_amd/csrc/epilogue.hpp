@@ -1,0 +1,109 @@
+// The epilogue of the matrix products (tbik_epilogue), shared by every kernel that ends one: on the fp32 value t = T(...) of
+// an output element, in this order and each step one fp32 operation,
+//   t * row_scale[m] * col_scale[n]  + bias[n]  -> activation  + residual[m][n]  -> one rounding to the output's type.
+// What is absent is skipped.  Position-wise, and the one definition for all kernels, so an element's bits do not depend on
+// the kernel, the tile, the K split or the launch that computes it.
+#pragma once
+
+#include "tbik_device.hpp"
+#include "tbik_internal.hpp"
+
+namespace tbik {
+
+// v / (1 + e^-v) as silu_mul() forms it: hardware exponential and reciprocal, about one fp32 ulp each.
+__device__ __forceinline__ float silu_of(float v) { return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -1.4426950408889634f)); }
+
+// v Phi(v), Phi the normal distribution function.  Its tail, Phi(-a) = erfc(a / sqrt 2) / 2, decides both sides (v < 0: the tail
+// itself; else one minus it), so it is formed without a cancellation: erfc(z) = e^(-z^2) erfcx(z), and erfcx(z) = t q(t) with
+// t = 1 / (1 + 0.375 z), q the polynomial of degree 8 whose largest relative error over z in [0, 10.2] is smallest (1.3e-8, fitted
+// for this kernel; 3.3e-7 evaluated in fp32); beyond, e^(-z^2) is zero in fp32.  The coefficients hold the half.
+__device__ __forceinline__ float gelu_of(float v) {
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(v), 0.26516504294495535f, 1.0f));      // 0.375 / sqrt 2
+    float q = 0.03065868280827999f;
+    q = __builtin_fmaf(q, t, -0.14314346015453339f);
+    q = __builtin_fmaf(q, t, 0.21515342593193054f);
+    q = __builtin_fmaf(q, t, -0.11354447156190872f);
+    q = __builtin_fmaf(q, t, 0.13608127832412720f);
+    q = __builtin_fmaf(q, t, 0.06107687950134277f);
+    q = __builtin_fmaf(q, t, 0.10257558524608612f);
+    q = __builtin_fmaf(q, t, 0.10533598810434341f);
+    q = __builtin_fmaf(q, t, 0.10580608993768692f);
+    const float tail = q * t * __builtin_amdgcn_exp2f(v * v * -0.72134752044448170f);
+    return v * (v < 0.0f ? tail : 1.0f - tail);
+}
+
+// v (1 + tanh u) / 2 with u = sqrt(2 / pi) (v + 0.044715 v^3), as v / (1 + e^(-2 u)).
+__device__ __forceinline__ float gelu_tanh_of(float v) {
+    const float u = v * __builtin_fmaf(v * v, 0.035677408136300125f, 0.79788456080286541f);
+    return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * -2.8853900817779268f));
+}
+
+template <int ACT>
+__device__ __forceinline__ float activation_of(float v) {
+    if constexpr (ACT == TBIK_ACT_RELU) return v < 0.0f ? 0.0f : v;            // NaN stays
+    else if constexpr (ACT == TBIK_ACT_SILU) return silu_of(v);
+    else if constexpr (ACT == TBIK_ACT_GELU) return gelu_of(v);
+    else return gelu_tanh_of(v);
+}
+
+__device__ __forceinline__ float widened(const void *p, int64_t i, int dtype) {
+    if (dtype == TBIK_F32) return reinterpret_cast<const float *>(p)[i];
+    const uint16_t h = reinterpret_cast<const uint16_t *>(p)[i];
+    return dtype == TBIK_F16 ? (float)__builtin_bit_cast(_Float16, h) : bf16_bits_to_f32(h);
+}
+__device__ __forceinline__ uint32_t pack_16x2(float lo, float hi, bool f16) { return f16 ? pack_f16x2(lo, hi) : pack_bf16x2(lo, hi); }
+
+// The steps on COUNT elements of one row, consecutive columns.  The fp32 value behind each is made one of its own: no merging
+// of a last operation with the rounding to 16 bits (see silu_mul).
+template <int COUNT>
+__device__ __forceinline__ void scale_and_bias(const EpilogueParams &e, float (&v)[COUNT], float rs, const float (&cs)[COUNT], const float (&b)[COUNT]) {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        if (e.row_scale) v[i] = v[i] * rs;
+        if (e.col_scale) v[i] = v[i] * cs[i];
+        if (e.bias) v[i] = v[i] + b[i];
+        asm("" : "+v"(v[i]));
+    }
+}
+template <int ACT, int COUNT>
+__device__ __forceinline__ void activate_as(float (&v)[COUNT]) {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        v[i] = activation_of<ACT>(v[i]);
+        asm("" : "+v"(v[i]));
+    }
+}
+template <int COUNT>
+__device__ __forceinline__ void activate(int act, float (&v)[COUNT]) {
+    switch (act) {                         // uniform
+        case TBIK_ACT_RELU: activate_as<TBIK_ACT_RELU>(v); break;
+        case TBIK_ACT_SILU: activate_as<TBIK_ACT_SILU>(v); break;
+        case TBIK_ACT_GELU: activate_as<TBIK_ACT_GELU>(v); break;
+        case TBIK_ACT_GELU_TANH: activate_as<TBIK_ACT_GELU_TANH>(v); break;
+        default: break;
+    }
+}
+template <int COUNT>
+__device__ __forceinline__ void add_residual(float (&v)[COUNT], const float (&r)[COUNT]) {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        v[i] = v[i] + r[i];
+        asm("" : "+v"(v[i]));
+    }
+}
+
+// One element, everything from memory, stored.
+__device__ __forceinline__ void finish_and_store(const EpilogueParams &e, float t, void *Y, int64_t ldy, int64_t row, int64_t col) {
+    float v[1] = {t}, cs[1] = {0.0f}, b[1] = {0.0f}, r[1] = {0.0f}, rs = 0.0f;
+    if (e.row_scale) rs = e.row_scale[row];
+    if (e.col_scale) cs[0] = e.col_scale[col];
+    if (e.bias) b[0] = widened(e.bias, col, e.bias_dtype);
+    if (e.residual) r[0] = widened(e.residual, row * e.ldr + col, e.y_dtype);
+    scale_and_bias(e, v, rs, cs, b);
+    activate(e.act, v);
+    if (e.residual) add_residual(v, r);
+    if (e.y_dtype == TBIK_F32) reinterpret_cast<float *>(Y)[row * ldy + col] = v[0];
+    else reinterpret_cast<uint16_t *>(Y)[row * ldy + col] = (uint16_t)pack_16x2(v[0], 0.0f, e.y_dtype == TBIK_F16);
+}
+
+}  // namespace tbik

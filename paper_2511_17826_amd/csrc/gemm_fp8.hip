@@ -25,6 +25,7 @@
 #include "tbik_device.hpp"
 #include "mx_scales.hpp"
 #include "tbik_internal.hpp"
+#include "tile_epilogue.hpp"
 #include "tile_store.hpp"
 #include "tree_walk.hpp"
 
@@ -53,12 +54,12 @@ __device__ __forceinline__ f32x16 mfma_32x32x64_8bit_scaled(i32x8 a, i32x8 b, f3
 
 constexpr int REF_MAX_LEVELS = 28;
 
-template <int FMT, bool MX>
+template <int FMT, bool MX, bool EPI>
 __global__ __launch_bounds__(64) void gemm_fp8_reference_kernel(
         const uint8_t *__restrict__ X, int64_t ldx, const uint8_t *__restrict__ Wt, int64_t ldw,
         const uint8_t *__restrict__ Xs, int64_t ldxs, const uint8_t *__restrict__ Ws, int64_t ldws,   // MX only
-        float *__restrict__ partials, void *__restrict__ Y, int64_t ldy, int y_dtype,
-        int M, int N, int superleaf, int ns_per_shard) {
+        float *__restrict__ partials, void *Y, int64_t ldy, int y_dtype,
+        int M, int N, int superleaf, int ns_per_shard, const ReferenceEpilogue<EPI> epilogue) {
     const int lane = threadIdx.x;
     const int i = lane & 31;      // row of X / row of Wt (= output column) held by this lane
     const int g = lane >> 5;      // which half of a step of 64 k
@@ -112,10 +113,14 @@ __global__ __launch_bounds__(64) void gemm_fp8_reference_kernel(
     for (int r = 0; r < 16; ++r) {
         const int row = m0 + 8 * (r >> 2) + 4 * g + (r & 3);
         if (row >= M) continue;
-        if (partials) partials[((int64_t)p * M + row) * N + col] = acc[r];
-        if (Y) {
-            if (y_dtype == TBIK_F32) reinterpret_cast<float *>(Y)[(int64_t)row * ldy + col] = acc[r];
-            else reinterpret_cast<uint16_t *>(Y)[(int64_t)row * ldy + col] = (uint16_t)f32_to_bf16_bits(acc[r]);
+        if constexpr (EPI) {
+            finish_and_store(epilogue, acc[r], Y, ldy, row, col);
+        } else {
+            if (partials) partials[((int64_t)p * M + row) * N + col] = acc[r];
+            if (Y) {
+                if (y_dtype == TBIK_F32) reinterpret_cast<float *>(Y)[(int64_t)row * ldy + col] = acc[r];
+                else reinterpret_cast<uint16_t *>(Y)[(int64_t)row * ldy + col] = (uint16_t)f32_to_bf16_bits(acc[r]);
+            }
         }
     }
 }
@@ -158,10 +163,14 @@ struct Fp8Params {
     int vector_stores;
     int stream_stores;
 };
+struct Fp8EpilogueParams : Fp8Params {
+    EpilogueParams epilogue;
+};
 
-template <int LEVELS, int WM, int WN, int MT, int NT, int RING8, int FMT, bool MX>
+// EPI: the output passes through an epilogue (epilogue.hpp); P == 1 then.
+template <int LEVELS, int WM, int WN, int MT, int NT, int RING8, int FMT, bool MX, bool EPI>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
-void gemm_fp8_tiled_kernel(const Fp8Params p) {
+void gemm_fp8_tiled_kernel(const std::conditional_t<EPI, Fp8EpilogueParams, Fp8Params> p) {
     constexpr int BM = 32 * MT * WM, BN = 32 * NT * WN;
     static_assert(BN == 128 && WM * WN == 4, "tile shape");
     constexpr int A_LOADS8 = BM / 32;                           // 1 KiB loads of X rows per wavefront and stage
@@ -410,7 +419,22 @@ void gemm_fp8_tiled_kernel(const Fp8Params p) {
         const int m0 = (tile / p.tiles_n) * BM, n0 = (tile % p.tiles_n) * BN;
         float *part = p.partials ? p.partials + (int64_t)shard * p.M * p.N : nullptr;
         const bool interior = (m0 + BM <= p.M) && (n0 + BN <= p.N);
-        if (interior && p.vector_stores) {
+        if constexpr (EPI) {                                // the patch and its barrier as below
+            const int wm_u = wave_u / WN, wn_u = wave_u % WN;
+            const int row0 = m0 + wm_u * MT * 32, col0 = n0 + wn_u * WCOLS;
+            const int last_slot = cur == 0 ? RING8 - 1 : cur - 1;
+            float *patch = reinterpret_cast<float *>(smem + last_slot * STAGE8 + wave * REGION8);
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            stores_in_flight = -1;
+            if (interior && p.vector_stores) {
+                store_with_epilogue<true>(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, 0, lane);
+                stores_in_flight = p.epilogue.y_dtype == TBIK_F32 ? STORES_F32 : STORES_BF16;
+            } else if (n0 + BN <= p.N && p.vector_stores) {
+                store_with_epilogue<false>(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, p.M - 1 - row0, lane);
+            } else {
+                store_elements_with_epilogue(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, p.M, p.N, lane);
+            }
+        } else if (interior && p.vector_stores) {
             // Each wavefront turns its 32 x 64 blocks around in its own region of the slot that was multiplied last
             // (nothing is loaded into it before the next stage's barrier; the barrier here is for the other wavefronts'
             // fragment reads), so that a lane stores 16 consecutive bytes.  A fixed number of store instructions.
@@ -544,12 +568,13 @@ int compute_units() {
     return cus;
 }
 
-template <int WM, int WN, int MT, int NT, int RING8, int FMT, bool MX>
+template <int WM, int WN, int MT, int NT, int RING8, int FMT, bool MX, bool EPI>
 hipError_t launch_tiled_fmt(const GemmArgs &a, const Mxfp4Scales *sc, hipStream_t s) {
     constexpr int BM = 32 * MT * WM, BN = 32 * NT * WN;
     constexpr int STAGE8 = 4 * (BM / 32 + B_LOADS8) * 1024 + (MX ? 1024 : 0);
     static_assert(RING8 * STAGE8 <= 160 * 1024, "LDS of a compute unit");
-    Fp8Params p;
+    std::conditional_t<EPI, Fp8EpilogueParams, Fp8Params> p;
+    if constexpr (EPI) p.epilogue = *a.epilogue;
     p.X = reinterpret_cast<const uint8_t *>(a.X); p.Wt = reinterpret_cast<const uint8_t *>(a.W);
     p.Xs = MX ? sc->Xs : nullptr; p.Ws = MX ? sc->Ws : nullptr;
     p.ldxs = MX ? sc->ldxs : 0; p.ldws = MX ? sc->ldws : 0;
@@ -573,13 +598,14 @@ hipError_t launch_tiled_fmt(const GemmArgs &a, const Mxfp4Scales *sc, hipStream_
     const void *out = p.partials ? (const void *)p.partials : p.Y;
     const int64_t ld_bytes = p.partials ? (int64_t)a.N * 4 : a.ldy * (p.y_bf16 ? 2 : 4);
     p.vector_stores = ((reinterpret_cast<uintptr_t>(out) & 15) == 0) && (ld_bytes % 16 == 0) && ld_bytes < kMaxVectorRowBytes;
+    if (EPI && !residual_in_vectors(*a.epilogue)) p.vector_stores = 0;
     p.stream_stores = a.partials != nullptr && (int64_t)a.P * a.M * a.N * 4 > ((int64_t)192 << 20);
     const int levels = levels_for(p.ns_per_shard);
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 32) dev = 32;
 #define TBIK_LAUNCH8(L)                                                                                  \
     case L: {                                                                                            \
-        auto k = gemm_fp8_tiled_kernel<L, WM, WN, MT, NT, RING8, FMT, MX>;                               \
+        auto k = gemm_fp8_tiled_kernel<L, WM, WN, MT, NT, RING8, FMT, MX, EPI>;                          \
         static std::atomic<unsigned> lds_allowed{0};                                                     \
         if (dev >= 32 || !((lds_allowed.load(std::memory_order_relaxed) >> dev) & 1u)) {                 \
             hipError_t e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds); \
@@ -604,18 +630,18 @@ hipError_t launch_tiled_fmt(const GemmArgs &a, const Mxfp4Scales *sc, hipStream_
 }  // namespace
 
 // rows: 128, 64 or 32 rows per workgroup tile (the caller's choice; the bits do not depend on it)
-template <int FMT>
+template <int FMT, bool EPI>
 static hipError_t launch_rows(const GemmArgs &a, int rows, hipStream_t s) {
-    if (rows == 32) return launch_tiled_fmt<1, 4, 1, 1, 8, FMT, false>(a, nullptr, s);   // 8 x 20 KiB slots: deep prefetch for weight streaming
-    if (rows == 64) return launch_tiled_fmt<1, 4, 2, 1, 6, FMT, false>(a, nullptr, s);   // 6 x 24 KiB
-    return launch_tiled_fmt<2, 2, 2, 2, 5, FMT, false>(a, nullptr, s);                   // 5 x 32 KiB
+    if (rows == 32) return launch_tiled_fmt<1, 4, 1, 1, 8, FMT, false, EPI>(a, nullptr, s);   // 8 x 20 KiB slots: deep prefetch for weight streaming
+    if (rows == 64) return launch_tiled_fmt<1, 4, 2, 1, 6, FMT, false, EPI>(a, nullptr, s);   // 6 x 24 KiB
+    return launch_tiled_fmt<2, 2, 2, 2, 5, FMT, false, EPI>(a, nullptr, s);                   // 5 x 32 KiB
 }
 // With block scales a slot is 1 KiB larger: one slot fewer where the ring filled LDS.
-template <int FMT>
+template <int FMT, bool EPI>
 static hipError_t launch_rows_mx(const GemmArgs &a, const Mxfp4Scales &sc, int rows, hipStream_t s) {
-    if (rows == 32) return launch_tiled_fmt<1, 4, 1, 1, 7, FMT, true>(a, &sc, s);        // 7 x 21 KiB
-    if (rows == 64) return launch_tiled_fmt<1, 4, 2, 1, 6, FMT, true>(a, &sc, s);        // 6 x 25 KiB
-    return launch_tiled_fmt<2, 2, 2, 2, 4, FMT, true>(a, &sc, s);                        // 4 x 33 KiB
+    if (rows == 32) return launch_tiled_fmt<1, 4, 1, 1, 7, FMT, true, EPI>(a, &sc, s);        // 7 x 21 KiB
+    if (rows == 64) return launch_tiled_fmt<1, 4, 2, 1, 6, FMT, true, EPI>(a, &sc, s);        // 6 x 25 KiB
+    return launch_tiled_fmt<2, 2, 2, 2, 4, FMT, true, EPI>(a, &sc, s);                        // 4 x 33 KiB
 }
 
 bool gemm_fp8_tiled_supports(const GemmArgs &a) {
@@ -628,7 +654,8 @@ bool gemm_fp8_tiled_supports(const GemmArgs &a) {
 hipError_t launch_gemm_fp8_tiled(const GemmArgs &a, int rows, hipStream_t s) {
     if (a.M <= 0 || a.N <= 0) return hipSuccess;
     if (!gemm_fp8_tiled_supports(a) || (rows != 32 && rows != 64 && rows != 128)) return hipErrorInvalidValue;
-    return a.x_dtype == TBIK_FP8_E5M2 ? launch_rows<1>(a, rows, s) : launch_rows<0>(a, rows, s);
+    if (a.epilogue) return a.x_dtype == TBIK_FP8_E5M2 ? launch_rows<1, true>(a, rows, s) : launch_rows<0, true>(a, rows, s);
+    return a.x_dtype == TBIK_FP8_E5M2 ? launch_rows<1, false>(a, rows, s) : launch_rows<0, false>(a, rows, s);
 }
 
 hipError_t launch_gemm_fp8_reference(const GemmArgs &a, hipStream_t s) {
@@ -637,10 +664,14 @@ hipError_t launch_gemm_fp8_reference(const GemmArgs &a, hipStream_t s) {
     dim3 grid((a.N + 31) / 32, (a.M + 31) / 32, a.P);
     if (grid.y > 65535u || grid.z > 65535u) return hipErrorInvalidValue;
     void *Y = (a.P == 1) ? a.Y : nullptr;
-    auto kernel = (a.x_dtype == TBIK_FP8_E5M2) ? gemm_fp8_reference_kernel<1, false> : gemm_fp8_reference_kernel<0, false>;
-    hipLaunchKernelGGL(kernel, grid, dim3(64), 0, s, reinterpret_cast<const uint8_t *>(a.X), a.ldx,
-                       reinterpret_cast<const uint8_t *>(a.W), a.ldw, nullptr, 0, nullptr, 0, a.partials, Y, a.ldy, a.y_dtype,
-                       a.M, a.N, a.superleaf, a.ns / a.P);
+    auto launch = [&](auto kernel, auto epilogue) {
+        hipLaunchKernelGGL(kernel, grid, dim3(64), 0, s, reinterpret_cast<const uint8_t *>(a.X), a.ldx,
+                           reinterpret_cast<const uint8_t *>(a.W), a.ldw, nullptr, 0, nullptr, 0, a.partials, Y, a.ldy, a.y_dtype,
+                           a.M, a.N, a.superleaf, a.ns / a.P, epilogue);
+    };
+    const bool e5m2 = a.x_dtype == TBIK_FP8_E5M2;
+    if (a.epilogue) launch(e5m2 ? gemm_fp8_reference_kernel<1, false, true> : gemm_fp8_reference_kernel<0, false, true>, *a.epilogue);
+    else launch(e5m2 ? gemm_fp8_reference_kernel<1, false, false> : gemm_fp8_reference_kernel<0, false, false>, ReferenceEpilogue<false>{});
     return hipGetLastError();
 }
 
@@ -663,7 +694,8 @@ hipError_t launch_mxfp8_retile(const Mxfp4Scales &raw, int M, int N, int K, void
 hipError_t launch_gemm_mxfp8_tiled(const GemmArgs &a, const Mxfp4Scales &sc, int rows, hipStream_t s) {
     if (a.M <= 0 || a.N <= 0) return hipSuccess;
     if (!gemm_mxfp8_tiled_supports(a, sc) || (rows != 32 && rows != 64 && rows != 128)) return hipErrorInvalidValue;
-    return a.x_dtype == TBIK_FP8_E5M2 ? launch_rows_mx<1>(a, sc, rows, s) : launch_rows_mx<0>(a, sc, rows, s);
+    if (a.epilogue) return a.x_dtype == TBIK_FP8_E5M2 ? launch_rows_mx<1, true>(a, sc, rows, s) : launch_rows_mx<0, true>(a, sc, rows, s);
+    return a.x_dtype == TBIK_FP8_E5M2 ? launch_rows_mx<1, false>(a, sc, rows, s) : launch_rows_mx<0, false>(a, sc, rows, s);
 }
 
 hipError_t launch_gemm_mxfp8_reference(const GemmArgs &a, const Mxfp4Scales &sc, hipStream_t s) {
@@ -672,10 +704,14 @@ hipError_t launch_gemm_mxfp8_reference(const GemmArgs &a, const Mxfp4Scales &sc,
     dim3 grid((a.N + 31) / 32, (a.M + 31) / 32, a.P);
     if (grid.y > 65535u || grid.z > 65535u) return hipErrorInvalidValue;
     void *Y = (a.P == 1) ? a.Y : nullptr;
-    auto kernel = (a.x_dtype == TBIK_FP8_E5M2) ? gemm_fp8_reference_kernel<1, true> : gemm_fp8_reference_kernel<0, true>;
-    hipLaunchKernelGGL(kernel, grid, dim3(64), 0, s, reinterpret_cast<const uint8_t *>(a.X), a.ldx,
-                       reinterpret_cast<const uint8_t *>(a.W), a.ldw, sc.Xs, sc.ldxs, sc.Ws, sc.ldws, a.partials, Y, a.ldy,
-                       a.y_dtype, a.M, a.N, a.superleaf, a.ns / a.P);
+    auto launch = [&](auto kernel, auto epilogue) {
+        hipLaunchKernelGGL(kernel, grid, dim3(64), 0, s, reinterpret_cast<const uint8_t *>(a.X), a.ldx,
+                           reinterpret_cast<const uint8_t *>(a.W), a.ldw, sc.Xs, sc.ldxs, sc.Ws, sc.ldws, a.partials, Y, a.ldy, a.y_dtype,
+                           a.M, a.N, a.superleaf, a.ns / a.P, epilogue);
+    };
+    const bool e5m2 = a.x_dtype == TBIK_FP8_E5M2;
+    if (a.epilogue) launch(e5m2 ? gemm_fp8_reference_kernel<1, true, true> : gemm_fp8_reference_kernel<0, true, true>, *a.epilogue);
+    else launch(e5m2 ? gemm_fp8_reference_kernel<1, true, false> : gemm_fp8_reference_kernel<0, true, false>, ReferenceEpilogue<false>{});
     return hipGetLastError();
 }
 

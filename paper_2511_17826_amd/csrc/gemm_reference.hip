@@ -7,6 +7,7 @@
 // of 16 k into an accumulator that starts at +0; after each superleaf the carry-over step of Alg. 1 folds the accumulator into the stash of
 // waiting subtrees.  The tuned kernels issue the same MFMA opcode over the same k -> (step, slot)
 // map and the same fp32 additions, so they must reproduce this kernel's bits.
+#include "epilogue.hpp"
 #include "tbik_device.hpp"
 #include "tbik_internal.hpp"
 
@@ -14,11 +15,11 @@ namespace tbik {
 
 constexpr int REF_MAX_LEVELS = 28;
 
-template <bool F16>
+template <bool F16, bool EPI>
 __global__ __launch_bounds__(64) void gemm_reference_kernel(
         const uint16_t *__restrict__ X, int64_t ldx, const uint16_t *__restrict__ W, int64_t ldw,
-        float *__restrict__ partials, void *__restrict__ Y, int64_t ldy, int y_dtype,
-        int M, int N, int K, int superleaf, int ns_per_shard) {
+        float *__restrict__ partials, void *Y, int64_t ldy, int y_dtype,
+        int M, int N, int K, int superleaf, int ns_per_shard, const ReferenceEpilogue<EPI> epilogue) {
     const int lane = threadIdx.x;
     const int i = lane & 31;      // row of A / column of B held by this lane
     const int g = lane >> 5;      // which group of 8 k inside a step of 16
@@ -68,10 +69,14 @@ __global__ __launch_bounds__(64) void gemm_reference_kernel(
     for (int r = 0; r < 16; ++r) {
         const int row = m0 + 8 * (r >> 2) + 4 * g + (r & 3);
         if (row >= M) continue;
-        if (partials) partials[((int64_t)p * M + row) * N + col] = acc[r];
-        if (Y) {
-            if (y_dtype == TBIK_F32) reinterpret_cast<float *>(Y)[(int64_t)row * ldy + col] = acc[r];
-            else reinterpret_cast<uint16_t *>(Y)[(int64_t)row * ldy + col] = (uint16_t)f32_to_16_bits<F16>(acc[r]);
+        if constexpr (EPI) {
+            finish_and_store(epilogue, acc[r], Y, ldy, row, col);
+        } else {
+            if (partials) partials[((int64_t)p * M + row) * N + col] = acc[r];
+            if (Y) {
+                if (y_dtype == TBIK_F32) reinterpret_cast<float *>(Y)[(int64_t)row * ldy + col] = acc[r];
+                else reinterpret_cast<uint16_t *>(Y)[(int64_t)row * ldy + col] = (uint16_t)f32_to_16_bits<F16>(acc[r]);
+            }
         }
     }
 }
@@ -81,9 +86,13 @@ hipError_t launch_gemm_reference(const GemmArgs &a, hipStream_t s) {
     dim3 grid((a.N + 31) / 32, (a.M + 31) / 32, a.P);
     if (grid.y > 65535u || grid.z > 65535u) return hipErrorInvalidValue;
     void *Y = (a.P == 1) ? a.Y : nullptr;
-    auto kernel = (a.x_dtype == TBIK_F16) ? gemm_reference_kernel<true> : gemm_reference_kernel<false>;
-    hipLaunchKernelGGL(kernel, grid, dim3(64), 0, s, a.X, a.ldx, a.W, a.ldw, a.partials, Y, a.ldy,
-                       a.y_dtype, a.M, a.N, a.K, a.superleaf, a.ns / a.P);
+    auto launch = [&](auto kernel, auto epilogue) {
+        hipLaunchKernelGGL(kernel, grid, dim3(64), 0, s, a.X, a.ldx, a.W, a.ldw, a.partials, Y, a.ldy,
+                           a.y_dtype, a.M, a.N, a.K, a.superleaf, a.ns / a.P, epilogue);
+    };
+    const bool f16 = a.x_dtype == TBIK_F16;
+    if (a.epilogue) launch(f16 ? gemm_reference_kernel<true, true> : gemm_reference_kernel<false, true>, *a.epilogue);
+    else launch(f16 ? gemm_reference_kernel<true, false> : gemm_reference_kernel<false, false>, ReferenceEpilogue<false>{});
     return hipGetLastError();
 }
 

@@ -13,6 +13,7 @@
 #include <atomic>
 #include <type_traits>
 
+#include "epilogue.hpp"
 #include "tbik_device.hpp"
 #include "tbik_internal.hpp"
 
@@ -52,6 +53,9 @@ struct SliceParams {
     int steps_per_leaf;                 // superleaf / step_k
     int leaves_per_wave, active_waves;
 };
+struct SliceEpilogueParams : SliceParams {
+    EpilogueParams epilogue;
+};
 
 template <int N>
 __device__ __forceinline__ void slice_wait_loads() {
@@ -80,8 +84,9 @@ __device__ __forceinline__ float slice_tree(const float *red, int active) {
     return v[0];
 }
 
-template <int FMT, bool MX, int GROUPS, int WAVES, int RING>
-__global__ __launch_bounds__(64 * WAVES) void gemm_slice_kernel(const SliceParams p) {
+// EPI: the output passes through an epilogue (epilogue.hpp).
+template <int FMT, bool MX, int GROUPS, int WAVES, int RING, bool EPI>
+__global__ __launch_bounds__(64 * WAVES) void gemm_slice_kernel(const std::conditional_t<EPI, SliceEpilogueParams, SliceParams> p) {
     using F = SliceFormat<FMT, MX>;
     constexpr int DATA_BYTES = (1 + GROUPS) * F::group_bytes, STEP_BYTES = DATA_BYTES + (MX ? 512 : 0);
     constexpr int LOADS = (1 + GROUPS) * F::group_loads + (MX ? 2 : 0);
@@ -255,17 +260,19 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_slice_kernel(const SliceParam
     const int row = threadIdx.x >> 4, col = n0 + (threadIdx.x & 15);
     if (threadIdx.x >= 512 || row >= p.M || col >= p.N) return;
     const float v = slice_tree<WAVES>(red + threadIdx.x, p.active_waves);
-    if (p.y_bf16) reinterpret_cast<uint16_t *>(p.Y)[(int64_t)row * p.ldy + col] = (uint16_t)f32_to_bf16_bits(v);
+    if constexpr (EPI) finish_and_store(p.epilogue, v, p.Y, p.ldy, row, col);
+    else if (p.y_bf16) reinterpret_cast<uint16_t *>(p.Y)[(int64_t)row * p.ldy + col] = (uint16_t)f32_to_bf16_bits(v);
     else reinterpret_cast<float *>(p.Y)[(int64_t)row * p.ldy + col] = v;
 }
 
 constexpr int SLICE_WAVES = 8;
 inline int64_t slices_of(int N) { return ((int64_t)N + 15) / 16; }
 
-template <int FMT, bool MX, int GROUPS, int RING, int WAVES = SLICE_WAVES>
+template <int FMT, bool MX, int GROUPS, int RING, bool EPI, int WAVES = SLICE_WAVES>
 hipError_t launch_slice_of(const GemmArgs &a, const Mxfp4Scales &sc, hipStream_t s) {
     using F = SliceFormat<FMT, MX>;
-    SliceParams p;
+    std::conditional_t<EPI, SliceEpilogueParams, SliceParams> p;
+    if constexpr (EPI) p.epilogue = *a.epilogue;
     p.X = reinterpret_cast<const uint8_t *>(a.X); p.Wt = reinterpret_cast<const uint8_t *>(a.W);
     p.Xs = sc.Xs; p.Ws = sc.Ws;
     p.Y = a.Y;
@@ -277,7 +284,7 @@ hipError_t launch_slice_of(const GemmArgs &a, const Mxfp4Scales &sc, hipStream_t
     p.active_waves = a.ns > WAVES ? WAVES : a.ns;
     constexpr int lds = WAVES * RING * ((1 + GROUPS) * F::group_bytes + (MX ? 512 : 0));
     static_assert(lds <= 160 * 1024 && lds >= WAVES * 2048, "LDS of a compute unit; room for the sums");
-    auto k = gemm_slice_kernel<FMT, MX, GROUPS, WAVES, RING>;
+    auto k = gemm_slice_kernel<FMT, MX, GROUPS, WAVES, RING, EPI>;
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 32) dev = 32;      // 32: not remembered, set every time
     static std::atomic<unsigned> lds_allowed{0};                                 // bit d: the attribute is set on device d
@@ -293,12 +300,12 @@ hipError_t launch_slice_of(const GemmArgs &a, const Mxfp4Scales &sc, hipStream_t
 // Steps in flight: all that LDS holds while every workgroup has a compute unit to itself; with more of them than compute units
 // two, which lets two workgroups share one (16 rows of 4096 x 6144 in 8 bits 10.4 -> 8.8 us; 17 .. 32 rows and 6-bit steps are
 // too large for that).
-template <int FMT, bool MX>
+template <int FMT, bool MX, bool EPI = false>
 hipError_t launch_slice_rows(const GemmArgs &a, const Mxfp4Scales &sc, hipStream_t s) {
     constexpr bool six_bits = FMT == 2 || FMT == 3;
-    if (a.M > 16) return launch_slice_of<FMT, MX, 2, six_bits ? 2 : 3>(a, sc, s);
-    if (!six_bits && slices_of(a.N) > 256) return launch_slice_of<FMT, MX, 1, 2>(a, sc, s);
-    return launch_slice_of<FMT, MX, 1, six_bits ? 3 : 4>(a, sc, s);
+    if (a.M > 16) return launch_slice_of<FMT, MX, 2, six_bits ? 2 : 3, EPI>(a, sc, s);
+    if (!six_bits && slices_of(a.N) > 256) return launch_slice_of<FMT, MX, 1, 2, EPI>(a, sc, s);
+    return launch_slice_of<FMT, MX, 1, six_bits ? 3 : 4, EPI>(a, sc, s);
 }
 
 }  // namespace
@@ -370,6 +377,11 @@ hipError_t launch_gemm_slice(const GemmArgs &a, const Mxfp4Scales *sc, hipStream
     if (!gemm_slice_takes(a, sc)) return hipErrorInvalidValue;
     static const Mxfp4Scales none{};
     const Mxfp4Scales &scales = sc ? *sc : none;
+    if (a.epilogue) {
+        if (a.x_dtype == TBIK_FP8_E4M3) return sc ? launch_slice_rows<0, true, true>(a, scales, s) : launch_slice_rows<0, false, true>(a, scales, s);
+        if (a.x_dtype == TBIK_FP8_E5M2) return sc ? launch_slice_rows<1, true, true>(a, scales, s) : launch_slice_rows<1, false, true>(a, scales, s);
+        return hipErrorInvalidValue;
+    }
     switch (a.x_dtype) {
         case TBIK_FP8_E4M3: return sc ? launch_slice_rows<0, true>(a, scales, s) : launch_slice_rows<0, false>(a, scales, s);
         case TBIK_FP8_E5M2: return sc ? launch_slice_rows<1, true>(a, scales, s) : launch_slice_rows<1, false>(a, scales, s);

@@ -21,6 +21,7 @@
 
 #include "tbik_device.hpp"
 #include "tbik_internal.hpp"
+#include "tile_epilogue.hpp"
 #include "tile_store.hpp"
 #include "tree_walk.hpp"
 
@@ -67,6 +68,9 @@ struct TiledParams {
     int stream_stores;          // fp32 outputs bypass the caches (partials too large to stay there until they are combined)
     int swiglu;                 // W is [gate | up] ([K, 2 I], N = 2 I); Y is act [M, I] = SiLU(gate) * up, 16-bit
 };
+struct TiledEpilogueParams : TiledParams {
+    EpilogueParams epilogue;
+};
 
 // ---------------------------------------------------------------------------------------------
 // BM = 32*MT*WM rows, BN = 32*NT*WN columns, WM*WN = 4 wavefronts.
@@ -76,9 +80,10 @@ struct TiledParams {
 // RING: LDS stage slots; RING - 3 stages of loads are in flight at a stage's entry, one more is issued during it.
 // F16: the operands (and a 16-bit output) are IEEE binary16 instead of bf16; only the MFMA opcode and the output
 // conversion differ.
-template <int LEVELS, int WM, int WN, int MT, int NT, int RING, bool F16>
+// EPI: the output passes through an epilogue (epilogue.hpp); P == 1 then, and no gated activation.
+template <int LEVELS, int WM, int WN, int MT, int NT, int RING, bool F16, bool EPI>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
-void gemm_tiled_kernel(const TiledParams p) {
+void gemm_tiled_kernel(const std::conditional_t<EPI, TiledEpilogueParams, TiledParams> p) {
     constexpr int BM = 32 * MT * WM, BN = 32 * NT * WN;
     static_assert(BN == BN_TILE && WM * WN == 4, "tile shape");
     constexpr int A_LOADS = BM / 32;          // 1 KiB loads per wavefront and stage: BM rows / 8 rows / 4 wavefronts
@@ -317,7 +322,22 @@ void gemm_tiled_kernel(const TiledParams p) {
         const int m0 = (tile / p.tiles_n) * BM, n0 = (tile % p.tiles_n) * BN;
         float *part = p.partials ? p.partials + (int64_t)shard * p.M * p.N : nullptr;
         const bool interior = (m0 + BM <= p.M) && (n0 + BN <= p.N);
-        if (interior && p.vector_stores) {
+        if constexpr (EPI) {                                // the patch and its barrier as below
+            const int wm_u = wave_u / WN, wn_u = wave_u % WN;
+            const int row0 = m0 + wm_u * MT * 32, col0 = n0 + wn_u * WCOLS;
+            const int last_slot = cur == 0 ? RING - 1 : cur - 1;
+            float *patch = reinterpret_cast<float *>(smem + last_slot * STAGE_BYTES + wave * REGION_BYTES);
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            stores_in_flight = -1;
+            if (interior && p.vector_stores) {
+                store_with_epilogue<true>(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, 0, lane);
+                stores_in_flight = p.epilogue.y_dtype == TBIK_F32 ? STORES_F32 : STORES_BF16;
+            } else if (n0 + BN <= p.N && p.vector_stores) {
+                store_with_epilogue<false>(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, p.M - 1 - row0, lane);
+            } else {
+                store_elements_with_epilogue(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, p.M, p.N, lane);
+            }
+        } else if (interior && p.vector_stores) {
             // Full tile, 16-byte aligned rows: each wavefront turns its 32 x (32*NT) blocks around in its private LDS
             // patch, so that a lane holds 4 (fp32) or 8 (bf16) consecutive columns and stores 16 bytes.  The number of
             // store instructions is fixed (no lane masks, no branches), which the load accounting above relies on.
@@ -529,10 +549,11 @@ static int compute_units() {
     return cus;
 }
 
-template <int WM, int WN, int MT, int NT, int RING, bool F16>
+template <int WM, int WN, int MT, int NT, int RING, bool F16, bool EPI>
 static hipError_t launch_shape(const GemmArgs &a, hipStream_t s) {
     constexpr int BM = 32 * MT * WM, BN = 32 * NT * WN;
-    TiledParams p;
+    std::conditional_t<EPI, TiledEpilogueParams, TiledParams> p;
+    if constexpr (EPI) p.epilogue = *a.epilogue;
     p.X = a.X; p.W = a.W; p.partials = a.partials; p.Y = (a.P == 1) ? a.Y : nullptr;
     p.ldx = a.ldx; p.ldw = a.ldw; p.ldy = a.ldy;
     p.M = a.M; p.N = a.N;
@@ -553,6 +574,7 @@ static hipError_t launch_shape(const GemmArgs &a, hipStream_t s) {
         const void *out = p.partials ? (const void *)p.partials : p.Y;
         const int64_t ld_bytes = p.partials ? (int64_t)a.N * 4 : a.ldy * (p.y_bf16 ? 2 : 4);   // act: 16-byte chunks of 8 channels
         p.vector_stores = ((reinterpret_cast<uintptr_t>(out) & 15) == 0) && (ld_bytes % 16 == 0) && ld_bytes < kMaxVectorRowBytes;
+        if (EPI && !residual_in_vectors(*a.epilogue)) p.vector_stores = 0;
         // Partials of many shards exceed the 256 MiB memory-side cache before the combine reads them: written around
         // the caches they do not evict the operands (P = 8 at 4096^2: 257 -> 170 us).  Fewer planes stay cached for
         // their reader, so those keep ordinary stores.
@@ -563,7 +585,7 @@ static hipError_t launch_shape(const GemmArgs &a, hipStream_t s) {
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 32) dev = 32;   // 32: not remembered, set every time
 #define TBIK_LAUNCH(L)                                                                                   \
     case L: {                                                                                            \
-        auto k = gemm_tiled_kernel<L, WM, WN, MT, NT, RING, F16>;                                            \
+        auto k = gemm_tiled_kernel<L, WM, WN, MT, NT, RING, F16, EPI>;                                       \
         static std::atomic<unsigned> lds_allowed{0};   /* bit d: the attribute is set on device d */     \
         if (dev >= 32 || !((lds_allowed.load(std::memory_order_relaxed) >> dev) & 1u)) {                 \
             hipError_t e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds); \
@@ -585,19 +607,24 @@ static hipError_t launch_shape(const GemmArgs &a, hipStream_t s) {
     return hipGetLastError();
 }
 
+template <bool F16, bool EPI>
+static hipError_t launch_variant(const GemmArgs &a, int variant, hipStream_t s) {
+    // 128 x 128, wave tile 64 x 64, 5 x 32 KiB stage slots = all of LDS
+    if (variant == VARIANT_T128) return launch_shape<2, 2, 2, 2, 5, F16, EPI>(a, s);
+    // 96 x 128, wave tile 96 x 32, 5 x 28 KiB: batches of 65..96 rows, a quarter fewer MFMAs than a 128-row tile and
+    // the same W stream (77 rows of 4096 x 6144 21.0 -> 18.3 us); bound by MFMA and LDS reads, four for three MFMAs
+    if (variant == VARIANT_T96) return launch_shape<1, 4, 3, 1, 5, F16, EPI>(a, s);
+    // 64 x 128, wave tile 64 x 32, 6 x 24 KiB: batches of 33..64 rows without the idle upper half of a 128-row tile
+    if (variant == VARIANT_T64) return launch_shape<1, 4, 2, 1, 6, F16, EPI>(a, s);
+    // 32 x 128, wave tile 32 x 32, 6 x 20 KiB: deep prefetch for weight streaming
+    return launch_shape<1, 4, 1, 1, 6, F16, EPI>(a, s);
+}
+
 hipError_t launch_gemm_tiled(const GemmArgs &a, int variant, hipStream_t s) {
     if (a.M <= 0 || a.N <= 0) return hipSuccess;
     if (!gemm_tiled_supports(a, variant)) return hipErrorInvalidValue;
-    const bool f16 = (a.x_dtype == TBIK_F16);
-    // 128 x 128, wave tile 64 x 64, 5 x 32 KiB stage slots = all of LDS
-    if (variant == VARIANT_T128) return f16 ? launch_shape<2, 2, 2, 2, 5, true>(a, s) : launch_shape<2, 2, 2, 2, 5, false>(a, s);
-    // 96 x 128, wave tile 96 x 32, 5 x 28 KiB: batches of 65..96 rows, a quarter fewer MFMAs than a 128-row tile and
-    // the same W stream (77 rows of 4096 x 6144 21.0 -> 18.3 us); bound by MFMA and LDS reads, four for three MFMAs
-    if (variant == VARIANT_T96) return f16 ? launch_shape<1, 4, 3, 1, 5, true>(a, s) : launch_shape<1, 4, 3, 1, 5, false>(a, s);
-    // 64 x 128, wave tile 64 x 32, 6 x 24 KiB: batches of 33..64 rows without the idle upper half of a 128-row tile
-    if (variant == VARIANT_T64) return f16 ? launch_shape<1, 4, 2, 1, 6, true>(a, s) : launch_shape<1, 4, 2, 1, 6, false>(a, s);
-    // 32 x 128, wave tile 32 x 32, 6 x 20 KiB: deep prefetch for weight streaming
-    return f16 ? launch_shape<1, 4, 1, 1, 6, true>(a, s) : launch_shape<1, 4, 1, 1, 6, false>(a, s);
+    if (a.epilogue) return a.x_dtype == TBIK_F16 ? launch_variant<true, true>(a, variant, s) : launch_variant<false, true>(a, variant, s);
+    return a.x_dtype == TBIK_F16 ? launch_variant<true, false>(a, variant, s) : launch_variant<false, false>(a, variant, s);
 }
 
 }  // namespace tbik

@@ -356,6 +356,32 @@ int low_bit_kernel(const GemmArgs &a, const Mxfp4Scales *sc, int split) {
     return forced != VARIANT_REFERENCE && tiled ? KERNEL_TILED : KERNEL_REFERENCE;
 }
 
+// The caller's epilogue (nullptr: none) against the output it ends in.
+int check_epilogue(const tbik_epilogue *e, const void *Y, int64_t ldy, int y_dtype, int M, int N, EpilogueParams *p) {
+    if (!e) return TBIK_OK;
+    if (e->activation < TBIK_ACT_NONE || e->activation > TBIK_ACT_GELU_TANH) return TBIK_ERR_DTYPE;
+    if (e->bias && e->bias_dtype != TBIK_F32 && e->bias_dtype != TBIK_BF16 && e->bias_dtype != TBIK_F16) return TBIK_ERR_DTYPE;
+    *p = {e->row_scale, e->col_scale, e->bias, e->residual, e->residual ? e->ldr : 0, (int)e->bias_dtype, (int)e->activation, y_dtype};
+    if (M == 0 || N == 0) return TBIK_OK;
+    if (e->residual && (e->ldr < N || (e->residual == Y && e->ldr != ldy))) return TBIK_ERR_SHAPE;
+    if (!aligned(e->row_scale, 4) || !aligned(e->col_scale, 4) || (e->bias && !aligned(e->bias, e->bias_dtype == TBIK_F32 ? 4 : 2)) ||
+        !aligned(e->residual, y_dtype == TBIK_F32 ? 4 : 2))
+        return TBIK_ERR_ALIGN;
+    return TBIK_OK;
+}
+// How a piece of a batch ends: with the rows' part of the epilogue, in the product's kernel or in the combine of its K split.
+struct PieceEnd {
+    const bool with_epilogue;
+    const EpilogueParams params;
+    PieceEnd(const tbik_epilogue *epilogue, const EpilogueParams &ends, int m0, GemmArgs *a) : with_epilogue(epilogue != nullptr), params(epilogue ? ends.from_row(m0) : EpilogueParams{}) {
+        a->epilogue = with_epilogue ? &params : nullptr;
+    }
+    PieceEnd(const PieceEnd &) = delete;
+    hipError_t combine(const float *partials, int P, void *y, int64_t ldy, int y_dtype, int m, int N, hipStream_t s) const {
+        return with_epilogue ? launch_tree_combine_epilogue(partials, P, params, y, ldy, m, N, s) : launch_tree_combine(partials, P, y, ldy, y_dtype, m, N, s);
+    }
+};
+
 // 16-bit output type that goes with an operand format.
 inline bool legal_y_dtype(int y_dtype, int x_dtype) { return y_dtype == TBIK_F32 || y_dtype == x_dtype; }
 
@@ -401,13 +427,17 @@ int gemm_shard_partials(int x_dtype, const void *X, int64_t ldx, const void *W, 
     return e == hipSuccess ? TBIK_OK : hip_fail(e);
 }
 
+// epilogue: nullptr, or what the output passes through (16-bit operands); so too in gemm_fp8 and gemm_mxfp8 below.
 int gemm(int x_dtype, const void *X, int64_t ldx, const void *W, int64_t ldw, void *Y, int64_t ldy,
          int y_dtype, int M, int N, int K, int leaf, int k_first,
-         void *workspace, size_t workspace_bytes, void *hip_stream) {
+         void *workspace, size_t workspace_bytes, void *hip_stream, const tbik_epilogue *epilogue = nullptr) {
     int sl, ns;
     int rc = check_tree(M, N, K, leaf, k_first, 1, &sl, &ns);
     if (rc != TBIK_OK) return rc;
     if (!legal_y_dtype(y_dtype, x_dtype)) return TBIK_ERR_DTYPE;
+    EpilogueParams ends;
+    rc = check_epilogue(epilogue, Y, ldy, y_dtype, M, N, &ends);
+    if (rc != TBIK_OK) return rc;
     if (M == 0 || N == 0) return TBIK_OK;
     rc = check_operands(x_dtype, X, ldx, W, ldw, N, K);
     if (rc != TBIK_OK) return rc;
@@ -423,6 +453,7 @@ int gemm(int x_dtype, const void *X, int64_t ldx, const void *W, int64_t ldw, vo
         void *y = static_cast<char *>(Y) + (int64_t)m0 * ldy * (y_dtype == TBIK_F32 ? 4 : 2);
         const char *x = static_cast<const char *>(X) + (int64_t)m0 * ldx * (x_dtype == TBIK_F32 ? 4 : 2);
         GemmArgs a{(const uint16_t *)x, ldx, (const uint16_t *)W, ldw, nullptr, y, ldy, y_dtype, m, N, K, sl, ns, 1, x_dtype};
+        const PieceEnd end(epilogue, ends, m0, &a);
         GemmArgs probe = a;
         probe.P = plan.split;
         const int v = pick_variant(probe, plan.rows);
@@ -431,8 +462,9 @@ int gemm(int x_dtype, const void *X, int64_t ldx, const void *W, int64_t ldw, vo
         a.partials = reinterpret_cast<float *>(workspace);
         a.Y = nullptr;
         a.P = plan.split;
+        a.epilogue = nullptr;
         hipError_t e = launch_tiled(a, v, s);
-        return e == hipSuccess ? launch_tree_combine(a.partials, plan.split, y, ldy, y_dtype, m, N, s) : e;
+        return e == hipSuccess ? end.combine(a.partials, plan.split, y, ldy, y_dtype, m, N, s) : e;
     };
     hipError_t e;
     if (x_dtype == TBIK_F32) {                          // its own split, unless the caller brought no room for it
@@ -477,6 +509,14 @@ int tbik_gemm_f16(const void *X, int64_t ldx, const void *W, int64_t ldw, void *
                   tbik_dtype y_dtype, int M, int N, int K, int leaf, int k_first,
                   void *workspace, size_t workspace_bytes, void *hip_stream) {
     return gemm(TBIK_F16, X, ldx, W, ldw, Y, ldy, (int)y_dtype, M, N, K, leaf, k_first, workspace, workspace_bytes, hip_stream);
+}
+
+int tbik_gemm_epilogue(const void *X, int64_t ldx, const void *W, int64_t ldw, const tbik_epilogue *epilogue, void *Y, int64_t ldy,
+                       tbik_dtype y_dtype, tbik_dtype x_dtype, int M, int N, int K, int leaf, int k_first,
+                       void *workspace, size_t workspace_bytes, void *hip_stream) {
+    if (x_dtype != TBIK_BF16 && x_dtype != TBIK_F16) return TBIK_ERR_DTYPE;
+    if (!epilogue) return TBIK_ERR_NULL;
+    return gemm((int)x_dtype, X, ldx, W, ldw, Y, ldy, (int)y_dtype, M, N, K, leaf, k_first, workspace, workspace_bytes, hip_stream, epilogue);
 }
 
 int tbik_gemm_shard_partials(const void *X, int64_t ldx, const void *W, int64_t ldw, float *partials,
@@ -536,6 +576,23 @@ int tbik_tree_combine(const float *partials, int P, void *Y, int64_t ldy, tbik_d
     return e == hipSuccess ? TBIK_OK : hip_fail(e);
 }
 
+int tbik_tree_combine_epilogue(const float *partials, int P, const tbik_epilogue *epilogue, void *Y, int64_t ldy, tbik_dtype y_dtype,
+                               int M, int N, void *hip_stream) {
+    if (M < 0 || N < 0) return TBIK_ERR_SHAPE;
+    if (P < 1 || !is_pow2(P) || P > TBIK_MAX_SHARDS) return TBIK_ERR_SHARDS;
+    if (y_dtype != TBIK_F32 && y_dtype != TBIK_BF16 && y_dtype != TBIK_F16) return TBIK_ERR_DTYPE;
+    if (!epilogue) return TBIK_ERR_NULL;
+    EpilogueParams ends;
+    const int rc = check_epilogue(epilogue, Y, ldy, (int)y_dtype, M, N, &ends);
+    if (rc != TBIK_OK) return rc;
+    if (M == 0 || N == 0) return TBIK_OK;
+    if (!partials || !Y) return TBIK_ERR_NULL;
+    if (ldy < N) return TBIK_ERR_SHAPE;
+    if (!aligned(partials, 16) || !aligned(Y, y_dtype == TBIK_F32 ? 4 : 2)) return TBIK_ERR_ALIGN;
+    hipError_t e = launch_tree_combine_epilogue(partials, P, ends, Y, ldy, M, N, (hipStream_t)hip_stream);
+    return e == hipSuccess ? TBIK_OK : hip_fail(e);
+}
+
 // ---- 8-bit floating-point operands ----
 static bool is_fp8(int d) { return d == TBIK_FP8_E4M3 || d == TBIK_FP8_E5M2; }
 
@@ -558,13 +615,19 @@ size_t tbik_gemm_fp8_workspace_bytes(int M, int N, int K, int leaf, int k_first)
     return plan_planes_bytes(OPERANDS_FP8, M, N, K, ns);
 }
 
-int tbik_gemm_fp8(const void *X, int64_t ldx, const void *Wt, int64_t ldwt, void *Y, int64_t ldy,
-                  tbik_dtype y_dtype, tbik_dtype x_dtype, int M, int N, int K, int leaf, int k_first,
-                  void *workspace, size_t workspace_bytes, void *hip_stream) {
+// Output types of the 8-bit and MXFP8 products: binary16 with an epilogue only.
+static bool legal_low_bit_y(int y_dtype, const tbik_epilogue *epilogue) { return y_dtype == TBIK_F32 || y_dtype == TBIK_BF16 || (epilogue && y_dtype == TBIK_F16); }
+
+static int gemm_fp8(const void *X, int64_t ldx, const void *Wt, int64_t ldwt, const tbik_epilogue *epilogue, void *Y, int64_t ldy,
+                    tbik_dtype y_dtype, tbik_dtype x_dtype, int M, int N, int K, int leaf, int k_first,
+                    void *workspace, size_t workspace_bytes, void *hip_stream) {
     int sl, ns;
     int rc = fp8_checks((int)x_dtype, X, ldx, Wt, ldwt, M, N, K, leaf, k_first, 1, &sl, &ns);
     if (rc != TBIK_OK) return rc;
-    if (y_dtype != TBIK_F32 && y_dtype != TBIK_BF16) return TBIK_ERR_DTYPE;
+    if (!legal_low_bit_y((int)y_dtype, epilogue)) return TBIK_ERR_DTYPE;
+    EpilogueParams ends;
+    rc = check_epilogue(epilogue, Y, ldy, (int)y_dtype, M, N, &ends);
+    if (rc != TBIK_OK) return rc;
     if (M == 0 || N == 0) return TBIK_OK;
     if (!Y) return TBIK_ERR_NULL;
     if (ldy < N) return TBIK_ERR_SHAPE;
@@ -578,6 +641,7 @@ int tbik_gemm_fp8(const void *X, int64_t ldx, const void *Wt, int64_t ldwt, void
         void *y = static_cast<char *>(Y) + (int64_t)m0 * ldy * (y_dtype == TBIK_F32 ? 4 : 2);
         GemmArgs a{(const uint16_t *)(static_cast<const char *>(X) + (int64_t)m0 * ldx), ldx, (const uint16_t *)Wt, ldwt, nullptr, y, ldy,
                    (int)y_dtype, m, N, K, sl, ns, 1, (int)x_dtype, 0};
+        const PieceEnd end(epilogue, ends, m0, &a);
         const int kernel = low_bit_kernel(a, nullptr, plan.split);
         if (kernel == KERNEL_SLICES) return launch_gemm_slice(a, nullptr, s);
         if (kernel == KERNEL_REFERENCE) return launch_gemm_fp8_reference(a, s);
@@ -585,10 +649,24 @@ int tbik_gemm_fp8(const void *X, int64_t ldx, const void *Wt, int64_t ldwt, void
         a.partials = reinterpret_cast<float *>(workspace);
         a.Y = nullptr;
         a.P = plan.split;
+        a.epilogue = nullptr;
         hipError_t pe = launch_gemm_fp8_tiled(a, plan.rows, s);
-        return pe == hipSuccess ? launch_tree_combine(a.partials, plan.split, y, ldy, (int)y_dtype, m, N, s) : pe;
+        return pe == hipSuccess ? end.combine(a.partials, plan.split, y, ldy, (int)y_dtype, m, N, s) : pe;
     });
     return e == hipSuccess ? TBIK_OK : hip_fail(e);
+}
+
+int tbik_gemm_fp8(const void *X, int64_t ldx, const void *Wt, int64_t ldwt, void *Y, int64_t ldy,
+                  tbik_dtype y_dtype, tbik_dtype x_dtype, int M, int N, int K, int leaf, int k_first,
+                  void *workspace, size_t workspace_bytes, void *hip_stream) {
+    return gemm_fp8(X, ldx, Wt, ldwt, nullptr, Y, ldy, y_dtype, x_dtype, M, N, K, leaf, k_first, workspace, workspace_bytes, hip_stream);
+}
+
+int tbik_gemm_fp8_epilogue(const void *X, int64_t ldx, const void *Wt, int64_t ldwt, const tbik_epilogue *epilogue, void *Y, int64_t ldy,
+                           tbik_dtype y_dtype, tbik_dtype x_dtype, int M, int N, int K, int leaf, int k_first,
+                           void *workspace, size_t workspace_bytes, void *hip_stream) {
+    if (!epilogue) return TBIK_ERR_NULL;
+    return gemm_fp8(X, ldx, Wt, ldwt, epilogue, Y, ldy, y_dtype, x_dtype, M, N, K, leaf, k_first, workspace, workspace_bytes, hip_stream);
 }
 
 int tbik_gemm_shard_partials_fp8(const void *X, int64_t ldx, const void *Wt, int64_t ldwt, float *partials,
@@ -775,14 +853,17 @@ size_t tbik_gemm_mxfp8_workspace_bytes(int M, int N, int K, int leaf, int k_firs
     return round_256(plan_planes_bytes(OPERANDS_MXFP8, M, N, K, ns)) + mxfp8_scales_room(M, N, K);
 }
 
-int tbik_gemm_mxfp8(const void *X, int64_t ldx, const void *Xs, int64_t ldxs, const void *Wt, int64_t ldwt,
-                    const void *Ws, int64_t ldws, void *Y, int64_t ldy, tbik_dtype y_dtype, tbik_dtype x_dtype,
-                    int M, int N, int K, int leaf, int k_first,
-                    void *workspace, size_t workspace_bytes, void *hip_stream) {
+static int gemm_mxfp8(const void *X, int64_t ldx, const void *Xs, int64_t ldxs, const void *Wt, int64_t ldwt,
+                      const void *Ws, int64_t ldws, const tbik_epilogue *epilogue, void *Y, int64_t ldy, tbik_dtype y_dtype, tbik_dtype x_dtype,
+                      int M, int N, int K, int leaf, int k_first,
+                      void *workspace, size_t workspace_bytes, void *hip_stream) {
     int sl, ns;
     int rc = mxfp8_checks((int)x_dtype, X, ldx, Xs, ldxs, Wt, ldwt, Ws, ldws, M, N, K, leaf, k_first, 1, &sl, &ns);
     if (rc != TBIK_OK) return rc;
-    if (y_dtype != TBIK_F32 && y_dtype != TBIK_BF16) return TBIK_ERR_DTYPE;
+    if (!legal_low_bit_y((int)y_dtype, epilogue)) return TBIK_ERR_DTYPE;
+    EpilogueParams ends;
+    rc = check_epilogue(epilogue, Y, ldy, (int)y_dtype, M, N, &ends);
+    if (rc != TBIK_OK) return rc;
     if (M == 0 || N == 0) return TBIK_OK;
     if (!Y) return TBIK_ERR_NULL;
     if (ldy < N) return TBIK_ERR_SHAPE;
@@ -799,6 +880,7 @@ int tbik_gemm_mxfp8(const void *X, int64_t ldx, const void *Xs, int64_t ldxs, co
         void *y = static_cast<char *>(Y) + (int64_t)m0 * ldy * (y_dtype == TBIK_F32 ? 4 : 2);
         GemmArgs a{(const uint16_t *)(static_cast<const char *>(X) + (int64_t)m0 * ldx), ldx, (const uint16_t *)Wt, ldwt, nullptr, y, ldy,
                    (int)y_dtype, m, N, K, sl, ns, 1, (int)x_dtype, 0};
+        const PieceEnd end(epilogue, ends, m0, &a);
         const Mxfp4Scales sc = scales.plain(m0);
         const int kernel = low_bit_kernel(a, &sc, plan.split);
         if (kernel == KERNEL_SLICES) return launch_gemm_slice(a, &sc, s);
@@ -810,10 +892,26 @@ int tbik_gemm_mxfp8(const void *X, int64_t ldx, const void *Xs, int64_t ldxs, co
         a.partials = reinterpret_cast<float *>(workspace);
         a.Y = nullptr;
         a.P = plan.split;
+        a.epilogue = nullptr;
         pe = launch_gemm_mxfp8_tiled(a, tiled, plan.rows, s);
-        return pe == hipSuccess ? launch_tree_combine(a.partials, plan.split, y, ldy, (int)y_dtype, m, N, s) : pe;
+        return pe == hipSuccess ? end.combine(a.partials, plan.split, y, ldy, (int)y_dtype, m, N, s) : pe;
     });
     return e == hipSuccess ? TBIK_OK : hip_fail(e);
+}
+
+int tbik_gemm_mxfp8(const void *X, int64_t ldx, const void *Xs, int64_t ldxs, const void *Wt, int64_t ldwt,
+                    const void *Ws, int64_t ldws, void *Y, int64_t ldy, tbik_dtype y_dtype, tbik_dtype x_dtype,
+                    int M, int N, int K, int leaf, int k_first,
+                    void *workspace, size_t workspace_bytes, void *hip_stream) {
+    return gemm_mxfp8(X, ldx, Xs, ldxs, Wt, ldwt, Ws, ldws, nullptr, Y, ldy, y_dtype, x_dtype, M, N, K, leaf, k_first, workspace, workspace_bytes, hip_stream);
+}
+
+int tbik_gemm_mxfp8_epilogue(const void *X, int64_t ldx, const void *Xs, int64_t ldxs, const void *Wt, int64_t ldwt,
+                             const void *Ws, int64_t ldws, const tbik_epilogue *epilogue, void *Y, int64_t ldy, tbik_dtype y_dtype, tbik_dtype x_dtype,
+                             int M, int N, int K, int leaf, int k_first,
+                             void *workspace, size_t workspace_bytes, void *hip_stream) {
+    if (!epilogue) return TBIK_ERR_NULL;
+    return gemm_mxfp8(X, ldx, Xs, ldxs, Wt, ldwt, Ws, ldws, epilogue, Y, ldy, y_dtype, x_dtype, M, N, K, leaf, k_first, workspace, workspace_bytes, hip_stream);
 }
 
 int tbik_gemm_shard_partials_mxfp8(const void *X, int64_t ldx, const void *Xs, int64_t ldxs, const void *Wt, int64_t ldwt,
@@ -1038,6 +1136,100 @@ int tbik_gemm_swiglu(const void *X, int64_t ldx, const void *W_gu, int64_t ldw, 
         e = launch_silu_mul(staged, N, staged + I, N, (uint16_t *)act, lda, (int)dtype, M, I, s);
     }
     return e == hipSuccess ? TBIK_OK : hip_fail(e);
+}
+
+// ---- 8-bit outputs with scales ----
+// What the calls have in common: n columns in whole chunks (micro: blocks), patterns stored 8 bytes at a time.
+static int check_8bit_out(tbik_dtype q_dtype, int M, int n, const void *q, int64_t ldq, const void *scales, int64_t lds, bool micro) {
+    if (!is_fp8((int)q_dtype)) return TBIK_ERR_DTYPE;
+    if (M < 0 || n <= 0 || n % (micro ? 32 : 8) != 0 || n > 65536) return TBIK_ERR_SHAPE;
+    if (M == 0) return TBIK_OK;
+    if (!q || !scales) return TBIK_ERR_NULL;
+    if (ldq < n || (micro && lds < n / 32)) return TBIK_ERR_SHAPE;
+    if (!aligned(q, 8) || ldq % 8 != 0 || (!micro && !aligned(scales, 4))) return TBIK_ERR_ALIGN;
+    return TBIK_OK;
+}
+static EightBitOut out_8bit(tbik_dtype q_dtype, void *q, int64_t ldq, void *scales, int64_t lds, bool micro) {
+    return {(uint8_t *)q, ldq, scales, lds, micro, q_dtype == TBIK_FP8_E5M2};
+}
+
+static int rmsnorm_8bit(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, float eps, void *hidden, int64_t ldh,
+                        void *q, int64_t ldq, void *scales, int64_t lds, bool micro, tbik_dtype dtype, tbik_dtype q_dtype, int M, int H, void *hip_stream) {
+    if (dtype != TBIK_BF16 && dtype != TBIK_F16) return TBIK_ERR_DTYPE;
+    const int rc = check_8bit_out(q_dtype, M, H, q, ldq, scales, lds, micro);
+    if (rc != TBIK_OK || M == 0) return rc;
+    if (!x || !weight || !residual != !hidden) return TBIK_ERR_NULL;
+    if (ldx < H || (residual && (ldr < H || ldh < H))) return TBIK_ERR_SHAPE;
+    if (!aligned(x, 16) || !aligned(weight, 16) || ldx % 8 != 0) return TBIK_ERR_ALIGN;
+    if (residual && (!aligned(residual, 16) || !aligned(hidden, 16) || ldr % 8 != 0 || ldh % 8 != 0)) return TBIK_ERR_ALIGN;
+    if (residual && ((hidden == x && ldh != ldx) || (hidden == residual && ldh != ldr))) return TBIK_ERR_SHAPE;
+    const Rms8Args a{(const uint16_t *)x, ldx, nullptr, 0, (const uint16_t *)residual, ldr, (const uint16_t *)weight, (uint16_t *)hidden, ldh,
+                     out_8bit(q_dtype, q, ldq, scales, lds, micro), M, H, eps};
+    hipError_t e = launch_rmsnorm_8bit(a, (int)dtype, (hipStream_t)hip_stream);
+    return e == hipSuccess ? TBIK_OK : hip_fail(e);
+}
+
+int tbik_rmsnorm_fp8(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, float eps, void *hidden, int64_t ldh,
+                     void *q, int64_t ldq, float *row_scale, tbik_dtype dtype, tbik_dtype q_dtype, int M, int H, void *hip_stream) {
+    return rmsnorm_8bit(x, ldx, residual, ldr, weight, eps, hidden, ldh, q, ldq, row_scale, 0, false, dtype, q_dtype, M, H, hip_stream);
+}
+
+int tbik_rmsnorm_mxfp8(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, float eps, void *hidden, int64_t ldh,
+                       void *q, int64_t ldq, void *scales, int64_t lds, tbik_dtype dtype, tbik_dtype q_dtype, int M, int H, void *hip_stream) {
+    return rmsnorm_8bit(x, ldx, residual, ldr, weight, eps, hidden, ldh, q, ldq, scales, lds, true, dtype, q_dtype, M, H, hip_stream);
+}
+
+static int combine_residual_rmsnorm_8bit(const float *partials, int P, const void *residual, int64_t ldr, const void *weight, float eps,
+                                         void *hidden, int64_t ldh, void *q, int64_t ldq, void *scales, int64_t lds, bool micro,
+                                         tbik_dtype dtype, tbik_dtype q_dtype, int M, int H, void *hip_stream) {
+    if (dtype != TBIK_BF16 && dtype != TBIK_F16) return TBIK_ERR_DTYPE;
+    if (P < 1 || !is_pow2(P) || P > TBIK_MAX_SHARDS) return TBIK_ERR_SHARDS;
+    if (P > 16) return TBIK_ERR_UNSUPPORTED;
+    const int rc = check_8bit_out(q_dtype, M, H, q, ldq, scales, lds, micro);
+    if (rc != TBIK_OK || M == 0) return rc;
+    if (!partials || !residual || !weight || !hidden) return TBIK_ERR_NULL;
+    if (ldr < H || ldh < H || (hidden == residual && ldh != ldr)) return TBIK_ERR_SHAPE;
+    if (!aligned(partials, 16) || !aligned(residual, 16) || !aligned(weight, 16) || !aligned(hidden, 16) || ldr % 8 != 0 || ldh % 8 != 0) return TBIK_ERR_ALIGN;
+    const Rms8Args a{nullptr, 0, partials, P, (const uint16_t *)residual, ldr, (const uint16_t *)weight, (uint16_t *)hidden, ldh,
+                     out_8bit(q_dtype, q, ldq, scales, lds, micro), M, H, eps};
+    hipError_t e = launch_rmsnorm_8bit(a, (int)dtype, (hipStream_t)hip_stream);
+    return e == hipSuccess ? TBIK_OK : hip_fail(e);
+}
+
+int tbik_combine_residual_rmsnorm_fp8(const float *partials, int P, const void *residual, int64_t ldr, const void *weight, float eps,
+                                      void *hidden, int64_t ldh, void *q, int64_t ldq, float *row_scale,
+                                      tbik_dtype dtype, tbik_dtype q_dtype, int M, int H, void *hip_stream) {
+    return combine_residual_rmsnorm_8bit(partials, P, residual, ldr, weight, eps, hidden, ldh, q, ldq, row_scale, 0, false, dtype, q_dtype, M, H, hip_stream);
+}
+
+int tbik_combine_residual_rmsnorm_mxfp8(const float *partials, int P, const void *residual, int64_t ldr, const void *weight, float eps,
+                                        void *hidden, int64_t ldh, void *q, int64_t ldq, void *scales, int64_t lds,
+                                        tbik_dtype dtype, tbik_dtype q_dtype, int M, int H, void *hip_stream) {
+    return combine_residual_rmsnorm_8bit(partials, P, residual, ldr, weight, eps, hidden, ldh, q, ldq, scales, lds, true, dtype, q_dtype, M, H, hip_stream);
+}
+
+static int silu_mul_8bit(const void *gate, int64_t ldg, const void *up, int64_t ldu, void *q, int64_t ldq, void *scales, int64_t lds, bool micro,
+                         tbik_dtype dtype, tbik_dtype q_dtype, int M, int I, void *hip_stream) {
+    if ((dtype != TBIK_BF16 && dtype != TBIK_F16) || !is_fp8((int)q_dtype)) return TBIK_ERR_DTYPE;
+    if (M >= 0 && I == 0) return TBIK_OK;
+    const int rc = check_8bit_out(q_dtype, M, I, q, ldq, scales, lds, micro);
+    if (rc != TBIK_OK || M == 0) return rc;
+    if (!gate || !up) return TBIK_ERR_NULL;
+    if (ldg < I || ldu < I) return TBIK_ERR_SHAPE;
+    if (!aligned(gate, 16) || !aligned(up, 16) || ldg % 8 != 0 || ldu % 8 != 0) return TBIK_ERR_ALIGN;
+    const Silu8Args a{(const uint16_t *)gate, ldg, (const uint16_t *)up, ldu, out_8bit(q_dtype, q, ldq, scales, lds, micro), M, I};
+    hipError_t e = launch_silu_mul_8bit(a, (int)dtype, (hipStream_t)hip_stream);
+    return e == hipSuccess ? TBIK_OK : hip_fail(e);
+}
+
+int tbik_silu_mul_fp8(const void *gate, int64_t ldg, const void *up, int64_t ldu, void *q, int64_t ldq, float *row_scale,
+                      tbik_dtype dtype, tbik_dtype q_dtype, int M, int I, void *hip_stream) {
+    return silu_mul_8bit(gate, ldg, up, ldu, q, ldq, row_scale, 0, false, dtype, q_dtype, M, I, hip_stream);
+}
+
+int tbik_silu_mul_mxfp8(const void *gate, int64_t ldg, const void *up, int64_t ldu, void *q, int64_t ldq, void *scales, int64_t lds,
+                        tbik_dtype dtype, tbik_dtype q_dtype, int M, int I, void *hip_stream) {
+    return silu_mul_8bit(gate, ldg, up, ldu, q, ldq, scales, lds, true, dtype, q_dtype, M, I, hip_stream);
 }
 
 int tbik_tree_allreduce(float *bufs, int P, int64_t n, void *hip_stream) {

@@ -8,6 +8,29 @@
 
 namespace tbik {
 
+// Resolved epilogue of a matrix product (tbik_epilogue); passed to the kernels by value.
+struct EpilogueParams {
+    const float *row_scale, *col_scale;   // [M], [N] or nullptr
+    const void *bias;                     // [N] of bias_dtype, or nullptr
+    const void *residual;                 // [M, ldr] of y_dtype, or nullptr; may be the output itself
+    int64_t ldr;
+    int bias_dtype, act, y_dtype;         // tbik_dtype, tbik_activation, tbik_dtype
+    // The same for the rows from m0 on.
+    EpilogueParams from_row(int m0) const {
+        EpilogueParams e = *this;
+        if (row_scale) e.row_scale += m0;
+        if (residual) e.residual = static_cast<const char *>(residual) + (int64_t)m0 * ldr * (y_dtype == TBIK_F32 ? 4 : 2);
+        return e;
+    }
+};
+struct NoEpilogue {};
+template <bool EPI>
+struct EpilogueArgument { using type = EpilogueParams; };
+template <>
+struct EpilogueArgument<false> { using type = NoEpilogue; };
+template <bool EPI>
+using ReferenceEpilogue = typename EpilogueArgument<EPI>::type;
+
 // Resolved description of one GEMM request; validated by the C ABI layer before any launch.
 struct GemmArgs {
     const uint16_t *X;   // x_dtype [M, ldx] (fp32 and 8-bit operands: the pointer is cast)
@@ -25,6 +48,7 @@ struct GemmArgs {
     int x_dtype;         // TBIK_BF16, TBIK_F16 or TBIK_F32: storage format of X, W (and of a 16-bit Y)
     int swiglu;          // 1: W is [gate | up], N = 2 I columns; Y is act [M, I] = SiLU(gate) * up in x_dtype.  Only the
                          // 128 x 128 tile of the 16-bit kernels, P == 1, I % 64 == 0 (gemm_tiled_supports() says).
+    const EpilogueParams *epilogue = nullptr;   // Y passes through it; 16-bit, 8-bit and MXFP8 operands, P == 1, no partials
 };
 
 // Reference kernel: one wavefront per 32x32 tile and shard.  Writes partials (if set) and, when P == 1
@@ -99,6 +123,9 @@ hipError_t launch_gemm_slice(const GemmArgs &a, const Mxfp4Scales *sc, hipStream
 hipError_t launch_tree_combine(const float *partials, int P, void *Y, int64_t ldy, int y_dtype, int M, int N,
                                hipStream_t s);
 
+// The same with the epilogue between the sum and the rounding (to epilogue.y_dtype).
+hipError_t launch_tree_combine_epilogue(const float *partials, int P, const EpilogueParams &epilogue, void *Y, int64_t ldy, int M, int N, hipStream_t s);
+
 // Alg. 2 round by round on P rank buffers [P, n], in place: afterwards every buffer holds T(buffers).
 hipError_t launch_tree_allreduce(float *bufs, int P, int64_t n, hipStream_t s);
 
@@ -106,6 +133,40 @@ hipError_t launch_tree_allreduce(float *bufs, int P, int64_t n, hipStream_t s);
 hipError_t launch_rmsnorm(const uint16_t *x, const uint16_t *w, uint16_t *y, int M, int H, float eps, int dtype, hipStream_t s);
 hipError_t launch_combine_residual_rmsnorm(const float *partials, int P, const uint16_t *res, const uint16_t *w,
                                            uint16_t *hidden, uint16_t *normed, int M, int H, float eps, int dtype, hipStream_t s);
+
+// 8-bit outputs with scales (eight_bit_rows.hpp).
+struct EightBitOut {
+    uint8_t *q;          // [., ldq]
+    int64_t ldq;
+    void *scales;        // fp32, one per row; micro: bytes [., lds], one per 32 columns
+    int64_t lds;
+    int micro, e5m2;
+};
+struct Rms8Args {
+    const uint16_t *x;         // [M, ldx], P == 0
+    int64_t ldx;
+    const float *partials;     // dense [P, M, H], P > 0
+    int P;
+    const uint16_t *residual;  // [M, ldr] or nullptr
+    int64_t ldr;
+    const uint16_t *weight;
+    uint16_t *hidden;          // [M, ldh], with a residual
+    int64_t ldh;
+    EightBitOut out;
+    int M, H;
+    float eps;
+};
+hipError_t launch_rmsnorm_8bit(const Rms8Args &a, int dtype, hipStream_t s);
+struct Silu8Args {
+    const uint16_t *gate;
+    int64_t ldg;
+    const uint16_t *up;
+    int64_t ldu;
+    EightBitOut out;
+    int64_t M;
+    int I;
+};
+hipError_t launch_silu_mul_8bit(const Silu8Args &a, int dtype, hipStream_t s);
 
 // Resolved description of one attention call; validated by the C ABI layer.
 struct AttnArgs {
