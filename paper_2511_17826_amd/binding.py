@@ -179,13 +179,24 @@ _NATIVE = {name: (i, *spec) for i, (name, *spec) in enumerate([
     ("tbik_row_reduce", 10, "tbik_row_reduce_workspace_bytes", torch.float32),
     ("tbik_attention", 11, "tbik_attention_workspace_bytes", torch.bfloat16),
     ("tbik_attention_f16", 11, "tbik_attention_workspace_bytes", torch.float16),
+    ("tbik_gemm_epilogue bf16", 12, "tbik_gemm_16bit_workspace_bytes", torch.bfloat16),
+    ("tbik_gemm_epilogue fp16", 12, "tbik_gemm_16bit_workspace_bytes", torch.float16),
+    ("tbik_gemm_fp8_epilogue", 13, "tbik_gemm_fp8_workspace_bytes", torch.uint8),
+    ("tbik_gemm_mxfp8_epilogue", 14, "tbik_gemm_mxfp8_workspace_bytes", torch.uint8),
+    ("tbik_tree_combine_epilogue", 15, None, torch.float32),
+    ("tbik_rmsnorm_fp8", 16, None, torch.uint8),
+    ("tbik_rmsnorm_mxfp8", 17, None, torch.uint8),
+    ("tbik_combine_residual_rmsnorm_fp8", 18, None, torch.uint8),
+    ("tbik_combine_residual_rmsnorm_mxfp8", 19, None, torch.uint8),
+    ("tbik_silu_mul_fp8", 20, None, torch.uint8),
+    ("tbik_silu_mul_mxfp8", 21, None, torch.uint8),
 ])}
 _NUMBER = {name: spec[0] for name, spec in _NATIVE.items()}
 
 
 class _NotLoaded:
     """Stands for the native half until the library is loaded, and where it cannot be loaded: no call is a common one."""
-    product = rmsnorm = combine = row_reduce = attention = staticmethod(lambda *a: None)
+    product = rmsnorm = combine = row_reduce = attention = epilogue = eight_bits = staticmethod(lambda *a: None)
 
 
 _native = _NotLoaded
@@ -798,6 +809,11 @@ def tbik_gemm_epilogue(X: torch.Tensor, W: torch.Tensor, leaf: int, k_first: int
     """act((X @ W) * row_scale[:, None] * col_scale + bias) + residual in the tree order, rounded once (bf16 or fp16 operands; the
     output is of their type or float32).  `bias` float32, bfloat16 or float16; `activation` "relu", "silu", "gelu" or "gelu_tanh";
     `residual` of the output's type, which may be `out` itself."""
+    if out is None and workspace is None:
+        y = _native.epilogue(_NUMBER["tbik_gemm_epilogue fp16" if X.dtype == torch.float16 else "tbik_gemm_epilogue bf16"], X, None, W, None, leaf, k_first,
+                             out_dtype or X.dtype, 0, row_scale, col_scale, bias, _ACTIVATIONS.get(activation), residual)
+        if y is not None:
+            return _done(y, "tbik_gemm_epilogue")
     ldx, ldw = _rowmajor(X, "X"), _rowmajor(W, "W")
     assert X.dtype == W.dtype and X.dtype in (torch.bfloat16, torch.float16)
     M, K = X.shape
@@ -826,6 +842,11 @@ def tbik_gemm_fp8_epilogue(X: torch.Tensor, Wt: torch.Tensor, leaf: int, k_first
                            out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
     """The same on 8-bit operands (Wt is [N, K]), with the scales of their quantisation: row_scale float32 [M], as tbik_rmsnorm_fp8
     and tbik_silu_mul_fp8 give it, col_scale float32 [N].  bfloat16, float16 or float32 output."""
+    if out is None and workspace is None:
+        y = _native.epilogue(_NUMBER["tbik_gemm_fp8_epilogue"], X, None, Wt, None, leaf, k_first, out_dtype, _FP8.get(fmt), row_scale, col_scale, bias,
+                             _ACTIVATIONS.get(activation), residual)
+        if y is not None:
+            return _done(y, "tbik_gemm_fp8_epilogue")
     X, Wt, dt = _fp8_operands(X, Wt, fmt)
     M, K = X.shape
     N = Wt.shape[0]
@@ -850,6 +871,11 @@ def tbik_gemm_mxfp8_epilogue(X, Xs, Wt, Ws, leaf: int, k_first: int = 1, fmt: st
                              residual: torch.Tensor | None = None, out_dtype=torch.bfloat16, out: torch.Tensor | None = None,
                              workspace: torch.Tensor | None = None) -> torch.Tensor:
     """The same on MXFP8 operands (X and Xs as tbik_rmsnorm_mxfp8 and tbik_silu_mul_mxfp8 give them)."""
+    if out is None and workspace is None:
+        y = _native.epilogue(_NUMBER["tbik_gemm_mxfp8_epilogue"], X, Xs, Wt, Ws, leaf, k_first, out_dtype, _FP8.get(fmt), row_scale, col_scale, bias,
+                             _ACTIVATIONS.get(activation), residual)
+        if y is not None:
+            return _done(y, "tbik_gemm_mxfp8_epilogue")
     X, Wt, dt, M, N, K = _mx8_operands(X, Xs, Wt, Ws, fmt)
     if out is None:
         out = X.new_empty((M, N), dtype=out_dtype)
@@ -872,6 +898,11 @@ def tbik_tree_combine_epilogue(partials: torch.Tensor, bias: torch.Tensor | None
                                residual: torch.Tensor | None = None, row_scale: torch.Tensor | None = None,
                                col_scale: torch.Tensor | None = None, out_dtype=torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
     """act(T(partials[0..P)) * row_scale[:, None] * col_scale + bias) + residual, rounded once: partial sums of any operand format."""
+    if out is None:
+        y = _native.epilogue(_NUMBER["tbik_tree_combine_epilogue"], partials, None, None, None, 0, 0, out_dtype, 0, row_scale, col_scale, bias,
+                             _ACTIVATIONS.get(activation), residual)
+        if y is not None:
+            return _done(y, "tbik_tree_combine_epilogue")
     assert partials.dim() == 3 and partials.is_contiguous() and partials.dtype == torch.float32
     P, M, N = partials.shape
     if out is None:
@@ -904,6 +935,10 @@ def _eight_bit_out(like, M, n, micro, fmt, out, scale):
 
 
 def _norm_8bit(name, micro, x, weight, eps, residual, fmt, hidden, out, scale):
+    if hidden is None and out is None and scale is None:
+        y = _native.eight_bits(_NUMBER[name], x, residual, weight, eps, _FP8.get(fmt))
+        if y is not None:
+            return _done(y, name)
     M, H = x.shape[-2:]
     if x.dim() == 3:                                  # shards' partial sums [P, M, H]
         assert x.is_contiguous() and x.dtype == torch.float32
@@ -957,6 +992,10 @@ def tbik_combine_residual_rmsnorm_mxfp8(partials: torch.Tensor, residual: torch.
 
 
 def _silu_mul_8bit(name, micro, gate, up, fmt, out, scale):
+    if out is None and scale is None:
+        y = _native.eight_bits(_NUMBER[name], gate, up, None, None, _FP8.get(fmt))
+        if y is not None:
+            return _done(y, name)
     ldg, ldu = _rowmajor(gate, "gate"), _rowmajor(up, "up")
     assert gate.dtype == up.dtype and gate.dtype in (torch.bfloat16, torch.float16) and gate.shape == up.shape
     M, I = gate.shape

@@ -23,8 +23,9 @@ __global__ __launch_bounds__(256) void tree_combine_epilogue_kernel(const float 
             f32x4 in[P];
 #pragma unroll
             for (int p = 0; p < P; ++p) in[p] = *reinterpret_cast<const f32x4 *>(partials + (int64_t)p * plane + row * N + col);
-            float v[4], cs[4] = {0, 0, 0, 0}, b[4] = {0, 0, 0, 0}, r[4] = {0, 0, 0, 0}, rs = 0.0f;
-            if (e.row_scale) rs = e.row_scale[row];
+            float y[1][4], cs[4] = {0, 0, 0, 0}, b[4] = {0, 0, 0, 0}, r[4] = {0, 0, 0, 0}, rs[1] = {0.0f};
+            float (&v)[4] = y[0];
+            if (e.row_scale) rs[0] = e.row_scale[row];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (e.col_scale) cs[i] = e.col_scale[col + i];
@@ -35,7 +36,7 @@ __global__ __launch_bounds__(256) void tree_combine_epilogue_kernel(const float 
                 for (int p = 0; p < P; ++p) t[p] = in[p][i];
                 v[i] = tree_of<P>(t);
             }
-            scale_and_bias(e, v, rs, cs, b);
+            scale_and_bias(e, y, rs, cs, b);
             activate(e.act, v);
             if (e.residual) add_residual(v, r);
             if (e.y_dtype == TBIK_F32) {

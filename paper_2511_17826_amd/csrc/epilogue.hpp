@@ -53,25 +53,41 @@ __device__ __forceinline__ float widened(const void *p, int64_t i, int dtype) {
 }
 __device__ __forceinline__ uint32_t pack_16x2(float lo, float hi, bool f16) { return f16 ? pack_f16x2(lo, hi) : pack_bf16x2(lo, hi); }
 
-// The steps on COUNT elements of one row, consecutive columns.  The fp32 value behind each is made one of its own: no merging
-// of a last operation with the rounding to 16 bits (see silu_mul).
+// The steps on COUNT elements of one row, consecutive columns; what is absent is skipped for all of them at once (uniform branches).
+// A step's fp32 values are made values of their own: no merging of a last operation with the rounding to 16 bits (see silu_mul).
 template <int COUNT>
-__device__ __forceinline__ void scale_and_bias(const EpilogueParams &e, float (&v)[COUNT], float rs, const float (&cs)[COUNT], const float (&b)[COUNT]) {
+__device__ __forceinline__ void values_of_their_own(float (&v)[COUNT]) {
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) {
-        if (e.row_scale) v[i] = v[i] * rs;
-        if (e.col_scale) v[i] = v[i] * cs[i];
-        if (e.bias) v[i] = v[i] + b[i];
-        asm("" : "+v"(v[i]));
+    for (int i = 0; i < COUNT; ++i) asm("" : "+v"(v[i]));
+}
+template <int ROWS, int COUNT>                  // of ROWS rows
+__device__ __forceinline__ void scale_and_bias(const EpilogueParams &e, float (&v)[ROWS][COUNT], const float (&rs)[ROWS], const float (&cs)[COUNT], const float (&b)[COUNT]) {
+    if (e.row_scale) {
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) v[r][i] = v[r][i] * rs[r];
     }
+    if (e.col_scale) {
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) v[r][i] = v[r][i] * cs[i];
+    }
+    if (e.bias) {
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) v[r][i] = v[r][i] + b[i];
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) values_of_their_own(v[r]);
 }
 template <int ACT, int COUNT>
 __device__ __forceinline__ void activate_as(float (&v)[COUNT]) {
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) {
-        v[i] = activation_of<ACT>(v[i]);
-        asm("" : "+v"(v[i]));
-    }
+    for (int i = 0; i < COUNT; ++i) v[i] = activation_of<ACT>(v[i]);
+    values_of_their_own(v);
 }
 template <int COUNT>
 __device__ __forceinline__ void activate(int act, float (&v)[COUNT]) {
@@ -86,24 +102,22 @@ __device__ __forceinline__ void activate(int act, float (&v)[COUNT]) {
 template <int COUNT>
 __device__ __forceinline__ void add_residual(float (&v)[COUNT], const float (&r)[COUNT]) {
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) {
-        v[i] = v[i] + r[i];
-        asm("" : "+v"(v[i]));
-    }
+    for (int i = 0; i < COUNT; ++i) v[i] = v[i] + r[i];
+    values_of_their_own(v);
 }
 
 // One element, everything from memory, stored.
 __device__ __forceinline__ void finish_and_store(const EpilogueParams &e, float t, void *Y, int64_t ldy, int64_t row, int64_t col) {
-    float v[1] = {t}, cs[1] = {0.0f}, b[1] = {0.0f}, r[1] = {0.0f}, rs = 0.0f;
-    if (e.row_scale) rs = e.row_scale[row];
+    float v[1][1] = {{t}}, cs[1] = {0.0f}, b[1] = {0.0f}, r[1] = {0.0f}, rs[1] = {0.0f};
+    if (e.row_scale) rs[0] = e.row_scale[row];
     if (e.col_scale) cs[0] = e.col_scale[col];
     if (e.bias) b[0] = widened(e.bias, col, e.bias_dtype);
     if (e.residual) r[0] = widened(e.residual, row * e.ldr + col, e.y_dtype);
     scale_and_bias(e, v, rs, cs, b);
-    activate(e.act, v);
-    if (e.residual) add_residual(v, r);
-    if (e.y_dtype == TBIK_F32) reinterpret_cast<float *>(Y)[row * ldy + col] = v[0];
-    else reinterpret_cast<uint16_t *>(Y)[row * ldy + col] = (uint16_t)pack_16x2(v[0], 0.0f, e.y_dtype == TBIK_F16);
+    activate(e.act, v[0]);
+    if (e.residual) add_residual(v[0], r);
+    if (e.y_dtype == TBIK_F32) reinterpret_cast<float *>(Y)[row * ldy + col] = v[0][0];
+    else reinterpret_cast<uint16_t *>(Y)[row * ldy + col] = (uint16_t)pack_16x2(v[0][0], 0.0f, e.y_dtype == TBIK_F16);
 }
 
 }  // namespace tbik

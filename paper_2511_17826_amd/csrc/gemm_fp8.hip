@@ -426,11 +426,13 @@ void gemm_fp8_tiled_kernel(const std::conditional_t<EPI, Fp8EpilogueParams, Fp8P
             float *patch = reinterpret_cast<float *>(smem + last_slot * STAGE8 + wave * REGION8);
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
             stores_in_flight = -1;
+            const bool wide = p.epilogue.y_dtype == TBIK_F32;
             if (interior && p.vector_stores) {
-                store_with_epilogue<true>(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, 0, lane);
-                stores_in_flight = p.epilogue.y_dtype == TBIK_F32 ? STORES_F32 : STORES_BF16;
-            } else if (n0 + BN <= p.N && p.vector_stores) {
-                store_with_epilogue<false>(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, p.M - 1 - row0, lane);
+                if (wide) store_with_epilogue<true, true>(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, 0, lane, false);
+                else store_with_epilogue<true, false>(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, 0, lane, p.epilogue.y_dtype == TBIK_F16);
+                stores_in_flight = wide ? STORES_F32 : STORES_BF16;
+            } else if (n0 + BN <= p.N && p.vector_stores && !wide) {
+                store_with_epilogue<false, false>(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, p.M - 1 - row0, lane, p.epilogue.y_dtype == TBIK_F16);
             } else {
                 store_elements_with_epilogue(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, p.M, p.N, lane);
             }

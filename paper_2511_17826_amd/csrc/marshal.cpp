@@ -23,7 +23,8 @@
 
 namespace {
 
-enum Kind { GEMM, GEMM_F32, PARTIALS, PARTIALS_F32, SWIGLU, FP8, MX, MXFP4, RMSNORM, COMBINE, ROWS, ATTENTION, KINDS };
+enum Kind { GEMM, GEMM_F32, PARTIALS, PARTIALS_F32, SWIGLU, FP8, MX, MXFP4, RMSNORM, COMBINE, ROWS, ATTENTION,
+            EPILOGUE, EPILOGUE_FP8, EPILOGUE_MX, EPILOGUE_COMBINE, NORM8, NORM8_MX, TAIL8, TAIL8_MX, SILU8, SILU8_MX, KINDS };
 struct Entry {
     int kind = -1;
     void *call = nullptr, *need = nullptr;      // the C entry point and its workspace query
@@ -130,6 +131,7 @@ SAME(tbik_gemm_mxfp8, tbik_gemm_mxfp6);
 SAME(tbik_rmsnorm, tbik_rmsnorm_f16);
 SAME(tbik_combine_residual_rmsnorm, tbik_combine_residual_rmsnorm_f16);
 SAME(tbik_attention, tbik_attention_f16);
+SAME(tbik_gemm_epilogue, tbik_gemm_fp8_epilogue);
 SAME(tbik_gemm_16bit_workspace_bytes, tbik_gemm_f32_workspace_bytes);
 SAME(tbik_gemm_16bit_workspace_bytes, tbik_gemm_swiglu_workspace_bytes);
 SAME(tbik_gemm_16bit_workspace_bytes, tbik_gemm_fp8_workspace_bytes);
@@ -211,6 +213,146 @@ PyObject *product(PyObject *, PyObject *const *a, Py_ssize_t n) {
         }
         Py_END_ALLOW_THREADS
         return wrapped(std::move(Y), st);
+    } catch (const std::exception &) {
+        if (PyErr_Occurred()) return nullptr;
+        UNCOMMON;
+    }
+}
+
+// A part of an epilogue: None, or a plain contiguous vector of n elements.  False: not a common one.
+bool part(PyObject *o, int n, const at::Tensor **t) {
+    *t = nullptr;
+    if (o == Py_None) return true;
+    *t = plain(o, 1);
+    return *t && (*t)->size(0) == n && (n == 1 || (*t)->stride(0) == 1) && type_code((*t)->scalar_type()) >= 0;
+}
+bool elsewhere(const at::Tensor *t, const at::Tensor &like) { return t && t->device() != like.device(); }
+
+// The parts of an epilogue (row_scale, col_scale, bias, activation, residual in a[0 .. 4]) of an output [M, N] like `like` of out_type.
+bool epilogue_of(PyObject *const *a, int M, int N, const at::Tensor &like, at::ScalarType out_type, tbik_epilogue *e) {
+    const at::Tensor *rs, *cs, *bias, *res = nullptr;
+    int act;
+    if (!part(a[0], M, &rs) || !part(a[1], N, &cs) || !part(a[2], N, &bias) || !integer(a[3], &act)) return false;
+    if (a[4] != Py_None && !(res = matrix(a[4], out_type))) return false;
+    if ((rs && rs->scalar_type() != at::kFloat) || (cs && cs->scalar_type() != at::kFloat) || (res && (res->size(0) != M || res->size(1) != N))) return false;
+    if (like.device().index() != c10::hip::current_device() || elsewhere(rs, like) || elsewhere(cs, like) || elsewhere(bias, like) || elsewhere(res, like)) return false;
+    *e = {rs ? (const float *)rs->data_ptr() : nullptr, cs ? (const float *)cs->data_ptr() : nullptr, bias ? bias->data_ptr() : nullptr,
+          (tbik_dtype)(bias ? type_code(bias->scalar_type()) : 0), (tbik_activation)act, res ? res->data_ptr() : nullptr, res ? res->stride(0) : 0};
+    return true;
+}
+
+// epilogue(entry, X, Xs, W, Ws, leaf, k_first, out dtype, format, row_scale, col_scale, bias, activation, residual); EPILOGUE_COMBINE: X the partial sums
+PyObject *epilogue(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 14) UNCOMMON;
+    const Entry *e = entry_of(a[0], EPILOGUE, EPILOGUE_COMBINE);
+    int leaf, k_first, fmt;
+    if (!e || !integer(a[5], &leaf) || !integer(a[6], &k_first) || !integer(a[8], &fmt) || !THPDtype_Check(a[7])) UNCOMMON;
+    const int kind = e->kind;
+    const at::ScalarType out_type = ((THPDtype *)a[7])->scalar_type;
+    if (type_code(out_type) < 0) UNCOMMON;
+    try {
+        const at::Tensor *X = kind == EPILOGUE_COMBINE ? plain(a[1], 3) : matrix(a[1], e->dtype), *W = nullptr, *Xs = nullptr, *Ws = nullptr;
+        if (!X) UNCOMMON;
+        int M, N, K = 0;
+        if (kind == EPILOGUE_COMBINE) {
+            if (X->scalar_type() != at::kFloat || !X->is_contiguous() || X->size(0) > INT_MAX || X->size(1) > INT_MAX || X->size(2) > INT_MAX) UNCOMMON;
+            M = (int)X->size(1);
+            N = (int)X->size(2);
+        } else {
+            if (!(W = matrix(a[3], e->dtype))) UNCOMMON;
+            M = (int)X->size(0);
+            K = (int)X->size(1);
+            N = (int)W->size(kind == EPILOGUE ? 1 : 0);
+            if (W->size(kind == EPILOGUE ? 0 : 1) != K || elsewhere(W, *X)) UNCOMMON;
+            if (kind == EPILOGUE_MX) {
+                Xs = matrix(a[2], at::kByte);
+                Ws = matrix(a[4], at::kByte);
+                if (!Xs || !Ws || Xs->size(0) != M || Xs->size(1) != K / 32 || Ws->size(0) != N || Ws->size(1) != K / 32 || elsewhere(Xs, *X) || elsewhere(Ws, *X)) UNCOMMON;
+            }
+        }
+        tbik_epilogue ends;
+        if (!epilogue_of(a + 9, M, N, *X, out_type, &ends)) UNCOMMON;
+        at::Tensor Y = output({M, N}, *X, out_type);
+        if (!Y.defined()) UNCOMMON;
+        void *stream = current_stream();
+        Room ws;
+        if (!room_for(e->need ? NEED(tbik_gemm_16bit_workspace_bytes)(M, N, K, leaf, k_first) : 0, a[1], *X, stream, &ws)) return nullptr;
+        P x = X->data_ptr(), w = W ? W->data_ptr() : nullptr, y = Y.data_ptr(), xs = Xs ? Xs->data_ptr() : nullptr, wsc = Ws ? Ws->data_ptr() : nullptr;
+        const L ldx = X->stride(0), ldw = W ? W->stride(0) : 0, ldxs = Xs ? Xs->stride(0) : 0, ldws = Ws ? Ws->stride(0) : 0, ldy = Y.stride(0);
+        const int shards = kind == EPILOGUE_COMBINE ? (int)X->size(0) : 0;
+        const tbik_dtype yt = (tbik_dtype)type_code(out_type), xt = (tbik_dtype)(kind == EPILOGUE ? type_code(e->dtype) : fmt);
+        int st = 0;
+        Py_BEGIN_ALLOW_THREADS
+        if (kind == EPILOGUE_COMBINE) st = CALL(tbik_tree_combine_epilogue)((const float *)x, shards, &ends, y, ldy, yt, M, N, stream);
+        else if (kind == EPILOGUE_MX) st = CALL(tbik_gemm_mxfp8_epilogue)(x, ldx, xs, ldxs, w, ldw, wsc, ldws, &ends, y, ldy, yt, xt, M, N, K, leaf, k_first, ws.at, ws.bytes, stream);
+        else st = CALL(tbik_gemm_epilogue)(x, ldx, w, ldw, &ends, y, ldy, yt, xt, M, N, K, leaf, k_first, ws.at, ws.bytes, stream);
+        Py_END_ALLOW_THREADS
+        return wrapped(std::move(Y), st);
+    } catch (const std::exception &) {
+        if (PyErr_Occurred()) return nullptr;
+        UNCOMMON;
+    }
+}
+
+// A new reference to None or to the tensor, or nullptr with an error set.
+PyObject *tensor_or_none(at::Tensor &t) {
+    if (t.defined()) return THPVariable_Wrap(std::move(t));
+    Py_RETURN_NONE;
+}
+
+// eight_bits(entry, x / partial sums / gate, residual or None / up, weight (None: the activation), eps, format)
+//   -> (hidden or None, q, scale) of the norms, (q, scale) of the activation
+PyObject *eight_bits(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 6) UNCOMMON;
+    const Entry *e = entry_of(a[0], NORM8, SILU8_MX);
+    float eps = 0.0f;
+    int fmt;
+    if (!e || !integer(a[5], &fmt)) UNCOMMON;
+    const int kind = e->kind;
+    const bool silu = kind == SILU8 || kind == SILU8_MX, tail = kind == TAIL8 || kind == TAIL8_MX, micro = kind == NORM8_MX || kind == TAIL8_MX || kind == SILU8_MX;
+    if (!silu && !number(a[4], &eps)) UNCOMMON;
+    try {
+        const at::Tensor *x = plain(a[1], tail ? 3 : 2), *second = nullptr, *weight = nullptr;
+        if (!x || x->size(-2) > INT_MAX || x->size(-1) > INT_MAX) UNCOMMON;
+        const int M = (int)x->size(-2), H = (int)x->size(-1);
+        at::ScalarType dtype = x->scalar_type();
+        if (tail) {
+            if (dtype != at::kFloat || !x->is_contiguous() || x->size(0) > INT_MAX || a[2] == Py_None) UNCOMMON;
+            second = plain(a[2], 2);
+            if (!second) UNCOMMON;
+            dtype = second->scalar_type();
+        } else if (x->stride(1) != 1) UNCOMMON;
+        if (dtype != at::kBFloat16 && dtype != at::kHalf) UNCOMMON;
+        if (a[2] != Py_None && (!(second = matrix(a[2], dtype)) || second->size(0) != M || second->size(1) != H)) UNCOMMON;
+        if (silu ? !second : !((weight = plain(a[3], 1)) && weight->size(0) == H && weight->scalar_type() == dtype && weight->is_contiguous())) UNCOMMON;
+        if (x->device().index() != c10::hip::current_device() || elsewhere(second, *x) || elsewhere(weight, *x)) UNCOMMON;
+        at::Tensor hidden, q = output({M, H}, *x, at::kByte), scale = micro ? output({M, H / 32}, *x, at::kByte) : output({M}, *x, at::kFloat);
+        if (!q.defined() || !scale.defined()) UNCOMMON;
+        if (!silu && second) {
+            hidden = output({M, H}, *x, dtype);
+            if (!hidden.defined()) UNCOMMON;
+        }
+        P px = x->data_ptr(), p2 = second ? second->data_ptr() : nullptr, pw = weight ? weight->data_ptr() : nullptr, ph = hidden.defined() ? hidden.data_ptr() : nullptr,
+          pq = q.data_ptr(), ps = scale.data_ptr(), stream = current_stream();
+        const L ldx = x->stride(-2), ld2 = second ? second->stride(0) : 0, ldq = q.stride(0), lds = micro ? scale.stride(0) : 0, ldh = hidden.defined() ? hidden.stride(0) : 0;
+        const int shards = tail ? (int)x->size(0) : 0;
+        const tbik_dtype t = (tbik_dtype)type_code(dtype), qt = (tbik_dtype)fmt;
+        int st = 0;
+        Py_BEGIN_ALLOW_THREADS
+        switch (kind) {
+            case NORM8: st = CALL(tbik_rmsnorm_fp8)(px, ldx, p2, ld2, pw, eps, ph, ldh, pq, ldq, (float *)ps, t, qt, M, H, stream); break;
+            case NORM8_MX: st = CALL(tbik_rmsnorm_mxfp8)(px, ldx, p2, ld2, pw, eps, ph, ldh, pq, ldq, ps, lds, t, qt, M, H, stream); break;
+            case TAIL8: st = CALL(tbik_combine_residual_rmsnorm_fp8)((const float *)px, shards, p2, ld2, pw, eps, ph, ldh, pq, ldq, (float *)ps, t, qt, M, H, stream); break;
+            case TAIL8_MX: st = CALL(tbik_combine_residual_rmsnorm_mxfp8)((const float *)px, shards, p2, ld2, pw, eps, ph, ldh, pq, ldq, ps, lds, t, qt, M, H, stream); break;
+            case SILU8: st = CALL(tbik_silu_mul_fp8)(px, ldx, p2, ld2, pq, ldq, (float *)ps, t, qt, M, H, stream); break;
+            default: st = CALL(tbik_silu_mul_mxfp8)(px, ldx, p2, ld2, pq, ldq, ps, lds, t, qt, M, H, stream); break;
+        }
+        Py_END_ALLOW_THREADS
+        if (st) return PyLong_FromLong(st);
+        PyObject *o[3] = {silu ? nullptr : tensor_or_none(hidden), tensor_or_none(q), tensor_or_none(scale)};
+        PyObject *all = !o[1] || !o[2] || (!silu && !o[0]) ? nullptr : silu ? PyTuple_Pack(2, o[1], o[2]) : PyTuple_Pack(3, o[0], o[1], o[2]);
+        for (PyObject *i : o) Py_XDECREF(i);
+        return all;
     } catch (const std::exception &) {
         if (PyErr_Occurred()) return nullptr;
         UNCOMMON;
@@ -385,6 +527,8 @@ PyMethodDef methods[] = {
     {"combine", (PyCFunction)(void (*)(void))combine, METH_FASTCALL, nullptr},
     {"row_reduce", (PyCFunction)(void (*)(void))row_reduce, METH_FASTCALL, nullptr},
     {"attention", (PyCFunction)(void (*)(void))attention, METH_FASTCALL, nullptr},
+    {"epilogue", (PyCFunction)(void (*)(void))epilogue, METH_FASTCALL, nullptr},
+    {"eight_bits", (PyCFunction)(void (*)(void))eight_bits, METH_FASTCALL, nullptr},
     {"register", register_entry, METH_VARARGS, nullptr},
     {"use", use, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
