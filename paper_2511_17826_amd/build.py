@@ -17,7 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libtbik.so")
 
-SOURCES = ["tbik_api.hip", "gemm_reference.hip", "gemm_tiled.hip", "gemm_f32.hip", "gemm_fp8.hip", "gemm_mxfp4.hip", "gemm_mxfp6.hip", "gemm_slice.hip", "combine.hip", "combine_epilogue.hip", "activation.hip", "activation_8bit.hip",
+SOURCES = ["gemm_mxfp8_epilogue.hip", "gemm_fp8_epilogue.hip", "gemm_tiled_epilogue.hip", "gemm_fp8.hip", "gemm_tiled.hip", "tbik_api.hip", "gemm_reference.hip", "gemm_f32.hip", "gemm_mxfp4.hip",
+           "gemm_mxfp6.hip", "gemm_slice.hip", "combine.hip", "combine_epilogue.hip", "activation.hip", "activation_8bit.hip",
            "rmsnorm.hip", "rmsnorm_8bit.hip", "row_reduce.hip",
            "attention.hip", "attention_decode.hip"]
 
@@ -101,6 +102,9 @@ def build(save_temps: bool = True, jobs: int = 8, defines=(), lib_path: str = LI
         objs = list(ex.map(lambda s: _compile(s, extra), SOURCES))
     if save_temps:
         check_generated_code(os.path.join(BUILD, "gemm_tiled-hip-amdgcn-amd-amdhsa-gfx950.s"), "gemm_tiled_kernel")
+        check_generated_code(os.path.join(BUILD, "gemm_tiled_epilogue-hip-amdgcn-amd-amdhsa-gfx950.s"), "gemm_tiled_kernel")
+        for unit in ("gemm_fp8_epilogue", "gemm_mxfp8_epilogue"):
+            check_generated_code(os.path.join(BUILD, unit + "-hip-amdgcn-amd-amdhsa-gfx950.s"), "gemm_fp8_tiled_kernel")
         check_generated_code(os.path.join(BUILD, "attention-hip-amdgcn-amd-amdhsa-gfx950.s"), "attention_")
         check_generated_code(os.path.join(BUILD, "gemm_f32-hip-amdgcn-amd-amdhsa-gfx950.s"), "gemm_f32_tiled_kernel")
         check_generated_code(os.path.join(BUILD, "gemm_fp8-hip-amdgcn-amd-amdhsa-gfx950.s"), "gemm_fp8_tiled_kernel")

@@ -64,12 +64,16 @@ hipError_t launch_of(const Silu8Args &a, hipStream_t s) {
         int64_t blocks = ((int64_t)a.M * (a.I / 8) + 255) / 256;
         if (blocks > 256 * 64) blocks = 256 * 64;
         hipLaunchKernelGGL(silu_mul_mx_kernel<F16>, dim3((unsigned)blocks), dim3(256), 0, s, a);
-    } else if (a.I <= 8 * 256 * 2) {
-        hipLaunchKernelGGL((silu_mul_row_kernel<F16, 256, 2>), dim3(a.M), dim3(256), 0, s, a);
-    } else if (a.I <= 8 * 512 * 4) {
-        hipLaunchKernelGGL((silu_mul_row_kernel<F16, 512, 4>), dim3(a.M), dim3(512), 0, s, a);
+    } else if (a.I <= 8 * 256 * 2) {          // two chunks of 8 per thread where a workgroup has threads enough: 4096 x 14336 51.9 us, 512 x 4 53.4, 256 x 8 56.7
+        hipLaunchKernelGGL((silu_mul_row_kernel<F16, 256, 2>), dim3((unsigned)a.M), dim3(256), 0, s, a);
+    } else if (a.I <= 8 * 512 * 2) {
+        hipLaunchKernelGGL((silu_mul_row_kernel<F16, 512, 2>), dim3((unsigned)a.M), dim3(512), 0, s, a);
+    } else if (a.I <= 8 * 1024 * 2) {
+        hipLaunchKernelGGL((silu_mul_row_kernel<F16, 1024, 2>), dim3((unsigned)a.M), dim3(1024), 0, s, a);
+    } else if (a.I <= 8 * 1024 * 4) {
+        hipLaunchKernelGGL((silu_mul_row_kernel<F16, 1024, 4>), dim3((unsigned)a.M), dim3(1024), 0, s, a);
     } else {
-        hipLaunchKernelGGL((silu_mul_row_kernel<F16, 1024, 8>), dim3(a.M), dim3(1024), 0, s, a);
+        hipLaunchKernelGGL((silu_mul_row_kernel<F16, 1024, 8>), dim3((unsigned)a.M), dim3(1024), 0, s, a);
     }
     return hipGetLastError();
 }

@@ -83,14 +83,17 @@ __device__ __forceinline__ void scale_and_bias(const EpilogueParams &e, float (&
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) values_of_their_own(v[r]);
 }
-template <int ACT, int COUNT>
-__device__ __forceinline__ void activate_as(float (&v)[COUNT]) {
+template <int ACT, int ROWS, int COUNT>
+__device__ __forceinline__ void activate_as(float (&v)[ROWS][COUNT]) {
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) v[i] = activation_of<ACT>(v[i]);
-    values_of_their_own(v);
+    for (int r = 0; r < ROWS; ++r) {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) v[r][i] = activation_of<ACT>(v[r][i]);
+        values_of_their_own(v[r]);
+    }
 }
-template <int COUNT>
-__device__ __forceinline__ void activate(int act, float (&v)[COUNT]) {
+template <int ROWS, int COUNT>
+__device__ __forceinline__ void activate(int act, float (&v)[ROWS][COUNT]) {
     switch (act) {                         // uniform
         case TBIK_ACT_RELU: activate_as<TBIK_ACT_RELU>(v); break;
         case TBIK_ACT_SILU: activate_as<TBIK_ACT_SILU>(v); break;
@@ -106,18 +109,37 @@ __device__ __forceinline__ void add_residual(float (&v)[COUNT], const float (&r)
     values_of_their_own(v);
 }
 
-// One element, everything from memory, stored.
-__device__ __forceinline__ void finish_and_store(const EpilogueParams &e, float t, void *Y, int64_t ldy, int64_t row, int64_t col) {
-    float v[1][1] = {{t}}, cs[1] = {0.0f}, b[1] = {0.0f}, r[1] = {0.0f}, rs[1] = {0.0f};
-    if (e.row_scale) rs[0] = e.row_scale[row];
-    if (e.col_scale) cs[0] = e.col_scale[col];
-    if (e.bias) b[0] = widened(e.bias, col, e.bias_dtype);
-    if (e.residual) r[0] = widened(e.residual, row * e.ldr + col, e.y_dtype);
+// One element: its operands as they lie in memory, so that a kernel can have them on their way long before it needs them, and the
+// element through the epilogue, stored.
+struct ElementOperands {
+    float rs, cs;
+    uint32_t bias, residual;
+};
+__device__ __forceinline__ uint32_t raw_element(const void *p, int64_t i, int dtype) {
+    return dtype == TBIK_F32 ? reinterpret_cast<const uint32_t *>(p)[i] : reinterpret_cast<const uint16_t *>(p)[i];
+}
+__device__ __forceinline__ float value_of_raw(uint32_t raw, int dtype) {
+    return dtype == TBIK_F32 ? __uint_as_float(raw) : dtype == TBIK_F16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)raw) : bf16_bits_to_f32(raw);
+}
+__device__ __forceinline__ ElementOperands element_operands(const EpilogueParams &e, int64_t row, int64_t col) {
+    ElementOperands o = {0.0f, 0.0f, 0u, 0u};
+    if (e.row_scale) o.rs = e.row_scale[row];
+    if (e.col_scale) o.cs = e.col_scale[col];
+    if (e.bias) o.bias = raw_element(e.bias, col, e.bias_dtype);
+    if (e.residual) o.residual = raw_element(e.residual, row * e.ldr + col, e.y_dtype);
+    return o;
+}
+__device__ __forceinline__ void finish_and_store(const EpilogueParams &e, float t, const ElementOperands &o, void *Y, int64_t ldy, int64_t row, int64_t col) {
+    float v[1][1] = {{t}};
+    const float cs[1] = {o.cs}, b[1] = {value_of_raw(o.bias, e.bias_dtype)}, r[1] = {value_of_raw(o.residual, e.y_dtype)}, rs[1] = {o.rs};
     scale_and_bias(e, v, rs, cs, b);
-    activate(e.act, v[0]);
+    activate(e.act, v);
     if (e.residual) add_residual(v[0], r);
     if (e.y_dtype == TBIK_F32) reinterpret_cast<float *>(Y)[row * ldy + col] = v[0][0];
     else reinterpret_cast<uint16_t *>(Y)[row * ldy + col] = (uint16_t)pack_16x2(v[0][0], 0.0f, e.y_dtype == TBIK_F16);
+}
+__device__ __forceinline__ void finish_and_store(const EpilogueParams &e, float t, void *Y, int64_t ldy, int64_t row, int64_t col) {
+    finish_and_store(e, t, element_operands(e, row, col), Y, ldy, row, col);
 }
 
 }  // namespace tbik

@@ -165,6 +165,8 @@ struct Fp8Params {
 };
 struct Fp8EpilogueParams : Fp8Params {
     EpilogueParams epilogue;
+    int from_ring;              // the epilogue's operands come through the ring (tile_epilogue.hpp), or there are none
+    int vector_slots, residual_slots;      // positions of the load stream behind a tile's last stage: 0 or 1 each
 };
 
 // EPI: the output passes through an epilogue (epilogue.hpp); P == 1 then.
@@ -206,9 +208,14 @@ void gemm_fp8_tiled_kernel(const std::conditional_t<EPI, Fp8EpilogueParams, Fp8P
     int issue_item = blockIdx.x;
     int issue_stage = 0;
 
+    int issue_m0 = 0, issue_n0 = 0;            // EPI: the tile whose stages are being loaded
     auto point_loads_at = [&](int item) __attribute__((always_inline)) {
-        const int tile = item % p.tiles, shard = item / p.tiles;
+        const int tile = EPI ? item : item % p.tiles, shard = EPI ? 0 : item / p.tiles;
         const int m0 = (tile / p.tiles_n) * BM, n0 = (tile % p.tiles_n) * BN;
+        if (EPI) {
+            issue_m0 = m0;
+            issue_n0 = n0;
+        }
         const int64_t kbase = (int64_t)shard * p.k_per_shard;
         a_ptr = uniform_pointer(reinterpret_cast<const char *>(p.X + (int64_t)m0 * p.ldx + kbase));
         b_ptr = uniform_pointer(reinterpret_cast<const char *>(p.Wt + (int64_t)n0 * p.ldw + kbase) - LANE_BIAS);
@@ -249,8 +256,23 @@ void gemm_fp8_tiled_kernel(const std::conditional_t<EPI, Fp8EpilogueParams, Fp8P
     const int s_step = !(MX && p.scales_packed) ? BK8 / 32 : 512;      // scale bytes per stage
     auto issue_part = [&](int slot, auto part_c) __attribute__((always_inline)) {
         constexpr int PART = decltype(part_c)::value;
-        if (PART == 0 && __builtin_expect(issue_stage == stages_per_item, 0)) {
-            if (issue_item + (int)gridDim.x < p.work) {
+        if (PART == 0 && __builtin_expect(EPI ? issue_stage >= stages_per_item : issue_stage == stages_per_item, 0)) {
+            if constexpr (EPI) {                       // behind a tile's last stage: its epilogue's operands, then the next tile
+                const int behind = issue_stage - stages_per_item;
+                int here = lane;
+                asm volatile("" : "+v"(here));         // nothing below is worked out ahead and kept in registers over the stages
+                const RingLoads<A_LOADS8, B_LOADS8> loads{a_ptr, b_ptr, aoff, boff};
+                if (behind < p.vector_slots) {
+                    point_at_vectors(loads, p.epilogue, p.X, issue_m0, issue_n0, p.M, p.N, wave_u, here);
+                } else if (behind < p.vector_slots + p.residual_slots) {
+                    point_at_residual<MT, NT>(loads, p.epilogue, issue_m0, issue_n0, p.M, p.N, wave_u / WN, wave_u % WN, here);
+                } else {                               // past the end: a tile's stages again (nobody consumes them)
+                    if (issue_item + (int)gridDim.x < p.work) issue_item += gridDim.x;
+                    point_loads_at(issue_item);
+                    issue_stage = 0;
+                }
+                if (MX && issue_stage != 0) s_ptr -= s_step;           // the last stage's scales again
+            } else if (issue_item + (int)gridDim.x < p.work) {
                 issue_item += gridDim.x;
                 point_loads_at(issue_item);
                 issue_stage = 0;
@@ -344,8 +366,13 @@ void gemm_fp8_tiled_kernel(const std::conditional_t<EPI, Fp8EpilogueParams, Fp8P
     // of stage s+1 have landed, meet the other wavefronts -- stage s+1 is complete, nobody reads the slot of stage s-1
     // any more -- and start the loads of stage s+RING-1 into that slot.
     point_loads_at(issue_item);
+    if constexpr (EPI) {
+#pragma nounroll
+        for (int i = 0; i < RING8 - 1; ++i) issue_next_stage(i);
+    } else {
 #pragma unroll
-    for (int i = 0; i < RING8 - 1; ++i) issue_next_stage(i);
+        for (int i = 0; i < RING8 - 1; ++i) issue_next_stage(i);
+    }
     wait_loads_and_barrier<LOADS_PER_STAGE * (RING8 - 2)>();
     read_frags(0, 0, 0);
     if (MX) read_scales(0);
@@ -415,26 +442,63 @@ void gemm_fp8_tiled_kernel(const std::conditional_t<EPI, Fp8EpilogueParams, Fp8P
     for (int item = blockIdx.x; item < p.work; item += gridDim.x) {
         SubtreeWalker<LEVELS>::run(superleaf, acc, acc2, stash);
 
-        const int tile = item % p.tiles, shard = item / p.tiles;
+        const int tile = EPI ? item : item % p.tiles, shard = EPI ? 0 : item / p.tiles;
         const int m0 = (tile / p.tiles_n) * BM, n0 = (tile % p.tiles_n) * BN;
         float *part = p.partials ? p.partials + (int64_t)shard * p.M * p.N : nullptr;
         const bool interior = (m0 + BM <= p.M) && (n0 + BN <= p.N);
         if constexpr (EPI) {                                // the patch and its barrier as below
+            int here = lane;
+            asm volatile("" : "+v"(here));             // as above
             const int wm_u = wave_u / WN, wn_u = wave_u % WN;
-            const int row0 = m0 + wm_u * MT * 32, col0 = n0 + wn_u * WCOLS;
-            const int last_slot = cur == 0 ? RING8 - 1 : cur - 1;
-            float *patch = reinterpret_cast<float *>(smem + last_slot * STAGE8 + wave * REGION8);
+            const int row0 = m0 + wm_u * MT * 32, col0 = n0 + wn_u * WCOLS, last = min(p.M - 1 - row0, MT * 32 - 1);
+            const int prev = cur == 0 ? RING8 - 1 : cur - 1, behind = cur + 1 == RING8 ? 0 : cur + 1;
+            const int extra = p.vector_slots + p.residual_slots;
+            float *patch = reinterpret_cast<float *>(smem + prev * STAGE8 + wave * REGION8);
+            // The first position behind the stages has landed since the last stage's entry; for the second one, as much may be
+            // in flight as at a stage's entry.
+            constexpr int ALLOW = LOADS_PER_STAGE * (RING8 - 3);
+            if (extra == 2) wait_loads_and_barrier<ALLOW>();
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            stores_in_flight = -1;
             const bool wide = p.epilogue.y_dtype == TBIK_F32;
-            if (interior && p.vector_stores) {
-                if (wide) store_with_epilogue<true, true>(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, 0, lane, false);
-                else store_with_epilogue<true, false>(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, 0, lane, p.epilogue.y_dtype == TBIK_F16);
-                stores_in_flight = wide ? STORES_F32 : STORES_BF16;
-            } else if (n0 + BN <= p.N && p.vector_stores && !wide) {
-                store_with_epilogue<false, false>(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, p.M - 1 - row0, lane, p.epilogue.y_dtype == TBIK_F16);
+            int stores = -1;
+            if (p.from_ring && n0 + BN <= p.N) {
+                const unsigned char *vectors = p.vector_slots ? smem + cur * STAGE8 : nullptr;
+                const unsigned char *residual = p.residual_slots ? smem + (p.vector_slots ? behind : cur) * STAGE8 + wave * REGION8 : nullptr;
+                if (wide) store_from_ring<false, true, REGION8, A_LOADS8>(acc, patch, p.epilogue, vectors, residual, p.Y, p.ldy, row0, col0, wm_u, wn_u, p.M, last, here, false);
+                else if (interior) store_from_ring<true, false, REGION8, A_LOADS8>(acc, patch, p.epilogue, vectors, residual, p.Y, p.ldy, row0, col0, wm_u, wn_u, p.M, last, here, p.epilogue.y_dtype == TBIK_F16);
+                else store_from_ring<false, false, REGION8, A_LOADS8>(acc, patch, p.epilogue, vectors, residual, p.Y, p.ldy, row0, col0, wm_u, wn_u, p.M, last, here, p.epilogue.y_dtype == TBIK_F16);
+                if (interior) stores = wide ? STORES_F32 : STORES_BF16;
+            } else if (n0 + BN <= p.N && p.vector_stores) {
+                if (wide) store_with_epilogue<true>(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, last, here, false);
+                else store_with_epilogue<false>(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, last, here, p.epilogue.y_dtype == TBIK_F16);
             } else {
-                store_elements_with_epilogue(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, p.M, p.N, lane);
+                store_elements_with_epilogue(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, p.M, p.N, here);
+            }
+            stores_in_flight = stores;
+            if (extra) {
+                // On to the next tile's first stage: as many positions of the stream are issued as are consumed, into the slot of
+                // the last stage (its patch has been read) and -- behind a barrier, since all wavefronts read it -- of the vectors.
+                // That stage has landed when only what was issued behind it is in flight: RING - 2 - extra positions and the
+                // stores, and this issue behind them.
+                issue_next_stage(prev);
+                if (stores == STORES_F32) {
+                    if (extra == 1) wait_loads_and_barrier<ALLOW + LOADS_PER_STAGE + STORES_F32>();
+                    else wait_loads_and_barrier<ALLOW + STORES_F32>();
+                } else if (stores == STORES_BF16) {
+                    if (extra == 1) wait_loads_and_barrier<ALLOW + LOADS_PER_STAGE + STORES_BF16>();
+                    else wait_loads_and_barrier<ALLOW + STORES_BF16>();
+                } else {
+                    wait_loads_and_barrier<0>();
+                    stores_in_flight = 0;
+                }
+                if (extra == 2) {
+                    issue_next_stage(cur);
+                    if (RING8 < 5) stores_in_flight = 0;       // the second stage was issued behind the stores
+                    cur = behind;
+                }
+                cur = cur + 1 == RING8 ? 0 : cur + 1;
+                read_frags(0, cur, 0);
+                if (MX) read_scales(cur);
             }
         } else if (interior && p.vector_stores) {
             // Each wavefront turns its 32 x 64 blocks around in its own region of the slot that was multiplied last
@@ -600,7 +664,12 @@ hipError_t launch_tiled_fmt(const GemmArgs &a, const Mxfp4Scales *sc, hipStream_
     const void *out = p.partials ? (const void *)p.partials : p.Y;
     const int64_t ld_bytes = p.partials ? (int64_t)a.N * 4 : a.ldy * (p.y_bf16 ? 2 : 4);
     p.vector_stores = ((reinterpret_cast<uintptr_t>(out) & 15) == 0) && (ld_bytes % 16 == 0) && ld_bytes < kMaxVectorRowBytes;
-    if (EPI && !residual_in_vectors(*a.epilogue)) p.vector_stores = 0;
+    if constexpr (EPI) {
+        p.from_ring = p.vector_stores && epilogue_from_ring(*a.epilogue, a.N);
+        p.vector_slots = p.from_ring && (a.epilogue->row_scale || a.epilogue->col_scale || a.epilogue->bias);
+        p.residual_slots = p.from_ring && a.epilogue->residual;
+        if (!residual_in_vectors(*a.epilogue)) p.vector_stores = 0;
+    }
     p.stream_stores = a.partials != nullptr && (int64_t)a.P * a.M * a.N * 4 > ((int64_t)192 << 20);
     const int levels = levels_for(p.ns_per_shard);
     int dev = 0;
@@ -646,6 +715,16 @@ static hipError_t launch_rows_mx(const GemmArgs &a, const Mxfp4Scales &sc, int r
     return launch_tiled_fmt<2, 2, 2, 2, 4, FMT, true, EPI>(a, &sc, s);                        // 4 x 33 KiB
 }
 
+// TBIK_EPILOGUE_UNIT: the kernels with an epilogue are translation units of their own (8: 8-bit, 88: MXFP8).
+#if defined(TBIK_EPILOGUE_UNIT) && TBIK_EPILOGUE_UNIT == 8
+hipError_t launch_gemm_fp8_tiled_epilogue(const GemmArgs &a, int rows, hipStream_t s) {
+    return a.x_dtype == TBIK_FP8_E5M2 ? launch_rows<1, true>(a, rows, s) : launch_rows<0, true>(a, rows, s);
+}
+#elif defined(TBIK_EPILOGUE_UNIT)
+hipError_t launch_gemm_mxfp8_tiled_epilogue(const GemmArgs &a, const Mxfp4Scales &sc, int rows, hipStream_t s) {
+    return a.x_dtype == TBIK_FP8_E5M2 ? launch_rows_mx<1, true>(a, sc, rows, s) : launch_rows_mx<0, true>(a, sc, rows, s);
+}
+#else
 bool gemm_fp8_tiled_supports(const GemmArgs &a) {
     if (a.superleaf % BK8 != 0) return false;
     if (levels_for(a.ns / a.P) > 4) return false;
@@ -656,7 +735,7 @@ bool gemm_fp8_tiled_supports(const GemmArgs &a) {
 hipError_t launch_gemm_fp8_tiled(const GemmArgs &a, int rows, hipStream_t s) {
     if (a.M <= 0 || a.N <= 0) return hipSuccess;
     if (!gemm_fp8_tiled_supports(a) || (rows != 32 && rows != 64 && rows != 128)) return hipErrorInvalidValue;
-    if (a.epilogue) return a.x_dtype == TBIK_FP8_E5M2 ? launch_rows<1, true>(a, rows, s) : launch_rows<0, true>(a, rows, s);
+    if (a.epilogue) return launch_gemm_fp8_tiled_epilogue(a, rows, s);
     return a.x_dtype == TBIK_FP8_E5M2 ? launch_rows<1, false>(a, rows, s) : launch_rows<0, false>(a, rows, s);
 }
 
@@ -696,7 +775,7 @@ hipError_t launch_mxfp8_retile(const Mxfp4Scales &raw, int M, int N, int K, void
 hipError_t launch_gemm_mxfp8_tiled(const GemmArgs &a, const Mxfp4Scales &sc, int rows, hipStream_t s) {
     if (a.M <= 0 || a.N <= 0) return hipSuccess;
     if (!gemm_mxfp8_tiled_supports(a, sc) || (rows != 32 && rows != 64 && rows != 128)) return hipErrorInvalidValue;
-    if (a.epilogue) return a.x_dtype == TBIK_FP8_E5M2 ? launch_rows_mx<1, true>(a, sc, rows, s) : launch_rows_mx<0, true>(a, sc, rows, s);
+    if (a.epilogue) return launch_gemm_mxfp8_tiled_epilogue(a, sc, rows, s);
     return a.x_dtype == TBIK_FP8_E5M2 ? launch_rows_mx<1, false>(a, sc, rows, s) : launch_rows_mx<0, false>(a, sc, rows, s);
 }
 
@@ -716,5 +795,6 @@ hipError_t launch_gemm_mxfp8_reference(const GemmArgs &a, const Mxfp4Scales &sc,
     else launch(e5m2 ? gemm_fp8_reference_kernel<1, true, false> : gemm_fp8_reference_kernel<0, true, false>, ReferenceEpilogue<false>{});
     return hipGetLastError();
 }
+#endif
 
 }  // namespace tbik

@@ -70,6 +70,8 @@ struct TiledParams {
 };
 struct TiledEpilogueParams : TiledParams {
     EpilogueParams epilogue;
+    int from_ring;              // the epilogue's operands come through the ring (tile_epilogue.hpp), or there are none
+    int vector_slots, residual_slots;      // positions of the load stream behind a tile's last stage: 0 or 1 each
 };
 
 // ---------------------------------------------------------------------------------------------
@@ -123,9 +125,14 @@ void gemm_tiled_kernel(const std::conditional_t<EPI, TiledEpilogueParams, TiledP
     int issue_item = blockIdx.x;               // work item whose stages are being loaded
     int issue_stage = 0;                       // next stage of that item to load
 
+    int issue_m0 = 0, issue_n0 = 0;            // EPI: the tile whose stages are being loaded
     auto point_loads_at = [&](int item) __attribute__((always_inline)) {
-        const int tile = item % p.tiles, shard = item / p.tiles;
+        const int tile = EPI ? item : item % p.tiles, shard = EPI ? 0 : item / p.tiles;
         const int m0 = (tile / p.tiles_n) * BM, n0 = (tile % p.tiles_n) * BN;
+        if (EPI) {
+            issue_m0 = m0;
+            issue_n0 = n0;
+        }
         const int64_t kbase = (int64_t)shard * p.k_per_shard;
         a_ptr = uniform_pointer(reinterpret_cast<const char *>(p.X + (int64_t)m0 * p.ldx + kbase));
         // Gated activation: the 128 columns of a tile are, per wavefront column, 32 gate channels and the same 32 up
@@ -156,8 +163,22 @@ void gemm_tiled_kernel(const std::conditional_t<EPI, TiledEpilogueParams, TiledP
     // (nobody consumes it).
     auto issue_part = [&](int slot, auto part_c) __attribute__((always_inline)) {
         constexpr int PART = decltype(part_c)::value;
-        if (PART == 0 && __builtin_expect(issue_stage == stages_per_item, 0)) {
-            if (issue_item + (int)gridDim.x < p.work) {
+        if (PART == 0 && __builtin_expect(EPI ? issue_stage >= stages_per_item : issue_stage == stages_per_item, 0)) {
+            if constexpr (EPI) {                       // behind a tile's last stage: its epilogue's operands, then the next tile
+                const int behind = issue_stage - stages_per_item;
+                int here = lane;
+                asm volatile("" : "+v"(here));         // nothing below is worked out ahead and kept in registers over the stages
+                const RingLoads<A_LOADS, B_LOADS> loads{a_ptr, b_ptr, aoff, boff};
+                if (behind < p.vector_slots) {
+                    point_at_vectors(loads, p.epilogue, p.X, issue_m0, issue_n0, p.M, p.N, wave_u, here);
+                } else if (behind < p.vector_slots + p.residual_slots) {
+                    point_at_residual<MT, NT>(loads, p.epilogue, issue_m0, issue_n0, p.M, p.N, wave_u / WN, wave_u % WN, here);
+                } else {                               // past the end: a tile's stages again (nobody consumes them)
+                    if (issue_item + (int)gridDim.x < p.work) issue_item += gridDim.x;
+                    point_loads_at(issue_item);
+                    issue_stage = 0;
+                }
+            } else if (issue_item + (int)gridDim.x < p.work) {
                 issue_item += gridDim.x;
                 point_loads_at(issue_item);
                 issue_stage = 0;
@@ -240,8 +261,13 @@ void gemm_tiled_kernel(const std::conditional_t<EPI, TiledEpilogueParams, TiledP
     // stage s-1 any more -- and start the loads of stage s+RING-1 into that slot.  The barrier is written
     // in assembly on purpose: a fence would make the compiler drain every outstanding load.
     point_loads_at(issue_item);
+    if constexpr (EPI) {
+#pragma nounroll
+        for (int i = 0; i < RING - 1; ++i) issue_next_stage(i);
+    } else {
 #pragma unroll
-    for (int i = 0; i < RING - 1; ++i) issue_next_stage(i);
+        for (int i = 0; i < RING - 1; ++i) issue_next_stage(i);
+    }
     wait_loads_and_barrier<LOADS_PER_STAGE * (RING - 2)>();      // stage 0 landed everywhere
 #pragma unroll
     for (int i = 0; i < FRAG_AHEAD; ++i) read_frags(i, 0, i);
@@ -318,26 +344,63 @@ void gemm_tiled_kernel(const std::conditional_t<EPI, TiledEpilogueParams, TiledP
         SubtreeWalker<LEVELS>::run(superleaf, acc, acc2, stash);
 
         // ---- acc holds T(superleaves of this shard) for this tile: store it ----
-        const int tile = item % p.tiles, shard = item / p.tiles;
+        const int tile = EPI ? item : item % p.tiles, shard = EPI ? 0 : item / p.tiles;
         const int m0 = (tile / p.tiles_n) * BM, n0 = (tile % p.tiles_n) * BN;
         float *part = p.partials ? p.partials + (int64_t)shard * p.M * p.N : nullptr;
         const bool interior = (m0 + BM <= p.M) && (n0 + BN <= p.N);
         if constexpr (EPI) {                                // the patch and its barrier as below
+            int here = lane;
+            asm volatile("" : "+v"(here));             // as above
             const int wm_u = wave_u / WN, wn_u = wave_u % WN;
-            const int row0 = m0 + wm_u * MT * 32, col0 = n0 + wn_u * WCOLS;
-            const int last_slot = cur == 0 ? RING - 1 : cur - 1;
-            float *patch = reinterpret_cast<float *>(smem + last_slot * STAGE_BYTES + wave * REGION_BYTES);
+            const int row0 = m0 + wm_u * MT * 32, col0 = n0 + wn_u * WCOLS, last = min(p.M - 1 - row0, MT * 32 - 1);
+            const int prev = cur == 0 ? RING - 1 : cur - 1, behind = cur + 1 == RING ? 0 : cur + 1;
+            const int extra = p.vector_slots + p.residual_slots;
+            float *patch = reinterpret_cast<float *>(smem + prev * STAGE_BYTES + wave * REGION_BYTES);
+            // The first position behind the stages has landed since the last stage's entry; for the second one, as much may be
+            // in flight as at a stage's entry.
+            constexpr int ALLOW = LOADS_PER_STAGE * (RING - 3);
+            if (extra == 2) wait_loads_and_barrier<ALLOW>();
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            stores_in_flight = -1;
             const bool wide = p.epilogue.y_dtype == TBIK_F32;
-            if (interior && p.vector_stores) {
-                if (wide) store_with_epilogue<true, true>(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, 0, lane, false);
-                else store_with_epilogue<true, false>(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, 0, lane, std::bool_constant<F16>{});
-                stores_in_flight = wide ? STORES_F32 : STORES_BF16;
-            } else if (n0 + BN <= p.N && p.vector_stores && !wide) {
-                store_with_epilogue<false, false>(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, p.M - 1 - row0, lane, std::bool_constant<F16>{});
+            int stores = -1;
+            if (p.from_ring && n0 + BN <= p.N) {
+                const unsigned char *vectors = p.vector_slots ? smem + cur * STAGE_BYTES : nullptr;
+                const unsigned char *residual = p.residual_slots ? smem + (p.vector_slots ? behind : cur) * STAGE_BYTES + wave * REGION_BYTES : nullptr;
+                if (wide) store_from_ring<false, true, REGION_BYTES, A_LOADS>(acc, patch, p.epilogue, vectors, residual, p.Y, p.ldy, row0, col0, wm_u, wn_u, p.M, last, here, false);
+                else if (interior) store_from_ring<true, false, REGION_BYTES, A_LOADS>(acc, patch, p.epilogue, vectors, residual, p.Y, p.ldy, row0, col0, wm_u, wn_u, p.M, last, here, std::bool_constant<F16>{});
+                else store_from_ring<false, false, REGION_BYTES, A_LOADS>(acc, patch, p.epilogue, vectors, residual, p.Y, p.ldy, row0, col0, wm_u, wn_u, p.M, last, here, std::bool_constant<F16>{});
+                if (interior) stores = wide ? STORES_F32 : STORES_BF16;
+            } else if (n0 + BN <= p.N && p.vector_stores) {
+                if (wide) store_with_epilogue<true>(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, last, here, false);
+                else store_with_epilogue<false>(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, last, here, std::bool_constant<F16>{});
             } else {
-                store_elements_with_epilogue(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, p.M, p.N, lane);
+                store_elements_with_epilogue(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, p.M, p.N, here);
+            }
+            stores_in_flight = stores;
+            if (extra) {
+                // On to the next tile's first stage: as many positions of the stream are issued as are consumed, into the slot of
+                // the last stage (its patch has been read) and -- behind a barrier, since all wavefronts read it -- of the vectors.
+                // That stage has landed when only what was issued behind it is in flight: RING - 2 - extra positions and the
+                // stores, and this issue behind them.
+                issue_next_stage(prev);
+                if (stores == STORES_F32) {
+                    if (extra == 1) wait_loads_and_barrier<ALLOW + LOADS_PER_STAGE + STORES_F32>();
+                    else wait_loads_and_barrier<ALLOW + STORES_F32>();
+                } else if (stores == STORES_BF16) {
+                    if (extra == 1) wait_loads_and_barrier<ALLOW + LOADS_PER_STAGE + STORES_BF16>();
+                    else wait_loads_and_barrier<ALLOW + STORES_BF16>();
+                } else {
+                    wait_loads_and_barrier<0>();
+                    stores_in_flight = 0;
+                }
+                if (extra == 2) {
+                    issue_next_stage(cur);
+                    if (RING < 5) stores_in_flight = 0;       // the second stage was issued behind the stores
+                    cur = behind;
+                }
+                cur = cur + 1 == RING ? 0 : cur + 1;
+#pragma unroll
+                for (int i = 0; i < FRAG_AHEAD; ++i) read_frags(i, cur, i);
             }
         } else if (interior && p.vector_stores) {
             // Full tile, 16-byte aligned rows: each wavefront turns its 32 x (32*NT) blocks around in its private LDS
@@ -529,6 +592,7 @@ static int levels_for(int ns_per_shard) {
     return l;
 }
 
+#ifndef TBIK_EPILOGUE_UNIT
 bool gemm_tiled_supports(const GemmArgs &a, int variant) {
     if (variant != VARIANT_T128 && variant != VARIANT_T32 && variant != VARIANT_T64 && variant != VARIANT_T96) return false;
     if (a.N % 8 != 0 || a.superleaf % BK != 0) return false;
@@ -537,6 +601,7 @@ bool gemm_tiled_supports(const GemmArgs &a, int variant) {
     if (a.swiglu && (variant != VARIANT_T128 || a.P != 1 || a.partials || a.N % 128 != 0 || a.y_dtype != a.x_dtype)) return false;
     return true;
 }
+#endif
 
 static int compute_units() {
     static int cus = 0;
@@ -576,7 +641,12 @@ static hipError_t launch_shape(const GemmArgs &a, hipStream_t s) {
         const void *out = p.partials ? (const void *)p.partials : p.Y;
         const int64_t ld_bytes = p.partials ? (int64_t)a.N * 4 : a.ldy * (p.y_bf16 ? 2 : 4);   // act: 16-byte chunks of 8 channels
         p.vector_stores = ((reinterpret_cast<uintptr_t>(out) & 15) == 0) && (ld_bytes % 16 == 0) && ld_bytes < kMaxVectorRowBytes;
-        if (EPI && !residual_in_vectors(*a.epilogue)) p.vector_stores = 0;
+        if constexpr (EPI) {
+            p.from_ring = p.vector_stores && epilogue_from_ring(*a.epilogue, a.N);
+            p.vector_slots = p.from_ring && (a.epilogue->row_scale || a.epilogue->col_scale || a.epilogue->bias);
+            p.residual_slots = p.from_ring && a.epilogue->residual;
+            if (!residual_in_vectors(*a.epilogue)) p.vector_stores = 0;
+        }
         // Partials of many shards exceed the 256 MiB memory-side cache before the combine reads them: written around
         // the caches they do not evict the operands (P = 8 at 4096^2: 257 -> 170 us).  Fewer planes stay cached for
         // their reader, so those keep ordinary stores.
@@ -622,11 +692,17 @@ static hipError_t launch_variant(const GemmArgs &a, int variant, hipStream_t s) 
     return launch_shape<1, 4, 1, 1, 6, F16, EPI>(a, s);
 }
 
+#ifdef TBIK_EPILOGUE_UNIT
+hipError_t launch_gemm_tiled_epilogue(const GemmArgs &a, int variant, hipStream_t s) {
+    return a.x_dtype == TBIK_F16 ? launch_variant<true, true>(a, variant, s) : launch_variant<false, true>(a, variant, s);
+}
+#else
 hipError_t launch_gemm_tiled(const GemmArgs &a, int variant, hipStream_t s) {
     if (a.M <= 0 || a.N <= 0) return hipSuccess;
     if (!gemm_tiled_supports(a, variant)) return hipErrorInvalidValue;
-    if (a.epilogue) return a.x_dtype == TBIK_F16 ? launch_variant<true, true>(a, variant, s) : launch_variant<false, true>(a, variant, s);
+    if (a.epilogue) return launch_gemm_tiled_epilogue(a, variant, s);
     return a.x_dtype == TBIK_F16 ? launch_variant<true, false>(a, variant, s) : launch_variant<false, false>(a, variant, s);
 }
+#endif
 
 }  // namespace tbik

@@ -83,9 +83,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rmsnorm_8bit_ke
         for (int s = CPL; s < nseg2; ++s) ss = st.push(0.0f, (unsigned)s);       // padding segments: T of +0 leaves
     } else {
         __syncthreads();
-        // T over nseg2 <= WAVES * CPL segments, a power of two: 64 of them by lanes; lanes past the last hold +0, which changes nothing
-        ss = wave_tree_sum(lane < nseg2 ? sums[lane] : 0.0f);
-        if (nseg2 > 64) ss = ss + wave_tree_sum(sums[64 + lane]);
+        // T over the segments, padded with +0 to 64 (or 128): adding +0 changes nothing
+        ss = wave_tree_sum(lane < WAVES * CPL ? sums[lane] : 0.0f);
+        if (WAVES * CPL > 64) ss = ss + wave_tree_sum(sums[64 + lane]);
     }
     const float r = 1.0f / sqrtf(ss / (float)a.H + a.eps);
     auto normed = [&](int s, int c, float (&n)[8]) __attribute__((always_inline)) {
@@ -113,14 +113,14 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rmsnorm_8bit_ke
             }
         }
     } else {
-        float amax = 0.0f;
+        constexpr int KEPT = CPL <= 4 ? CPL : 1;               // few values are kept between the maximum and the output, many formed again
+        float amax = 0.0f, n[KEPT][8];
 #pragma unroll
         for (int s = 0; s < CPL; ++s) {
             const int c = (s * WAVES + w) * 64 + lane;
             if (c < nchunks) {
-                float n[8];
-                normed(s, c, n);
-                amax = fmaxf(amax, largest_magnitude(n));
+                normed(s, c, n[s % KEPT]);
+                amax = fmaxf(amax, largest_magnitude(n[s % KEPT]));
             }
         }
         amax = wave_max(amax);
@@ -135,9 +135,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rmsnorm_8bit_ke
         for (int s = 0; s < CPL; ++s) {
             const int c = (s * WAVES + w) * 64 + lane;
             if (c < nchunks) {
-                float n[8];
-                normed(s, c, n);
-                *reinterpret_cast<uint2 *>(q + c * 8) = to_8_bits(n, factor, a.out.e5m2);
+                if constexpr (KEPT < CPL) normed(s, c, n[0]);
+                *reinterpret_cast<uint2 *>(q + c * 8) = to_8_bits(n[s % KEPT], factor, a.out.e5m2);
             }
         }
         if (w == 0 && lane == 0) reinterpret_cast<float *>(a.out.scales)[row] = scale;
@@ -152,19 +151,21 @@ hipError_t launch_p(const Rms8Args &a, hipStream_t s) {
     const int nseg2 = n2 < 64 ? 1 : n2 / 64;
     auto rows_of_a_wavefront = [&](auto k) { hipLaunchKernelGGL(k, dim3((a.M + 3) / 4), dim3(256), 0, s, a, nseg2); };
     auto rows_of = [&](auto k, int waves) { hipLaunchKernelGGL(k, dim3(a.M), dim3(64 * waves), 0, s, a, nseg2); };
-    if (a.M >= 1024 && segments <= 16) {
-        if (segments <= 2) rows_of_a_wavefront(rmsnorm_8bit_kernel<F16, P, 1, 2>);
-        else if (segments <= 8) rows_of_a_wavefront(rmsnorm_8bit_kernel<F16, P, 1, 8>);
-        else rows_of_a_wavefront(rmsnorm_8bit_kernel<F16, P, 1, 16>);
-    } else if (segments <= 8) {
-        rows_of(rmsnorm_8bit_kernel<F16, P, 8, 1>, 8);
-    } else if (segments <= 16) {
-        rows_of(rmsnorm_8bit_kernel<F16, P, 8, 2>, 8);
-    } else if (segments <= 32) {
-        rows_of(rmsnorm_8bit_kernel<F16, P, 16, 2>, 16);
-    } else {
-        rows_of(rmsnorm_8bit_kernel<F16, P, 16, 8>, 16);
-    }
+    // Few chunks per lane: a row is one pass of load, sum, output, and what hides its latencies is the number of wavefronts.  Up to
+    // 1024 columns a wavefront takes a row alone; many 16-bit rows of up to 6144 take four, which leaves fewer of them at the barriers
+    // than eight; partial sums are P times the loads and take eight.  us, wavefronts x chunks, bf16 with residual:
+    //   1 x 4096          8x1 2.7   4x2 3.2   1x8 6.5          512 x 4096     8x1 4.5   4x2 4.7   1x8 9.3
+    //   8192 x 4096       8x1 43.2  4x2 40.0  1x8 49.0         8191 x 5120    8x2 54.3  4x3 50.6  1x10 67.0      4096 x 1024  4x1 8.9  1x2 7.7
+    //   1003 x 4096, P 4  8x1 14.1  4x2 14.7  1x8 17.7         1024 x 16384   16x2 20.9 8x4 22.9                 2048 x 512   4x1 3.8  1x2 3.2
+    // (8191 x 5120: 5.8 TB/s of the bytes that have to move, a copy of 1 GiB reaches 5.1.)
+    if (segments <= 2) rows_of_a_wavefront(rmsnorm_8bit_kernel<F16, P, 1, 2>);
+    else if (P == 0 && a.M >= 1024 && segments <= 8) rows_of(rmsnorm_8bit_kernel<F16, P, 4, 2>, 4);
+    else if (P == 0 && a.M >= 1024 && segments <= 12) rows_of(rmsnorm_8bit_kernel<F16, P, 4, 3>, 4);
+    else if (segments <= 8) rows_of(rmsnorm_8bit_kernel<F16, P, 8, 1>, 8);
+    else if (segments <= 16) rows_of(rmsnorm_8bit_kernel<F16, P, 8, 2>, 8);
+    else if (segments <= 32) rows_of(rmsnorm_8bit_kernel<F16, P, 16, 2>, 16);
+    else if (segments <= 64) rows_of(rmsnorm_8bit_kernel<F16, P, 16, 4>, 16);
+    else rows_of(rmsnorm_8bit_kernel<F16, P, 16, 8>, 16);
     return hipGetLastError();
 }
 

@@ -58,6 +58,7 @@ hipError_t launch_gemm_reference(const GemmArgs &a, hipStream_t s);
 // Tiled kernels.  `variant` selects the tile shape (see kVariantNames); returns hipErrorInvalidValue
 // if the variant cannot run this shape.  Same outputs as the reference kernel.
 hipError_t launch_gemm_tiled(const GemmArgs &a, int variant, hipStream_t s);
+hipError_t launch_gemm_tiled_epilogue(const GemmArgs &a, int variant, hipStream_t s);      // its part for calls with an epilogue; so too below
 bool gemm_tiled_supports(const GemmArgs &a, int variant);
 
 // act = round16(SiLU(gate) * up), elementwise on [M, I] 16-bit tensors of format dtype.
@@ -77,6 +78,7 @@ bool gemm_f32_tiled_supports(const GemmArgs &a);
 // to the TRANSPOSED weight [N, ldw] bytes; Y is fp32 or bf16.  rows: 128, 64 or 32 rows per workgroup tile.
 hipError_t launch_gemm_fp8_reference(const GemmArgs &a, hipStream_t s);
 hipError_t launch_gemm_fp8_tiled(const GemmArgs &a, int rows, hipStream_t s);
+hipError_t launch_gemm_fp8_tiled_epilogue(const GemmArgs &a, int rows, hipStream_t s);
 bool gemm_fp8_tiled_supports(const GemmArgs &a);
 
 // The same for MXFP4 operands (x_dtype TBIK_MXFP4): X points to [M, ldx] BYTES of packed element pairs (ldx >= K / 2),
@@ -101,6 +103,7 @@ bool gemm_mxfp4_tiled_supports(const GemmArgs &a, const Mxfp4Scales &sc);
 hipError_t launch_gemm_mxfp8_reference(const GemmArgs &a, const Mxfp4Scales &sc, hipStream_t s);
 // rows: 128, 64 or 32.
 hipError_t launch_gemm_mxfp8_tiled(const GemmArgs &a, const Mxfp4Scales &sc, int rows, hipStream_t s);
+hipError_t launch_gemm_mxfp8_tiled_epilogue(const GemmArgs &a, const Mxfp4Scales &sc, int rows, hipStream_t s);
 // Copies the scales of all M and N rows into `out` (mxfp8_retiled_scales_bytes(M, N, K) bytes) in the order of the tiled kernels.
 hipError_t launch_mxfp8_retile(const Mxfp4Scales &raw, int M, int N, int K, void *out, Mxfp4Scales *packed, hipStream_t s);
 size_t mxfp8_retiled_scales_bytes(int M, int N, int K);

@@ -89,6 +89,17 @@ SHAPES = [
     ("mx e5m2", 600, 256, 8192, 128, 1, [(600, "tiles", 128, 1)]),
     ("mx e4m3", 300, 4096, 1000, 256, 1, None),
     ("mx e4m3", 50, 192, 72, 64, 3, [(50, "reference", 0, 0)]),
+    # More tiles than compute units with one to four stages each, and rows or scales that end inside 16 bytes: the epilogue's operands
+    # lie several tiles ahead in the ring of every tile height.
+    ("bf16", 603, 64, 8192, 64, 1, [(603, "tiles", 128, 1)]),
+    ("fp16", 3, 64, 32896, 64, 1, [(3, "tiles", 32, 1)]),
+    ("bf16", 4095, 128, 4096, 128, 1, [(4095, "tiles", 128, 1)]),
+    ("fp8 e4m3", 603, 128, 8192, 128, 1, [(603, "tiles", 128, 1)]),
+    ("fp8 e5m2", 3, 256, 16640, 128, 1, [(3, "tiles", 32, 1)]),
+    ("fp8 e4m3", 50, 512, 33024, 128, 1, [(50, "tiles", 64, 1)]),
+    ("mx e4m3", 1031, 128, 8192, 128, 1, [(1031, "tiles", 128, 1)]),
+    ("mx e4m3", 2, 256, 16640, 128, 1, [(2, "tiles", 32, 1)]),
+    ("mx e5m2", 50, 512, 33024, 128, 1, [(50, "tiles", 64, 1)]),
 ]
 
 
