@@ -212,6 +212,7 @@ void gemm_tiled_kernel(const std::conditional_t<EPI, TiledEpilogueParams, TiledP
     for (int a = 0; a < MT; ++a) {
         const int R = (wm * MT + a) * 32 + li;
         a_off[a] = (R / (8 * A_LOADS)) * REGION_BYTES + (R % (8 * A_LOADS)) * A_ROW;
+        if (EPI && 32 % (8 * A_LOADS) == 0) a_off[a] = a_off[0] + a * (32 / (8 * A_LOADS)) * REGION_BYTES;      // the same, as one address register
     }
     const int a_sw = (lg ^ ((li >> 1) & 7)) << 4;
     // W fragment b, half h, K-step ks: region ks holds rows 16*ks .. 16*ks+15; a 16-lane group reads rows
