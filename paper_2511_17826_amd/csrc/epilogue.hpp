@@ -60,21 +60,22 @@ __device__ __forceinline__ void values_of_their_own(float (&v)[COUNT]) {
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) asm("" : "+v"(v[i]));
 }
-template <int ROWS, int COUNT>                  // of ROWS rows
-__device__ __forceinline__ void scale_and_bias(const EpilogueParams &e, float (&v)[ROWS][COUNT], const float (&rs)[ROWS], const float (&cs)[COUNT], const float (&b)[COUNT]) {
-    if (e.row_scale) {
+// of ROWS rows; the flags say which parts there are, at run time or as constants
+template <int ROWS, int COUNT, class Flag1, class Flag2, class Flag3>
+__device__ __forceinline__ void scale_and_bias(Flag1 row_scale, Flag2 col_scale, Flag3 bias, float (&v)[ROWS][COUNT], const float (&rs)[ROWS], const float (&cs)[COUNT], const float (&b)[COUNT]) {
+    if (row_scale) {
 #pragma unroll
         for (int r = 0; r < ROWS; ++r)
 #pragma unroll
             for (int i = 0; i < COUNT; ++i) v[r][i] = v[r][i] * rs[r];
     }
-    if (e.col_scale) {
+    if (col_scale) {
 #pragma unroll
         for (int r = 0; r < ROWS; ++r)
 #pragma unroll
             for (int i = 0; i < COUNT; ++i) v[r][i] = v[r][i] * cs[i];
     }
-    if (e.bias) {
+    if (bias) {
 #pragma unroll
         for (int r = 0; r < ROWS; ++r)
 #pragma unroll
@@ -82,6 +83,10 @@ __device__ __forceinline__ void scale_and_bias(const EpilogueParams &e, float (&
     }
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) values_of_their_own(v[r]);
+}
+template <int ROWS, int COUNT>
+__device__ __forceinline__ void scale_and_bias(const EpilogueParams &e, float (&v)[ROWS][COUNT], const float (&rs)[ROWS], const float (&cs)[COUNT], const float (&b)[COUNT]) {
+    scale_and_bias(e.row_scale != nullptr, e.col_scale != nullptr, e.bias != nullptr, v, rs, cs, b);
 }
 template <int ACT, int ROWS, int COUNT>
 __device__ __forceinline__ void activate_as(float (&v)[ROWS][COUNT]) {
