@@ -1,5 +1,7 @@
 // The gated activation (activation.hip) with an 8-bit output with scales: v = SiLU(gate) * up in fp32 as silu_mul() forms it, then 8 bits
 // of v (eight_bit_rows.hpp) -- the operand of an 8-bit or microscaling down_proj.  HBM-bound: 4 bytes read and 1 written per element.
+#include <algorithm>
+
 #include "eight_bit_rows.hpp"
 
 namespace tbik {
@@ -80,9 +82,14 @@ hipError_t launch_of(const Silu8Args &a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_silu_mul_8bit(const Silu8Args &a, int dtype, hipStream_t s) {
-    if (a.M <= 0 || a.I <= 0) return hipSuccess;
-    return dtype == TBIK_F16 ? launch_of<true>(a, s) : launch_of<false>(a, s);
+hipError_t launch_silu_mul_8bit(const Silu8Args &all, int dtype, hipStream_t s) {
+    const int64_t most = all.out.micro ? all.M : kRowsOfALaunch;        // (a loop over the elements, or a workgroup per row)
+    for (int64_t m = 0; m < all.M && all.I > 0; m += most) {
+        const Silu8Args a{all.gate + m * all.ldg, all.ldg, all.up + m * all.ldu, all.ldu, all.out.from_row(m), std::min(most, all.M - m), all.I};
+        const hipError_t e = dtype == TBIK_F16 ? launch_of<true>(a, s) : launch_of<false>(a, s);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace tbik

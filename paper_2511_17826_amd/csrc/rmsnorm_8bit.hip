@@ -4,6 +4,8 @@
 //   q, scales = 8 bits of n                                            eight_bit_rows.hpp
 // HBM-bound: per element 2 bytes of x (4 P of partials), 2 + 2 of residual and h, 1 written.  A row stays in registers as 16-bit
 // values between the sum of squares and the output, so it is read once.
+#include <algorithm>
+
 #include "eight_bit_rows.hpp"
 
 namespace tbik {
@@ -35,14 +37,13 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rmsnorm_8bit_ke
             if constexpr (P == 0) {
                 h[s] = *reinterpret_cast<const uint4 *>(a.x + row * a.ldx + c * 8);
             } else {
-                const int64_t plane = (int64_t)a.M * a.H;
                 const float *src = a.partials + row * a.H + c * 8;
                 float y[8];
                 f32x4 in[2][P];
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
-                    in[0][p] = *reinterpret_cast<const f32x4 *>(src + p * plane);
-                    in[1][p] = *reinterpret_cast<const f32x4 *>(src + p * plane + 4);
+                    in[0][p] = *reinterpret_cast<const f32x4 *>(src + p * a.plane);
+                    in[1][p] = *reinterpret_cast<const f32x4 *>(src + p * a.plane + 4);
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -184,9 +185,21 @@ hipError_t launch_of(const Rms8Args &a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_rmsnorm_8bit(const Rms8Args &a, int dtype, hipStream_t s) {
-    if (a.M <= 0) return hipSuccess;
-    return dtype == TBIK_F16 ? launch_of<true>(a, s) : launch_of<false>(a, s);
+hipError_t launch_rmsnorm_8bit(const Rms8Args &all, int dtype, hipStream_t s) {
+    for (int64_t m = 0; m < all.M; m += kRowsOfALaunch) {
+        Rms8Args a = all;
+        a.M = (int)std::min<int64_t>(kRowsOfALaunch, all.M - m);
+        if (a.x) a.x += m * a.ldx;
+        if (a.partials) a.partials += m * a.H;
+        if (a.residual) {
+            a.residual += m * a.ldr;
+            a.hidden += m * a.ldh;
+        }
+        a.out = all.out.from_row(m);
+        const hipError_t e = dtype == TBIK_F16 ? launch_of<true>(a, s) : launch_of<false>(a, s);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace tbik

@@ -1164,7 +1164,7 @@ static int rmsnorm_8bit(const void *x, int64_t ldx, const void *residual, int64_
     if (residual && (!aligned(residual, 16) || !aligned(hidden, 16) || ldr % 8 != 0 || ldh % 8 != 0)) return TBIK_ERR_ALIGN;
     if (residual && ((hidden == x && ldh != ldx) || (hidden == residual && ldh != ldr))) return TBIK_ERR_SHAPE;
     const Rms8Args a{(const uint16_t *)x, ldx, nullptr, 0, (const uint16_t *)residual, ldr, (const uint16_t *)weight, (uint16_t *)hidden, ldh,
-                     out_8bit(q_dtype, q, ldq, scales, lds, micro), M, H, eps};
+                     out_8bit(q_dtype, q, ldq, scales, lds, micro), M, H, eps, (int64_t)M * H};
     hipError_t e = launch_rmsnorm_8bit(a, (int)dtype, (hipStream_t)hip_stream);
     return e == hipSuccess ? TBIK_OK : hip_fail(e);
 }
@@ -1191,7 +1191,7 @@ static int combine_residual_rmsnorm_8bit(const float *partials, int P, const voi
     if (ldr < H || ldh < H || (hidden == residual && ldh != ldr)) return TBIK_ERR_SHAPE;
     if (!aligned(partials, 16) || !aligned(residual, 16) || !aligned(weight, 16) || !aligned(hidden, 16) || ldr % 8 != 0 || ldh % 8 != 0) return TBIK_ERR_ALIGN;
     const Rms8Args a{nullptr, 0, partials, P, (const uint16_t *)residual, ldr, (const uint16_t *)weight, (uint16_t *)hidden, ldh,
-                     out_8bit(q_dtype, q, ldq, scales, lds, micro), M, H, eps};
+                     out_8bit(q_dtype, q, ldq, scales, lds, micro), M, H, eps, (int64_t)M * H};
     hipError_t e = launch_rmsnorm_8bit(a, (int)dtype, (hipStream_t)hip_stream);
     return e == hipSuccess ? TBIK_OK : hip_fail(e);
 }

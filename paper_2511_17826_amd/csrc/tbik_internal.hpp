@@ -144,7 +144,10 @@ struct EightBitOut {
     void *scales;        // fp32, one per row; micro: bytes [., lds], one per 32 columns
     int64_t lds;
     int micro, e5m2;
+    EightBitOut from_row(int64_t m) const { return {q + m * ldq, ldq, micro ? (void *)(static_cast<uint8_t *>(scales) + m * lds) : (void *)(static_cast<float *>(scales) + m), lds, micro, e5m2}; }
 };
+// Rows of one launch: a grid has fewer than 2^32 threads, and a row has up to 1024.
+constexpr int kRowsOfALaunch = 1 << 21;
 struct Rms8Args {
     const uint16_t *x;         // [M, ldx], P == 0
     int64_t ldx;
@@ -158,6 +161,7 @@ struct Rms8Args {
     EightBitOut out;
     int M, H;
     float eps;
+    int64_t plane;             // elements from one shard's sums to the next
 };
 hipError_t launch_rmsnorm_8bit(const Rms8Args &a, int dtype, hipStream_t s);
 struct Silu8Args {

@@ -227,3 +227,20 @@ def test_another_stream():
         copy = got[1].clone()
     s.synchronize()
     assert torch.equal(copy, want[1]) and torch.equal(got[2], want[2])
+
+
+@pytest.mark.parametrize("name", ["norm", "tail", "silu"])
+def test_more_rows_than_threads_of_a_grid(name):
+    """2^32 threads are a grid's limit: 17 million rows of 256 of them, 68 million of 64.  The last rows against a call of their own, and
+    the rows around every 2^21."""
+    M, H = (17 if name == "silu" else 68) * 10 ** 6 + 5, 8
+    x = torch.randint(-30000, 16000, (M, H), dtype=torch.int16, device="cuda").view(torch.bfloat16) if name != "tail" else torch.rand((2, M, H), device="cuda")
+    w = torch.full((H,), 0.75, dtype=torch.bfloat16, device="cuda")
+    calls = {"norm": lambda t: tb.tbik_rmsnorm_fp8(t, w), "tail": lambda t: tb.tbik_combine_residual_rmsnorm_fp8(t, torch.ones_like(t[0], dtype=torch.bfloat16), w),
+             "silu": lambda t: tb.tbik_silu_mul_fp8(t, t)}
+    q, scale = calls[name](x)[-2:]
+    for m in (0, 1 << 21, 5 << 21, 8 << 21, M):
+        rows = slice(max(m - 70, 0), min(m + 70, M))
+        part = x[rows] if name != "tail" else x[:, rows].contiguous()
+        q1, s1 = calls[name](part)[-2:]
+        assert torch.equal(q[rows], q1) and torch.equal(scale[rows].view(torch.int32), s1.view(torch.int32)), m
