@@ -245,6 +245,22 @@ def test_rows_of_output_and_residual_far_apart(ld):
     assert same(far, want)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp8 e4m3", "mx e4m3"])
+def test_residual_of_many_distant_rows_in_place(kind):
+    """Offsets past 32 bits from one tile to another where a tile's residual is loaded ahead of its product; columns around it untouched."""
+    M, N, K, leaf, ld = 1100, 8192, 256, 128, 2 ** 22 - 8
+    product, _, call = operands(kind, M, K, N, 5)
+    bias, res = torch.randn(N, device="cuda"), torch.randn(M, N, device="cuda").bfloat16()
+    want = composed(product(leaf, 1), torch.bfloat16, None, bias, None, res)
+    buf = torch.empty((M - 1) * ld + N + 16, dtype=torch.bfloat16, device="cuda")
+    far, around = buf.as_strided((M, N), (ld, 1)), [buf.as_strided((M, 8), (ld, 1), N)]
+    for b in around:
+        b.fill_(3)
+    far.copy_(res)
+    call(leaf, 1, bias=bias, residual=far, out=far)
+    assert same(far, want) and all(bool((b == 3).all()) for b in around)
+
+
 @pytest.mark.parametrize("P", [1, 2, 4, 8, 16, 32, 64])
 @pytest.mark.parametrize("M,N", [(3, 64), (5, 37), (1, 1), (130, 1028)])
 def test_combine_with_an_epilogue(P, M, N):
