@@ -108,3 +108,50 @@ def test_overwritten_workspaces_of_two_streams():
     torch.cuda.synchronize()
     for i in range(2):
         assert all(torch.equal(y, want[i]) for y in got[i])
+
+
+def test_outputs_are_ordinary_tensors():
+    """What the native half puts together itself behaves as a tensor that torch made."""
+    x = torch.randn(3, 64, device="cuda", dtype=torch.bfloat16)
+    w = torch.ones(64, device="cuda", dtype=torch.bfloat16)
+    for t in tb.tbik_rmsnorm_fp8(x, w, residual=x):
+        torch_s = torch.empty(t.shape, dtype=t.dtype, device="cuda")
+        assert t.device == torch_s.device and t.stride() == torch_s.stride() and t.is_contiguous() and t.storage_offset() == 0 and t.is_leaf
+        assert torch._C._dispatch_key_set(t) == torch._C._dispatch_key_set(torch_s) and t.untyped_storage().nbytes() == torch_s.untyped_storage().nbytes()
+        assert t.untyped_storage().device == torch_s.untyped_storage().device
+        want = t.cpu()
+        u = t.clone()
+        t.record_stream(torch.cuda.current_stream())
+        assert torch.equal(t.new_empty(t.shape).copy_(t), u) and torch.equal(t[1:], u[1:]) and repr(t) == repr(u)
+        t.resize_(t.numel() * 2)
+        assert t.device == u.device and torch.equal(t[:u.numel()].cpu(), want.flatten())
+        if t.is_floating_point():
+            u.requires_grad_()
+            (u * 2).sum().backward()
+    with torch.inference_mode():
+        y = tb.tbik_rmsnorm_fp8(x, w, residual=x)
+    assert all(t.is_inference() for t in y) and not tb.tbik_rmsnorm_fp8(x, w, residual=x)[0].is_inference()
+    before = torch.cuda.memory_allocated()
+    y = tb.tbik_rmsnorm_fp8(x, w, residual=x)
+    assert torch.cuda.memory_allocated() > before - 3 * 512
+    del y
+    empty = tb.tbik_rmsnorm_fp8(x[:0], w, residual=x[:0])
+    assert [tuple(t.shape) for t in empty] == [(0, 64), (0, 64), (0,)]
+
+
+def test_outputs_under_a_dispatch_mode():
+    """Torch is asked for them where a mode listens; the mode sees the allocation."""
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    class Counts(TorchDispatchMode):
+        n = 0
+
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            Counts.n += "empty" in str(func)
+            return func(*args, **(kwargs or {}))
+
+    x = torch.randn(3, 64, device="cuda", dtype=torch.bfloat16)
+    want = tb.tbik_silu_mul_fp8(x, x)
+    with Counts():
+        got = tb.tbik_silu_mul_fp8(x, x)
+    assert Counts.n >= 2 and all(torch.equal(a, b) for a, b in zip(got, want))
