@@ -465,7 +465,8 @@ void gemm_fp8_tiled_kernel(const std::conditional_t<EPI, Fp8EpilogueParams, Fp8P
                 const unsigned char *vectors = p.vector_slots ? smem + cur * STAGE8 : nullptr;
                 const unsigned char *residual = p.residual_slots ? smem + (p.vector_slots ? behind : cur) * STAGE8 + wave * REGION8 : nullptr;
                 if (wide) store_from_ring<false, true, REGION8, A_LOADS8>(acc, patch, p.epilogue, vectors, residual, p.Y, p.ldy, row0, col0, wm_u, wn_u, p.M, last, here, false);
-                else if (interior) store_from_ring<true, false, REGION8, A_LOADS8>(acc, patch, p.epilogue, vectors, residual, p.Y, p.ldy, row0, col0, wm_u, wn_u, p.M, last, here, p.epilogue.y_dtype == TBIK_F16);
+                else if (interior && p.epilogue.y_dtype == TBIK_BF16) store_from_ring<true, false, REGION8, A_LOADS8>(acc, patch, p.epilogue, vectors, residual, p.Y, p.ldy, row0, col0, wm_u, wn_u, p.M, last, here, std::false_type{});
+                else if (interior) store_from_ring<true, false, REGION8, A_LOADS8>(acc, patch, p.epilogue, vectors, residual, p.Y, p.ldy, row0, col0, wm_u, wn_u, p.M, last, here, std::true_type{});
                 else store_from_ring<false, false, REGION8, A_LOADS8>(acc, patch, p.epilogue, vectors, residual, p.Y, p.ldy, row0, col0, wm_u, wn_u, p.M, last, here, p.epilogue.y_dtype == TBIK_F16);
                 if (interior) stores = wide ? STORES_F32 : STORES_BF16;
             } else if (n0 + BN <= p.N && p.vector_stores) {

@@ -246,7 +246,8 @@ __device__ __forceinline__ void store_from_ring(const Acc<MT, NT> &acc, float *p
         }
     }
     // The block rows.  Flags that are constants give straight code; values that pass around a branch are copied there, one or two
-    // instructions each (in 8 bits, 4096 x 4096 x 8192: with no part at all 146 -> 143 us, all parts but an activation 163.5 -> 161).
+    // instructions each (in 8 bits, 4096 x 4096 x 8192: with no part at all 146 -> 143 us, all parts but an activation 163.5 -> 161; the
+    // 16-bit output's type as a constant too, 168.5 -> 165).
     auto rows = [&](auto row_scale, auto col_scale, auto bias, auto act, auto added) __attribute__((always_inline)) {
 #pragma unroll
         for (int a = 0; a < MT; ++a) {
