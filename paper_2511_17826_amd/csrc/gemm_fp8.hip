@@ -454,11 +454,15 @@ void gemm_fp8_tiled_kernel(const std::conditional_t<EPI, Fp8EpilogueParams, Fp8P
             const int prev = cur == 0 ? RING8 - 1 : cur - 1, behind = cur + 1 == RING8 ? 0 : cur + 1;
             const int extra = p.vector_slots + p.residual_slots;
             float *patch = reinterpret_cast<float *>(smem + prev * STAGE8 + wave * REGION8);
-            // The first position behind the stages has landed since the last stage's entry; for the second one, as much may be
-            // in flight as at a stage's entry.
+            // The first position behind the stages has landed since the last stage's entry; for the second one -- with one position the next
+            // tile's first stage, whose fragments are then read ahead of the epilogue -- as much may be in flight as at a stage's entry.
             constexpr int ALLOW = LOADS_PER_STAGE * (RING8 - 3);
-            if (extra == 2) wait_loads_and_barrier<ALLOW>();
-            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            if (extra) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(ALLOW) : "memory");
+            else asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            if (extra == 1) {
+                read_frags(0, behind, 0);
+                if (MX) read_scales(behind);
+            }
             const bool wide = p.epilogue.y_dtype == TBIK_F32;
             int stores = -1;
             if (p.from_ring && n0 + BN <= p.N) {
@@ -477,27 +481,26 @@ void gemm_fp8_tiled_kernel(const std::conditional_t<EPI, Fp8EpilogueParams, Fp8P
             }
             stores_in_flight = stores;
             if (extra) {
-                // On to the next tile's first stage: as many positions of the stream are issued as are consumed, into the slot of
-                // the last stage (its patch has been read) and -- behind a barrier, since all wavefronts read it -- of the vectors.
-                // That stage has landed when only what was issued behind it is in flight: RING - 2 - extra positions and the
-                // stores, and this issue behind them.
+                // On to the next tile's first stage: as many positions of the stream are issued as are consumed, the first into the slot of
+                // the last stage (its patch has been read).  With one position the rest is a stage's entry as always: its wait leaves
+                // RING8 - 3 positions and the stores in flight, the vectors' slot is free behind its barrier.
                 issue_next_stage(prev);
+                cur = behind;
+            }
+            if (extra == 2) {
+                // The second goes into the slot of the vectors, behind a barrier, since all wavefronts read it.  The next tile's first stage
+                // has landed when only what was issued behind it is in flight: RING8 - 4 positions, the stores, and the issue above.
                 if (stores == STORES_F32) {
-                    if (extra == 1) wait_loads_and_barrier<ALLOW + LOADS_PER_STAGE + STORES_F32>();
-                    else wait_loads_and_barrier<ALLOW + STORES_F32>();
+                    wait_loads_and_barrier<ALLOW + STORES_F32>();
                 } else if (stores == STORES_BF16) {
-                    if (extra == 1) wait_loads_and_barrier<ALLOW + LOADS_PER_STAGE + STORES_BF16>();
-                    else wait_loads_and_barrier<ALLOW + STORES_BF16>();
+                    wait_loads_and_barrier<ALLOW + STORES_BF16>();
                 } else {
                     wait_loads_and_barrier<0>();
                     stores_in_flight = 0;
                 }
-                if (extra == 2) {
-                    issue_next_stage(cur);
-                    if (RING8 < 5) stores_in_flight = 0;       // the second stage was issued behind the stores
-                    cur = behind;
-                }
-                cur = cur + 1 == RING8 ? 0 : cur + 1;
+                issue_next_stage(behind == 0 ? RING8 - 1 : behind - 1);
+                if (RING8 < 5) stores_in_flight = 0;             // the second stage was issued behind the stores
+                cur = behind + 1 == RING8 ? 0 : behind + 1;
                 read_frags(0, cur, 0);
                 if (MX) read_scales(cur);
             }
