@@ -480,14 +480,15 @@ void gemm_fp8_tiled_kernel(const std::conditional_t<EPI, Fp8EpilogueParams, Fp8P
                 store_elements_with_epilogue(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, p.M, p.N, here);
             }
             stores_in_flight = stores;
-            if (extra) {
+            const int behind_it = item + (int)gridDim.x < p.work ? extra : 0;      // the last tile: no more loads
+            if (behind_it) {
                 // On to the next tile's first stage: as many positions of the stream are issued as are consumed, the first into the slot of
                 // the last stage (its patch has been read).  With one position the rest is a stage's entry as always: its wait leaves
                 // RING8 - 3 positions and the stores in flight, the vectors' slot is free behind its barrier.
                 issue_next_stage(prev);
                 cur = behind;
             }
-            if (extra == 2) {
+            if (behind_it == 2) {
                 // The second goes into the slot of the vectors, behind a barrier, since all wavefronts read it.  The next tile's first stage
                 // has landed when only what was issued behind it is in flight: RING8 - 4 positions, the stores, and the issue above.
                 if (stores == STORES_F32) {
