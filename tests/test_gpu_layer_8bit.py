@@ -142,3 +142,54 @@ def test_two_layers_on_two_streams():
                 g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(o, w) for o, w in zip(outs, wants))
+
+
+@pytest.mark.parametrize("M", [1, 150, 1000])
+def test_shards_and_16_bit_products_in_a_hip_graph(M):
+    """The other entry points, into buffers of the caller's, with one workspace that two captured graphs share (replayed one after the
+    other): products with an epilogue that split K and that do not, a residual updated in place, shards' sums to 8 bits."""
+    K, N, P, leaf = 4096, 1024, 4, 256
+    X, W = rnd(60, M, K).bfloat16(), (0.02 * rnd(61, K, N)).bfloat16()
+    bias, w = rnd(62, N), (1 + 0.1 * rnd(63, N)).bfloat16()
+    need = max(tb.gemm_16bit_workspace_bytes(M, N, K, leaf, 1), 256)
+    workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
+
+    def buffers():
+        e = lambda *s, t=torch.uint8: torch.empty(s, dtype=t, device="cuda")
+        return dict(stream=e(M, N, t=torch.bfloat16), parts=e(P, M, N, t=torch.float32), hidden=e(M, N, t=torch.bfloat16), combined=e(M, N, t=torch.float16),
+                    q=e(M, N), s=e(M, t=torch.float32), q2=e(M, N), s2=e(M, N // 32), hidden2=e(M, N, t=torch.bfloat16))
+
+    def one_pass(b, r):
+        b["stream"].copy_(r)
+        tb.tbik_gemm_epilogue(X, W, leaf, 1, bias=bias, activation="gelu_tanh", residual=b["stream"], out=b["stream"], workspace=workspace)
+        tb.tbik_gemm_shard_partials(X, W, leaf, 1, P, out=b["parts"], workspace=workspace)
+        tb.tbik_tree_combine_epilogue(b["parts"], bias=bias, activation="silu", out=b["combined"])
+        tb.tbik_combine_residual_rmsnorm_fp8(b["parts"], b["stream"], w, EPS, hidden=b["hidden"], out=b["q"], scale=b["s"])
+        tb.tbik_combine_residual_rmsnorm_mxfp8(b["parts"], b["stream"], w, EPS, fmt="e5m2", hidden=b["hidden2"], out=b["q2"], scale=b["s2"])
+
+    r = [rnd(64 + i, M, N).bfloat16() for i in range(2)]
+    eager, captured = buffers(), [buffers(), buffers()]
+    one_pass(eager, r[0])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graphs = []
+    with torch.cuda.stream(side):
+        for b, x in zip(captured, r):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                one_pass(b, x)
+            graphs.append(g)
+    for rep in range(3):
+        X.copy_(rnd(80 + rep, M, K).bfloat16())
+        for i in range(2):
+            for t in captured[i].values():
+                t.zero_()
+        workspace.fill_(0xFF)
+        torch.cuda.synchronize()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for b, x in zip(captured, r):
+            one_pass(eager, x)
+            torch.cuda.synchronize()
+            assert all(torch.equal(b[k].view(torch.uint8), eager[k].view(torch.uint8)) for k in b), rep
