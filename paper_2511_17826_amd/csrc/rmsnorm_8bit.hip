@@ -39,18 +39,27 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rmsnorm_8bit_ke
             } else {
                 const float *src = a.partials + row * a.H + c * 8;
                 float y[8];
-                f32x4 in[2][P];
+                // Eight columns of 16 planes are 128 registers, all that a thread of 1024 has: eight planes at a time there, half of the tree
+                // each (256 x 32768 with all 16, three registers spilled, 134 -> 114 us; 16 x 65536, 47 spilled, 82 -> 56; with four
+                // columns of all 16 at a time, half a cache line per load, 155 and 72).
+                constexpr int AT_ONCE = P > 8 && WAVES == 16 && CPL > 2 ? 8 : P;
 #pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    in[0][p] = *reinterpret_cast<const f32x4 *>(src + p * a.plane);
-                    in[1][p] = *reinterpret_cast<const f32x4 *>(src + p * a.plane + 4);
-                }
+                for (int first = 0; first < P; first += AT_ONCE) {
+                    f32x4 in[2][AT_ONCE];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float v[P];
+                    for (int p = 0; p < AT_ONCE; ++p) {
+                        in[0][p] = *reinterpret_cast<const f32x4 *>(src + (first + p) * a.plane);
+                        in[1][p] = *reinterpret_cast<const f32x4 *>(src + (first + p) * a.plane + 4);
+                    }
 #pragma unroll
-                    for (int p = 0; p < P; ++p) v[p] = in[e >> 2][p][e & 3];
-                    y[e] = tree_of<P>(v);
+                    for (int e = 0; e < 8; ++e) {
+                        float v[AT_ONCE];
+#pragma unroll
+                        for (int p = 0; p < AT_ONCE; ++p) v[p] = in[e >> 2][p][e & 3];
+                        const float t = tree_of<AT_ONCE>(v);
+                        y[e] = first == 0 ? t : y[e] + t;
+                    }
+                    if (AT_ONCE < P) __builtin_amdgcn_sched_barrier(0);
                 }
                 h[s] = make_uint4(pack_16x2<F16>(y[0], y[1]), pack_16x2<F16>(y[2], y[3]), pack_16x2<F16>(y[4], y[5]), pack_16x2<F16>(y[6], y[7]));
             }
