@@ -168,9 +168,14 @@ hipError_t launch_p(const Rms8Args &a, hipStream_t s) {
     //   8192 x 4096       8x1 43.2  4x2 40.0  1x8 49.0         8191 x 5120    8x2 54.3  4x3 50.6  1x10 67.0      4096 x 1024  4x1 8.9  1x2 7.7
     //   1003 x 4096, P 4  8x1 14.1  4x2 14.7  1x8 17.7         1024 x 16384   16x2 20.9 8x4 22.9                 2048 x 512   4x1 3.8  1x2 3.2
     // (8191 x 5120: 5.8 TB/s of the bytes that have to move, a copy of 1 GiB reaches 5.1.)
+    if constexpr (P == 0) {
+        if (a.M >= 1024 && segments > 2 && segments <= 12) {
+            if (segments <= 8) rows_of(rmsnorm_8bit_kernel<F16, P, 4, 2>, 4);
+            else rows_of(rmsnorm_8bit_kernel<F16, P, 4, 3>, 4);
+            return hipGetLastError();
+        }
+    }
     if (segments <= 2) rows_of_a_wavefront(rmsnorm_8bit_kernel<F16, P, 1, 2>);
-    else if (P == 0 && a.M >= 1024 && segments <= 8) rows_of(rmsnorm_8bit_kernel<F16, P, 4, 2>, 4);
-    else if (P == 0 && a.M >= 1024 && segments <= 12) rows_of(rmsnorm_8bit_kernel<F16, P, 4, 3>, 4);
     else if (segments <= 8) rows_of(rmsnorm_8bit_kernel<F16, P, 8, 1>, 8);
     else if (segments <= 16) rows_of(rmsnorm_8bit_kernel<F16, P, 8, 2>, 8);
     else if (segments <= 32) rows_of(rmsnorm_8bit_kernel<F16, P, 16, 2>, 16);
