@@ -34,3 +34,16 @@ def test_wide_rows_of_partial_sums(P, M, H, dtype, micro):
     v = ref.normed32(hidden.float().cpu().numpy(), w.float().cpu().numpy(), EPS)
     want_q, want_s = (ref.micro_scaled if micro else ref.row_scaled)(v, fmt)
     assert (scale.cpu().numpy() == want_s).all() and ref.same_patterns(q.cpu().numpy(), want_q, fmt)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H", [2048, 4096, 5120, 6144])
+def test_rows_around_the_switch_of_forms(H):
+    """512 rows take another form of the kernel than 513: a row's bits are the same in both."""
+    g = torch.Generator(device="cuda").manual_seed(H)
+    x, r = (torch.randn((1100, H), generator=g, device="cuda").bfloat16() for _ in range(2))
+    w = torch.randn(H, generator=g, device="cuda").bfloat16()
+    for f in (tb.tbik_rmsnorm_fp8, tb.tbik_rmsnorm_mxfp8):
+        whole = f(x, w, EPS, residual=r)
+        for M in (511, 512, 513, 1024):
+            assert all(torch.equal(a, b[:M]) for a, b in zip(f(x[:M], w, EPS, residual=r[:M]), whole)), M
