@@ -95,13 +95,12 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_slice_kernel(const std::condi
     const int li = lane & 31, lg = lane >> 5;
     const int n0 = blockIdx.x * 16;
     float *const red = reinterpret_cast<float *>(smem);
-    // The thread's output element, and its epilogue's operands: on their way before the weights (16 rows, K = 12288, E4M3 with scales
+    // The epilogue's operands of the thread's output element: on their way before the weights (16 rows, K = 12288, E4M3 with scales
     // and a residual 10.5 us, with loads at the end 10.8; without an epilogue 10.0).
-    const int row = threadIdx.x >> 4, col = n0 + (threadIdx.x & 15);
-    const bool owns = threadIdx.x < 512 && row < p.M && col < p.N;
     std::conditional_t<EPI, ElementOperands, int> operands{};
     if constexpr (EPI) {
-        if (owns) operands = element_operands(p.epilogue, row, col);
+        const int row = threadIdx.x >> 4, col = n0 + (threadIdx.x & 15);
+        if (threadIdx.x < 512 && row < p.M && col < p.N) operands = element_operands(p.epilogue, row, col);
     }
 
     f32x16 acc;
@@ -265,7 +264,8 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_slice_kernel(const std::condi
         for (int r = 0; r < 16; ++r) red[wave * 512 + (8 * (r >> 2) + 4 * lg + (r & 3)) * 16 + li] = acc[r];
     }
     __syncthreads();
-    if (!owns) return;
+    const int row = threadIdx.x >> 4, col = n0 + (threadIdx.x & 15);
+    if (threadIdx.x >= 512 || row >= p.M || col >= p.N) return;
     const float v = slice_tree<WAVES>(red + threadIdx.x, p.active_waves);
     if constexpr (EPI) finish_and_store(p.epilogue, v, operands, p.Y, p.ldy, row, col);
     else if (p.y_bf16) reinterpret_cast<uint16_t *>(p.Y)[(int64_t)row * p.ldy + col] = (uint16_t)f32_to_bf16_bits(v);
