@@ -568,7 +568,7 @@ int tbik_tree_combine_epilogue(const float *partials, int P, const tbik_epilogue
  *   weight    device, `dtype`, [H], 16-byte aligned          partials   device, fp32, dense [P, M, H], 16-byte aligned, P a power of two <= 16
  *   q         device, [M, ldq] bytes, 8-byte aligned, ldq a multiple of 8 (the products ask for 16); no overlap with an input
  *   scales    device: row_scale fp32 [M]; _mxfp8: [M, lds] bytes, lds >= H / 32
- *   H, I      up to 65536; a multiple of 8 (_fp8) or 32 (_mxfp8)
+ *   H, I      up to 65536; a multiple of 8 (_fp8) or 32 (_mxfp8).  With I = 0 nothing is written, row_scale neither
  * Errors: NULL, SHAPE, DTYPE, ALIGN, HIP; combine_residual: SHARDS, UNSUPPORTED.
  */
 int tbik_rmsnorm_fp8(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, float eps, void *hidden, int64_t ldh,

@@ -1003,6 +1003,8 @@ def _silu_mul_8bit(name, micro, gate, up, fmt, out, scale):
     _on_current_device(gate, up, out, scale)
     types = ((scale.stride(0),) if micro else ()) + (_dt(gate), _FP8[fmt], M, I, _stream())
     _check(getattr(lib(), name)(gate.data_ptr(), ldg, up.data_ptr(), ldu, out.data_ptr(), out.stride(0), scale.data_ptr(), *types), name)
+    if I == 0:
+        scale.fill_(1)                                # that of zeros; the library writes nothing for rows without columns
     return out, scale
 
 

@@ -333,6 +333,7 @@ PyObject *eight_bits(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const at::Tensor *x = plain(a[1], tail ? 3 : 2), *second = nullptr, *weight = nullptr;
         if (!x || x->size(-2) > INT_MAX || x->size(-1) > INT_MAX) UNCOMMON;
         const int M = (int)x->size(-2), H = (int)x->size(-1);
+        if (H == 0) UNCOMMON;
         at::ScalarType dtype = x->scalar_type();
         if (tail) {
             if (dtype != at::kFloat || !x->is_contiguous() || x->size(0) > INT_MAX || a[2] == Py_None) UNCOMMON;
