@@ -507,7 +507,8 @@ int tbik_combine_residual_rmsnorm_f16(const float *partials, int P, const void *
  *   GELU       v Phi(v), Phi the normal distribution function          GELU_TANH  v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) / 2
  * with the hardware's exponential and reciprocal (about one fp32 ulp each).  Each is off by at most its factor times 2^-24 |act(v)|,
  * plus 2^-100: SILU 6 + 2 |v|, GELU 15 + 1.5 v^2, GELU_TANH 6 + 12 |sqrt(2/pi) (v + 0.044715 v^3)| (the terms in v are the rounding
- * of an exponent, so they matter in the negative tails only).
+ * of an exponent, so they matter in the negative tails only).  NaN stays NaN and +infinity +infinity; -infinity becomes 0 in RELU and NaN
+ * in the others, as their formulas have it (infinity times 0).
  * Determinism contract: the bits of row m depend on row m of X and residual, row_scale[m], and the weights, scales and biases of
  * the columns only, and
  *   tbik_gemm_*_epilogue(...) == tbik_tree_combine_epilogue(tbik_gemm_shard_partials_*(..., P), P, ...)      bit for bit, every legal P;
