@@ -15,8 +15,9 @@ __device__ __forceinline__ float silu_of(float v) { return v * __builtin_amdgcn_
 
 // v Phi(v), Phi the normal distribution function.  Its tail, Phi(-a) = erfc(a / sqrt 2) / 2, decides both sides (v < 0: the tail
 // itself; else one minus it), so it is formed without a cancellation: erfc(z) = e^(-z^2) erfcx(z), and erfcx(z) = t q(t) with
-// t = 1 / (1 + 0.375 z), q the polynomial of degree 8 whose largest relative error over z in [0, 10.2] is smallest (1.3e-8, fitted
-// for this kernel; 3.3e-7 evaluated in fp32); beyond, e^(-z^2) is zero in fp32.  The coefficients hold the half.
+// t = 1 / (1 + 0.375 z), q the polynomial of degree 8 whose largest relative error over z in [0, 10.2] is smallest, fitted for this
+// kernel (3.2e-8 with its coefficients in fp32; t q(t) formed from v in fp32, with a correctly rounded reciprocal, 3.6e-7); beyond,
+// e^(-z^2) is zero in fp32.  The coefficients hold the half.
 __device__ __forceinline__ float gelu_of(float v) {
     const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(v), 0.26516504294495535f, 1.0f));      // 0.375 / sqrt 2
     float q = 0.03065868280827999f;

@@ -74,7 +74,7 @@ __device__ __forceinline__ void store_with_epilogue(const Acc<MT, NT> &acc, floa
         if (last < 32 * a) continue;
         fill_patch(acc, a, patch, lane);
         if (activated) {
-            // A loop, and back into the patch: unrolled with the stores, the five activations are 30 KiB of code per kernel.
+            // A loop, and back into the patch: unrolled with the stores, the four activations are 30 KiB of code per kernel.
 #pragma nounroll
             for (int it = 0; it < N_IT; ++it) {
                 const int row = it * RPI + lrow;
