@@ -96,12 +96,18 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_slice_kernel(const std::condi
     const int n0 = blockIdx.x * 16;
     float *const red = reinterpret_cast<float *>(smem);
     // The epilogue's operands of the thread's output element: on their way before the weights (16 rows, K = 12288, E4M3 with scales
-    // and a residual 10.5 us, with loads at the end 10.8; without an epilogue 10.0).
+    // and a residual 10.5 us, with loads at the end 10.8; without an epilogue 10.0).  Where two workgroups are to share a compute unit
+    // they come behind the weights, since two registers of 128 are left and with operands held over the loop one workgroup runs at a time
+    // (1 x 4096 x 12288 11.8 -> 10.4 us, 16 rows 12.2 -> 10.8; without an epilogue 9.8 and 10.1).
+    constexpr bool EARLY = MX || RING != 2;
     std::conditional_t<EPI, ElementOperands, int> operands{};
-    if constexpr (EPI) {
-        const int row = threadIdx.x >> 4, col = n0 + (threadIdx.x & 15);
-        if (threadIdx.x < 512 && row < p.M && col < p.N) operands = element_operands(p.epilogue, row, col);
-    }
+    auto load_operands = [&]() __attribute__((always_inline)) {
+        if constexpr (EPI) {
+            const int row = threadIdx.x >> 4, col = n0 + (threadIdx.x & 15);
+            if (threadIdx.x < 512 && row < p.M && col < p.N) operands = element_operands(p.epilogue, row, col);
+        }
+    };
+    if constexpr (EARLY) load_operands();
 
     f32x16 acc;
     if (wave < p.active_waves) {
@@ -258,6 +264,7 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_slice_kernel(const std::condi
         for (int s = RING; s < steps; ++s) consume(Int<RING - 1>{}, std::true_type{});
         slice_tail<RING - 1>(steps, consume);
     }
+    if constexpr (!EARLY) load_operands();
     __syncthreads();                                                   // the rings have been read: the sums take their place
     if (wave < p.active_waves && li < 16) {
 #pragma unroll
