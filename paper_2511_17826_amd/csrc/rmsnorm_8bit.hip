@@ -167,7 +167,7 @@ hipError_t launch_p(const Rms8Args &a, hipStream_t s) {
     //   1 x 4096          8x1 2.7   4x2 3.2   1x8 6.5          512 x 4096     8x1 4.5   4x2 4.7   1x8 9.3
     //   8192 x 4096       8x1 43.2  4x2 40.0  1x8 49.0         8191 x 5120    8x2 54.3  4x3 50.6  1x10 67.0      4096 x 1024  4x1 8.9  1x2 7.7
     //   1003 x 4096, P 4  8x1 14.1  4x2 14.7  1x8 17.7         1024 x 16384   16x2 20.9 8x4 22.9                 2048 x 512   4x1 3.8  1x2 3.2
-    // Where four begin to pay, two rows per compute unit, on operands that come from HBM:
+    // Where four begin to pay is near two rows per compute unit (six sets of operands in turn):
     //   rows of 4096      256  8x1 3.7   4x2 4.1     512  5.7  5.6     640  6.9  6.5     896   8.2  7.6     2048  13.2  12.6
     //   rows of 5120      256  8x2 4.7   4x3 5.4     512  6.5  6.5     640  7.8  7.4     896   9.3  8.7     2048  16.9  15.8
     // (8191 x 5120: 5.8 TB/s of the bytes that have to move, a copy of 1 GiB reaches 5.1.)
