@@ -587,6 +587,109 @@ int tbik_silu_mul_fp8(const void *gate, int64_t ldg, const void *up, int64_t ldu
 int tbik_silu_mul_mxfp8(const void *gate, int64_t ldg, const void *up, int64_t ldu, void *q, int64_t ldq, void *scales, int64_t lds,
                         tbik_dtype dtype, tbik_dtype q_dtype, int M, int I, void *hip_stream);
 
+/*
+ * ---- An MLP that is a mixture of experts: router, products grouped by expert, weighted sum. ----
+ *
+ * tbik_route_topk: each token's k experts and their weights, and the order in which the grouped products take the tokens.
+ *   experts[t][0..k)   the experts of the k largest logits, falling; among equal ones (+0 and -0 are) the lower index first; NaN is
+ *                      below everything else
+ *   weights[t][j]      e^(l_j - l_0) / sum, the sum over the chosen in order (renormalize), or over all E; 0 where l_0 is -infinity
+ *                      (a token all of whose experts are masked out); NaN and +infinity spread as the formula has it
+ *   offsets[0..E]      offsets[e] = number of choices of experts below e; offsets[E] = T k (T == 0: zeros are written)
+ *   slots[t][j]        the choice's row in the order of the experts: offsets[e] + number of tokens before t that chose e
+ *   rows[slots[t][j]]  = t
+ * A token's choices, their weights' bits, and the order do not depend on the launch; a token's choices and weights depend on its own logits only.
+ *
+ *   logits   device, dtype (TBIK_F32, TBIK_BF16 or TBIK_F16), [T, ldl], ldl >= E, aligned to their type
+ *   experts, slots  device, int32, dense [T, k]     weights  device, fp32, dense [T, k]     offsets  device, int32 [E + 1]     rows  device, int32 [T k]
+ *   1 <= k <= E; E <= 512, k <= 32, T <= 2^26 (else TBIK_ERR_UNSUPPORTED); T k < 2^31
+ *   workspace  tbik_route_topk_workspace_bytes(T, E) bytes, 256-byte aligned (0 up to 64 tokens)
+ * Errors: NULL, SHAPE, DTYPE, UNSUPPORTED, ALIGN, WORKSPACE, HIP.
+ */
+size_t tbik_route_topk_workspace_bytes(int T, int E);
+int tbik_route_topk(const void *logits, int64_t ldl, tbik_dtype dtype, int T, int E, int k, int renormalize, int32_t *experts, float *weights,
+                    int32_t *offsets, int32_t *rows, int32_t *slots, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Matrix products grouped by expert: Y[i] = X[rows[i]] W_e for the rows offsets[e] <= i < offsets[e + 1] of group e (without `rows`: X[i] W_e).
+ * The sum of a row is that of tbik_gemm, bit for bit: the bits of Y[i] are those of tbik_gemm on that row of X and that weight, whatever other rows
+ * and groups there are, and of the sums of P shards tbik_tree_combine makes the same.
+ *   _swiglu          act[i] = tbik_gemm_swiglu of that row and W_e = [gate | up] [K, 2 I], bit for bit
+ *   _shard_partials  partials[p][i] = tbik_gemm_shard_partials of that row and weight
+ * Rows before offsets[0] and from offsets[groups] on are left as they were, in shards' sums too.
+ *
+ *   X        device, x_dtype (TBIK_BF16 or TBIK_F16), [tokens, ldx]
+ *   rows     device, int32 [R], or NULL (then tokens >= R); an index outside 0 .. tokens - 1 is taken as the nearest one
+ *   W        device, x_dtype, `groups` matrices [K, ldw], weight_stride elements apart (a multiple of 8; 0: the same for all); groups <= 512
+ *   offsets  device, int32 [groups + 1]; not falling and within 0 .. R; values that are not are taken as the largest before them, within 0 .. R
+ *   Y        device, y_dtype (TBIK_F32 or x_dtype), [R, ldy]; act likewise, of `dtype`; partials device, fp32, dense [P, R, N]
+ *   Everything else as for tbik_gemm, tbik_gemm_swiglu and tbik_gemm_shard_partials; no workspace.  tokens == 0 or groups == 0: nothing is written.
+ * Errors: NULL, SHAPE, SHARDS, DTYPE, UNSUPPORTED, ALIGN, HIP.
+ */
+int tbik_gemm_grouped(const void *X, int64_t ldx, int tokens, const int32_t *rows, const void *W, int64_t ldw, int64_t weight_stride, int groups,
+                      const int32_t *offsets, void *Y, int64_t ldy, tbik_dtype y_dtype, tbik_dtype x_dtype, int R, int N, int K, int leaf, int k_first,
+                      void *hip_stream);
+int tbik_gemm_grouped_swiglu(const void *X, int64_t ldx, int tokens, const int32_t *rows, const void *W_gu, int64_t ldw, int64_t weight_stride, int groups,
+                             const int32_t *offsets, void *act, int64_t lda, tbik_dtype dtype, int R, int I, int K, int leaf, int k_first, void *hip_stream);
+int tbik_gemm_grouped_shard_partials(const void *X, int64_t ldx, int tokens, const int32_t *rows, const void *W, int64_t ldw, int64_t weight_stride, int groups,
+                                     const int32_t *offsets, float *partials, tbik_dtype x_dtype, int R, int N, int K, int leaf, int k_first, int P,
+                                     void *hip_stream);
+
+/*
+ * The weighted sum of a token's experts: out[t] = round( sum_j weights[t][j] Y[slots[t][j]] (+ residual[t]) ), per element one chain of fp32 fused
+ * multiply-adds from +0 over j ascending, then one addition, then the one rounding.  With fp32 Y of P shards, Y = T(partials) first (P = 1: itself), so the result of P
+ * shards is bit for bit that of the fp32 product.  A choice whose slot is outside 0 .. R - 1 (a dropped one: -1) adds nothing.
+ *
+ *   Y        device, y_dtype: TBIK_BF16 or TBIK_F16, [R, ldy], P == 1; or TBIK_F32, dense [P, R, H] (ldy is not read), P a power of two <= 16
+ *   slots    device, int32, dense [T, k]        weights   device, fp32, dense [T, k]        k <= 32
+ *   residual device, out_dtype, [T, ldr], or NULL; may be out itself (ldr == ldo), and must not overlap it otherwise
+ *   out      device, out_dtype (TBIK_F32, or Y's 16-bit type; any 16-bit type of fp32 Y), [T, ldo]
+ *   16-byte aligned pointers and rows with H a multiple of 8 take the vector path; anything aligned to its type works.
+ * Errors: NULL, SHAPE, SHARDS, DTYPE, UNSUPPORTED, ALIGN, HIP.
+ */
+int tbik_combine_experts(const void *Y, int64_t ldy, tbik_dtype y_dtype, int P, int R, const int32_t *slots, const float *weights,
+                         const void *residual, int64_t ldr, void *out, int64_t ldo, tbik_dtype out_dtype, int T, int H, int k, void *hip_stream);
+
+/*
+ * 16-bit rows times a weight of 4-bit whole numbers with a scale per group of consecutive k and output channel:
+ *   W[k][n] = scales[n][k / group] (q[n][k] - zeros[n][k / group])         zeros NULL: 8 everywhere
+ * Per output element and superleaf: for the groups in ascending k, acc = fma(scale, S, acc) in fp32 from +0, S the group's products x (q - zero) accumulated
+ * in fp32 from +0 (q - zero is exact in 16 bits, so the weight is never rounded); the superleaf sums are combined by T, the result is rounded once.  (The 16
+ * products of one matrix instruction are added in that instruction's own fixed order, as for the other formats; of each 64 consecutive k -- 32, where 64
+ * does not divide the group -- instruction i takes 8 i .. 8 i + 7 of either half.)  The determinism contract is that of tbik_gemm, P included.
+ *
+ *   X       device, x_dtype (TBIK_BF16 or TBIK_F16), [M, ldx], 16-byte aligned, ldx a multiple of 8
+ *   Wq      device, [N, ldwq] bytes, ldwq >= K / 2 a multiple of 16, 16-byte aligned: two elements a byte, the one with the even k in the low four bits
+ *   scales  device, x_dtype, [N, lds], lds >= K / group          zeros   device, bytes (the low four bits count), [N, ldz], or NULL
+ *   group   a multiple of 32 that divides leaf * k_first; K / (leaf * k_first) / P <= 128
+ *   Y       device, y_dtype (TBIK_F32 or x_dtype), [M, ldy], aligned to its type          partials   device, fp32, dense [P, M, N], 16-byte aligned
+ *   No workspace.
+ * Errors: NULL, SHAPE, SHARDS, DTYPE, UNSUPPORTED, ALIGN, HIP.
+ */
+int tbik_gemm_w4(const void *X, int64_t ldx, const void *Wq, int64_t ldwq, const void *scales, int64_t lds, const void *zeros, int64_t ldz, int group,
+                 void *Y, int64_t ldy, tbik_dtype y_dtype, tbik_dtype x_dtype, int M, int N, int K, int leaf, int k_first, void *hip_stream);
+int tbik_gemm_shard_partials_w4(const void *X, int64_t ldx, const void *Wq, int64_t ldwq, const void *scales, int64_t lds, const void *zeros, int64_t ldz,
+                                int group, float *partials, tbik_dtype x_dtype, int M, int N, int K, int leaf, int k_first, int P, void *hip_stream);
+
+/*
+ * What joins one block to the next where a norm follows the block as well: in one pass,
+ *   n = RMSNorm(y; post_weight) as tbik_rmsnorm forms it before its rounding (post_weight NULL: y itself)
+ *   hidden = r16( residual * residual_scale + gate * n )        products and sum one fp32 operation each; gate NULL: n itself
+ *   normed = RMSNorm(hidden; next_weight)                       exactly tbik_rmsnorm (next_weight and normed NULL: not formed)
+ * y is 16-bit, or r16(T(partials)) of P shards' partial sums, exactly tbik_tree_combine's.  The bits of a row depend on that row and the weights only.
+ *
+ *   y         device, dtype (TBIK_BF16 or TBIK_F16), [M, ldy]; or NULL with partials device, fp32, dense [P, M, H], P a power of two <= 16
+ *   residual  device, dtype, [M, ldr]        post_weight, next_weight   device, dtype, [H]
+ *   gate      device, dtype: element (m, i) at m * gate_row_stride + i * gate_column_stride; column stride 0 (a gate per row; any row stride) or 1 (row stride
+ *             0: a gate per channel, else a multiple of 8: per element; 16-byte aligned)
+ *   hidden, normed   device, dtype, [M, ldh], [M, ldn]; hidden may be y or residual itself (same ld); no other overlap
+ *   H a multiple of 8, H <= 65536; pointers 16-byte aligned, leading dimensions multiples of 8
+ * Errors: NULL, SHAPE, SHARDS, DTYPE, UNSUPPORTED, ALIGN, HIP.
+ */
+int tbik_rmsnorm_residual_rmsnorm(const void *y, int64_t ldy, const float *partials, int P, const void *residual, int64_t ldr, float residual_scale,
+                                  const void *post_weight, const void *gate, int64_t gate_row_stride, int gate_column_stride, const void *next_weight, float eps,
+                                  void *hidden, int64_t ldh, void *normed, int64_t ldn, tbik_dtype dtype, int M, int H, void *hip_stream);
+
 /* Forces an internal GEMM variant (testing and tuning only; the bits never depend on it).
  * 0 = choose from the shape (default); other values are listed in tbik_variant_name(). */
 int tbik_set_gemm_variant(int variant);

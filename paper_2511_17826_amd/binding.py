@@ -40,6 +40,9 @@ _TAIL8 = [C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_void_p, C.c_float, C.c
 _SILU8 = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
 _TYPES8 = [C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p]         # dtype, q_dtype, rows, columns, stream
 
+_GROUPED = [C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int, C.c_void_p]      # X .. offsets
+_W4 = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int]          # X .. group
+
 # name -> (restype, argtypes); mirrors include/tbik.h
 SIGNATURES = {
     "tbik_gemm_epilogue": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.POINTER(Epilogue), C.c_void_p, C.c_int64, C.c_int, C.c_int,
@@ -142,6 +145,18 @@ SIGNATURES = {
                                  C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_int64,
                                  C.c_float, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
     "tbik_attention_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int, C.c_int, C.c_int]),
+    "tbik_route_topk_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int]),
+    "tbik_route_topk": (C.c_int, [C.c_void_p, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                  C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "tbik_gemm_grouped": (C.c_int, _GROUPED + [C.c_void_p, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p]),
+    "tbik_gemm_grouped_swiglu": (C.c_int, _GROUPED + [C.c_void_p, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p]),
+    "tbik_gemm_grouped_shard_partials": (C.c_int, _GROUPED + [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p]),
+    "tbik_combine_experts": (C.c_int, [C.c_void_p, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                       C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p]),
+    "tbik_gemm_w4": (C.c_int, _W4 + [C.c_void_p, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p]),
+    "tbik_gemm_shard_partials_w4": (C.c_int, _W4 + [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p]),
+    "tbik_rmsnorm_residual_rmsnorm": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_void_p, C.c_int64, C.c_int,
+                                                C.c_void_p, C.c_float, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_void_p]),
     "tbik_set_gemm_variant": (C.c_int, [C.c_int]),
     "tbik_gemm_route": (C.c_int, [C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_int)]),
     "tbik_set_attention_variant": (C.c_int, [C.c_int]),
@@ -1213,6 +1228,238 @@ def _gemm_reference(entry: str, in_dtype, X, W, leaf, k_first, P, out_dtype):
                                _dt(Y) if Y is not None else TBIK_F32, M, N, K, leaf, k_first, P, _stream())
     _check(st, entry)
     return parts, Y
+
+
+# ---- an MLP that is a mixture of experts, 4-bit weights, norms around a block ----
+
+_SIXTEEN_BITS = (torch.bfloat16, torch.float16)
+
+
+def _scratch(nbytes: int, device):
+    """The cached workspace of this stream; under capture a tensor of the graph's own, which no other call's workspace replaces and no
+    other graph shares.  None for no bytes."""
+    if nbytes == 0:
+        return None
+    if torch.cuda.is_current_stream_capturing():
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return _workspace(nbytes, device)
+
+
+def _int32(t: torch.Tensor, name: str, shape):
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError("%s must be a contiguous int32 GPU tensor of shape %s" % (name, tuple(shape)))
+
+
+def tbik_route_topk(logits: torch.Tensor, k: int, renormalize: bool = True, workspace: torch.Tensor | None = None):
+    """(experts int32 [T, k], weights float32 [T, k], offsets int32 [E + 1], rows int32 [T k], slots int32 [T, k]) of router logits [T, E]
+    (float32, bfloat16 or float16): each token's k largest, falling, the lower expert first among equals; their softmax, over the chosen
+    ones or (renormalize=False) over all; and the order by expert that tbik_gemm_grouped takes (offsets, rows) and
+    tbik_combine_experts undoes (slots)."""
+    ldl = _rowmajor(logits, "logits")
+    T, E = logits.shape
+    L = lib()
+    if workspace is None:
+        workspace = _scratch(int(L.tbik_route_topk_workspace_bytes(T, E)), logits.device)
+    shape = (T, k) if k > 0 else (T, 0)                          # the library refuses k < 1
+    new = lambda *n: torch.empty(n, dtype=torch.int32, device=logits.device)
+    experts, weights, offsets, rows, slots = new(*shape), torch.empty(shape, dtype=torch.float32, device=logits.device), new(E + 1), new(shape[0] * shape[1]), new(*shape)
+    _on_current_device(logits, workspace)
+    room, room_bytes = _room(workspace)
+    _check(L.tbik_route_topk(logits.data_ptr(), ldl, _dt(logits), T, E, k, int(bool(renormalize)), experts.data_ptr(), weights.data_ptr(),
+                             offsets.data_ptr(), rows.data_ptr(), slots.data_ptr(), room, room_bytes, _stream()), "tbik_route_topk")
+    return experts, weights, offsets, rows, slots
+
+
+def _grouped_operands(X, W, offsets, rows):
+    """(arguments up to the offsets, rows of the output, columns of a weight, K)"""
+    ldx = _rowmajor(X, "X")
+    if W.dim() != 3 or W.stride(2) != 1 or not W.is_cuda:
+        raise ValueError("W must be a 3-D GPU tensor [groups, K, N] with contiguous rows")
+    if X.dtype not in _SIXTEEN_BITS or W.dtype != X.dtype:
+        raise TypeError("X and W are both bfloat16 or both float16, got %s and %s" % (X.dtype, W.dtype))
+    tokens, K = X.shape
+    groups, K2, N = W.shape
+    if K != K2:
+        raise ValueError("X has %d columns, the weights %d rows" % (K, K2))
+    _int32(offsets, "offsets", (groups + 1,))
+    R = tokens
+    if rows is not None:
+        R = rows.numel()
+        _int32(rows, "rows", (R,))
+    return (X.data_ptr(), ldx, tokens, rows.data_ptr() if rows is not None else None, W.data_ptr(), W.stride(1), W.stride(0), groups, offsets.data_ptr()), R, N, K
+
+
+def tbik_gemm_grouped(X: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, leaf: int, k_first: int = 1, rows: torch.Tensor | None = None,
+                      out_dtype=None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Y[i] = X[rows[i]] @ W[e] for offsets[e] <= i < offsets[e + 1], in the tree order: the bits of tbik_gemm on that row and weight.  W
+    [groups, K, N]; offsets int32 [groups + 1] and rows int32 [R] on the GPU (tbik_route_topk's); without rows Y[i] = X[i] @ W[e].  Y is
+    float32 or (default) X's type; its rows outside every group are left as they were (undefined in a new tensor)."""
+    operands, R, N, K = _grouped_operands(X, W, offsets, rows)
+    if out is None:
+        out = torch.empty((R, N), dtype=out_dtype or X.dtype, device=X.device)
+    ldy = _rowmajor(out, "out")
+    if out.shape != (R, N):
+        raise ValueError("out must have the shape %s" % ((R, N),))
+    _on_current_device(X, W, offsets, rows, out)
+    _check(lib().tbik_gemm_grouped(*operands, out.data_ptr(), ldy, _dt(out), _dt(X), R, N, K, leaf, k_first, _stream()), "tbik_gemm_grouped")
+    return out
+
+
+def tbik_gemm_grouped_swiglu(X: torch.Tensor, W_gu: torch.Tensor, offsets: torch.Tensor, leaf: int, k_first: int = 1, rows: torch.Tensor | None = None,
+                             out: torch.Tensor | None = None) -> torch.Tensor:
+    """act[i] = tbik_gemm_swiglu of X[rows[i]] and W_gu[e], bit for bit; W_gu [groups, K, 2 I], gate columns first.  Otherwise as tbik_gemm_grouped."""
+    operands, R, N, K = _grouped_operands(X, W_gu, offsets, rows)
+    if N % 2 != 0:
+        raise ValueError("W_gu holds gate and up columns: an even number, got %d" % N)
+    if out is None:
+        out = torch.empty((R, N // 2), dtype=X.dtype, device=X.device)
+    lda = _rowmajor(out, "out")
+    if out.shape != (R, N // 2) or out.dtype != X.dtype:
+        raise ValueError("out must have the shape %s and X's type" % ((R, N // 2),))
+    _on_current_device(X, W_gu, offsets, rows, out)
+    _check(lib().tbik_gemm_grouped_swiglu(*operands, out.data_ptr(), lda, _dt(X), R, N // 2, K, leaf, k_first, _stream()), "tbik_gemm_grouped_swiglu")
+    return out
+
+
+def tbik_gemm_grouped_shard_partials(X: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, leaf: int, k_first: int, P: int,
+                                     rows: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """partials [P, R, N] (float32): tbik_gemm_shard_partials of each row and its group's weight."""
+    operands, R, N, K = _grouped_operands(X, W, offsets, rows)
+    if out is None:
+        out = torch.empty((max(P, 0), R, N), dtype=torch.float32, device=X.device)
+    if out.shape != (P, R, N) or out.dtype != torch.float32 or not out.is_contiguous():
+        raise ValueError("out must be a contiguous float32 tensor of shape %s" % ((P, R, N),))
+    _on_current_device(X, W, offsets, rows, out)
+    _check(lib().tbik_gemm_grouped_shard_partials(*operands, out.data_ptr(), _dt(X), R, N, K, leaf, k_first, P, _stream()), "tbik_gemm_grouped_shard_partials")
+    return out
+
+
+def tbik_combine_experts(Y: torch.Tensor, slots: torch.Tensor, weights: torch.Tensor, residual: torch.Tensor | None = None, out_dtype=None,
+                         out: torch.Tensor | None = None) -> torch.Tensor:
+    """out[t] = sum_j weights[t, j] * Y[slots[t, j]] (+ residual[t]), j ascending in fp32, rounded once.  Y [R, H] is bfloat16 or float16, or float32
+    [R, H] or [P, R, H], the partial sums of P shards.  A slot that is no row of Y adds nothing.  The output's type: residual's, else Y's."""
+    if Y.dim() == 3:
+        if Y.dtype != torch.float32:
+            raise TypeError("shards' partial sums are float32, got %s" % Y.dtype)
+        P, R, H = Y.shape
+    else:
+        P, (R, H) = 1, Y.shape
+    if Y.dtype == torch.float32:
+        if not Y.is_contiguous() or not Y.is_cuda:
+            raise ValueError("float32 Y must be a contiguous GPU tensor")
+        ldy = H
+    else:
+        ldy = _rowmajor(Y, "Y")
+    T, k = slots.shape
+    _int32(slots, "slots", (T, k))
+    if weights.shape != slots.shape or weights.dtype != torch.float32 or not weights.is_contiguous():
+        raise ValueError("weights must be a contiguous float32 tensor of slots' shape")
+    if out is None:
+        out = torch.empty((T, H), dtype=out_dtype or (residual.dtype if residual is not None else Y.dtype), device=Y.device)
+    ldo = _rowmajor(out, "out")
+    if out.shape != (T, H) or (residual is not None and (residual.shape != (T, H) or residual.dtype != out.dtype)):
+        raise ValueError("out and residual must have the shape %s and one type" % ((T, H),))
+    ldr = _rowmajor(residual, "residual") if residual is not None else 0
+    _on_current_device(Y, slots, weights, residual, out)
+    _check(lib().tbik_combine_experts(Y.data_ptr(), ldy, _dt(Y), P, R, slots.data_ptr(), weights.data_ptr(), residual.data_ptr() if residual is not None else None,
+                                      ldr, out.data_ptr(), ldo, _dt(out), T, H, k, _stream()), "tbik_combine_experts")
+    return out
+
+
+def _w4_operands(X, Wq, scales, zeros):
+    """(arguments up to the group, M, N, K)"""
+    ldx, ldw, lds = _rowmajor(X, "X"), _rowmajor(Wq, "Wq"), _rowmajor(scales, "scales")
+    if X.dtype not in _SIXTEEN_BITS or scales.dtype != X.dtype:
+        raise TypeError("X and scales are both bfloat16 or both float16, got %s and %s" % (X.dtype, scales.dtype))
+    if Wq.dtype != torch.uint8 or (zeros is not None and zeros.dtype != torch.uint8):
+        raise TypeError("Wq and zeros hold bytes (uint8)")
+    M, K = X.shape
+    N = Wq.shape[0]
+    groups = scales.shape[1]
+    if K % 2 != 0 or Wq.shape[1] != K // 2 or scales.shape[0] != N or groups == 0 or K % groups != 0:
+        raise ValueError("Wq must be [N, K / 2] and scales [N, K / group], got %s and %s for K = %d" % (tuple(Wq.shape), tuple(scales.shape), K))
+    ldz = 0
+    if zeros is not None:
+        ldz = _rowmajor(zeros, "zeros")
+        if zeros.shape != scales.shape:
+            raise ValueError("zeros must have scales' shape")
+    return (X.data_ptr(), ldx, Wq.data_ptr(), ldw, scales.data_ptr(), lds, zeros.data_ptr() if zeros is not None else None, ldz, K // groups), M, N, K
+
+
+def tbik_gemm_w4(X: torch.Tensor, Wq: torch.Tensor, scales: torch.Tensor, leaf: int, k_first: int = 1, zeros: torch.Tensor | None = None, out_dtype=None,
+                 out: torch.Tensor | None = None) -> torch.Tensor:
+    """Y = X @ W in the tree order, W[k, n] = scales[n, k / group] * (q[n, k] - zeros[n, k / group]) (8 without zeros).  Wq uint8 [N, K / 2]: two
+    4-bit elements a byte, the even k in the low half; scales [N, K / group] of X's type; zeros uint8 likewise.  Y is float32 or (default) X's type."""
+    operands, M, N, K = _w4_operands(X, Wq, scales, zeros)
+    if out is None:
+        out = torch.empty((M, N), dtype=out_dtype or X.dtype, device=X.device)
+    ldy = _rowmajor(out, "out")
+    if out.shape != (M, N):
+        raise ValueError("out must have the shape %s" % ((M, N),))
+    _on_current_device(X, Wq, scales, zeros, out)
+    _check(lib().tbik_gemm_w4(*operands, out.data_ptr(), ldy, _dt(out), _dt(X), M, N, K, leaf, k_first, _stream()), "tbik_gemm_w4")
+    return out
+
+
+def tbik_gemm_shard_partials_w4(X: torch.Tensor, Wq: torch.Tensor, scales: torch.Tensor, leaf: int, k_first: int, P: int, zeros: torch.Tensor | None = None,
+                                out: torch.Tensor | None = None) -> torch.Tensor:
+    """partials [P, M, N] (float32) of the same product, for tbik_tree_combine."""
+    operands, M, N, K = _w4_operands(X, Wq, scales, zeros)
+    if out is None:
+        out = torch.empty((max(P, 0), M, N), dtype=torch.float32, device=X.device)
+    if out.shape != (P, M, N) or out.dtype != torch.float32 or not out.is_contiguous():
+        raise ValueError("out must be a contiguous float32 tensor of shape %s" % ((P, M, N),))
+    _on_current_device(X, Wq, scales, zeros, out)
+    _check(lib().tbik_gemm_shard_partials_w4(*operands, out.data_ptr(), _dt(X), M, N, K, leaf, k_first, P, _stream()), "tbik_gemm_shard_partials_w4")
+    return out
+
+
+def tbik_rmsnorm_residual_rmsnorm(y: torch.Tensor, residual: torch.Tensor, post_weight: torch.Tensor | None, next_weight: torch.Tensor | None, eps: float = 1e-6,
+                                  residual_scale: float = 1.0, gate: torch.Tensor | None = None, hidden: torch.Tensor | None = None,
+                                  normed: torch.Tensor | None = None):
+    """(hidden, normed): hidden = residual * residual_scale + gate * RMSNorm(y; post_weight), rounded to residual's type; normed = RMSNorm(hidden;
+    next_weight).  y [M, H] of that type, or float32 [P, M, H], shards' partial sums, which are combined and rounded first.  gate: [H] or [1, H],
+    [M, 1] or [M, H].  Without post_weight y is taken as it is; without next_weight normed is None.  `hidden` may be residual or y."""
+    ldr = _rowmajor(residual, "residual")
+    M, H = residual.shape
+    dtype = residual.dtype
+    if dtype not in _SIXTEEN_BITS:
+        raise TypeError("residual is bfloat16 or float16, got %s" % dtype)
+    if y.dim() == 3:
+        if y.dtype != torch.float32 or y.shape[1:] != (M, H) or not y.is_contiguous():
+            raise ValueError("shards' partial sums are a contiguous float32 tensor [P, %d, %d]" % (M, H))
+        first = (None, 0, y.data_ptr(), y.shape[0])
+    else:
+        if y.shape != (M, H) or y.dtype != dtype:
+            raise ValueError("y must have residual's shape and type")
+        first = (y.data_ptr(), _rowmajor(y, "y"), None, 1)
+    for name, w in (("post_weight", post_weight), ("next_weight", next_weight)):
+        if w is not None and (w.shape != (H,) or w.dtype != dtype or not w.is_contiguous()):
+            raise ValueError("%s must be a contiguous tensor [%d] of residual's type" % (name, H))
+    gates = (None, 0, 0)
+    if gate is not None:
+        if gate.dtype != dtype or (gate.dim() == 1 and gate.shape != (H,)) or (gate.dim() != 1 and (gate.dim() != 2 or gate.shape[0] not in (1, M) or gate.shape[1] not in (1, H))):
+            raise ValueError("gate must be [H], [1, H], [M, 1] or [M, H] of residual's type, got %s" % (tuple(gate.shape),))
+        wide = gate.shape[-1] == H and H > 1
+        if wide and gate.stride(-1) != 1:
+            raise ValueError("gate's channels must be contiguous")
+        gates = (gate.data_ptr(), gate.stride(0) if gate.dim() == 2 and gate.shape[0] == M and M > 1 else 0, int(wide))
+    if hidden is None:
+        hidden = torch.empty((M, H), dtype=dtype, device=residual.device)
+    ldh, ldn = _rowmajor(hidden, "hidden"), 0
+    if next_weight is not None:
+        if normed is None:
+            normed = torch.empty((M, H), dtype=dtype, device=residual.device)
+        ldn = _rowmajor(normed, "normed")
+    elif normed is not None:
+        raise ValueError("normed needs next_weight")
+    if hidden.shape != (M, H) or hidden.dtype != dtype or (normed is not None and (normed.shape != (M, H) or normed.dtype != dtype)):
+        raise ValueError("hidden and normed must have residual's shape and type")
+    _on_current_device(y, residual, post_weight, next_weight, gate, hidden, normed)
+    _check(lib().tbik_rmsnorm_residual_rmsnorm(*first, residual.data_ptr(), ldr, residual_scale, post_weight.data_ptr() if post_weight is not None else None, *gates,
+                                               next_weight.data_ptr() if next_weight is not None else None, eps, hidden.data_ptr(), ldh,
+                                               normed.data_ptr() if normed is not None else None, ldn, _DTYPES[dtype], M, H, _stream()), "tbik_rmsnorm_residual_rmsnorm")
+    return hidden, normed
 
 
 def tbik_set_row_wait_limit(polls: int) -> int:

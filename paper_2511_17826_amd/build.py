@@ -20,7 +20,7 @@ LIB = os.path.join(HERE, "libtbik.so")
 SOURCES = ["gemm_mxfp8_epilogue.hip", "gemm_fp8_epilogue.hip", "gemm_tiled_epilogue.hip", "gemm_fp8.hip", "gemm_tiled.hip", "tbik_api.hip", "gemm_reference.hip", "gemm_f32.hip", "gemm_mxfp4.hip",
            "gemm_mxfp6.hip", "gemm_slice.hip", "combine.hip", "combine_epilogue.hip", "activation.hip", "activation_8bit.hip",
            "rmsnorm.hip", "rmsnorm_8bit.hip", "row_reduce.hip",
-           "attention.hip", "attention_decode.hip"]
+           "attention.hip", "attention_decode.hip", "route.hip", "gemm_grouped.hip", "experts_sum.hip", "gemm_w4.hip", "rmsnorm_join.hip"]
 
 # -ffp-contract=off: a tree addition or an RMSNorm multiply must never be fused into an FMA.
 # packed-fp32 ops are switched off for the device pass (known-bad forms on the test machines).

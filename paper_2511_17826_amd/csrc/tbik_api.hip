@@ -1232,6 +1232,150 @@ int tbik_silu_mul_mxfp8(const void *gate, int64_t ldg, const void *up, int64_t l
     return silu_mul_8bit(gate, ldg, up, ldu, q, ldq, scales, lds, true, dtype, q_dtype, M, I, hip_stream);
 }
 
+// ---- an MLP that is a mixture of experts, 4-bit weights, norms around a block ----
+size_t tbik_route_topk_workspace_bytes(int T, int E) { return T < 0 || E < 1 || E > kMaxGroups ? 0 : route_topk_workspace(T, E); }
+
+int tbik_route_topk(const void *logits, int64_t ldl, tbik_dtype dtype, int T, int E, int k, int renormalize, int32_t *experts, float *weights,
+                    int32_t *offsets, int32_t *rows, int32_t *slots, void *workspace, size_t workspace_bytes, void *hip_stream) {
+    if (dtype != TBIK_F32 && dtype != TBIK_BF16 && dtype != TBIK_F16) return TBIK_ERR_DTYPE;
+    if (T < 0 || E < 1 || k < 1 || k > E || (int64_t)T * k > 0x7fffffff) return TBIK_ERR_SHAPE;
+    if (E > kMaxGroups || k > kMaxChoices || T > (1 << 26)) return TBIK_ERR_UNSUPPORTED;
+    if (!offsets || (T > 0 && (!logits || !experts || !weights || !rows || !slots))) return TBIK_ERR_NULL;
+    if (T > 0 && ldl < E) return TBIK_ERR_SHAPE;
+    if (!aligned(logits, dtype == TBIK_F32 ? 4 : 2) || !aligned(experts, 4) || !aligned(weights, 4) || !aligned(offsets, 4) || !aligned(rows, 4) || !aligned(slots, 4))
+        return TBIK_ERR_ALIGN;
+    const size_t need = route_topk_workspace(T, E);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return TBIK_ERR_WORKSPACE;
+    if (need > 0 && !aligned(workspace, 256)) return TBIK_ERR_ALIGN;
+    hipError_t e = launch_route_topk(logits, ldl, (int)dtype, T, E, k, renormalize != 0, experts, weights, offsets, rows, slots, workspace, (hipStream_t)hip_stream);
+    return e == hipSuccess ? TBIK_OK : hip_fail(e);
+}
+
+// Y: [R, ldy] of y_dtype, or partials: dense [P, R, N]; swiglu: N = 2 I columns of the weights, Y is [R, I].
+static int gemm_grouped(tbik_dtype x_dtype, const void *X, int64_t ldx, int tokens, const int32_t *rows, const void *W, int64_t ldw, int64_t stride, int groups,
+                        const int32_t *offsets, void *Y, int64_t ldy, tbik_dtype y_dtype, float *partials, bool swiglu,
+                        int R, int N, int K, int leaf, int k_first, int P, void *hip_stream) {
+    int sl, ns;
+    int rc = check_tree(R, N, K, leaf, k_first, P, &sl, &ns);
+    if (rc != TBIK_OK) return rc;
+    if (x_dtype != TBIK_BF16 && x_dtype != TBIK_F16) return TBIK_ERR_DTYPE;
+    if (!partials && !legal_y_dtype((int)y_dtype, (int)x_dtype)) return TBIK_ERR_DTYPE;
+    if (tokens < 0 || groups < 0 || (!rows && tokens < R)) return TBIK_ERR_SHAPE;
+    if (groups > kMaxGroups) return TBIK_ERR_UNSUPPORTED;
+    if (R == 0 || N == 0 || groups == 0 || tokens == 0) return TBIK_OK;
+    rc = check_operands((int)x_dtype, X, ldx, W, ldw, N, K);
+    if (rc != TBIK_OK) return rc;
+    if (!offsets || (!Y && !partials)) return TBIK_ERR_NULL;
+    if (stride < 0 || (Y && ldy < (swiglu ? N / 2 : N))) return TBIK_ERR_SHAPE;
+    if (stride % 8 != 0 || !aligned(offsets, 4) || !aligned(rows, 4) || (Y && !aligned(Y, y_dtype == TBIK_F32 ? 4 : 2)) || !aligned(partials, 16)) return TBIK_ERR_ALIGN;
+    GroupedArgs a;
+    static_cast<GemmArgs &>(a) = GemmArgs{(const uint16_t *)X, ldx, (const uint16_t *)W, ldw, partials, Y, ldy, (int)y_dtype, R, N, K, sl, ns, P, (int)x_dtype, swiglu};
+    a.offsets = offsets;
+    a.rows = rows;
+    a.tokens = tokens;
+    a.groups = groups;
+    a.weight_stride = stride;
+    hipError_t e = launch_gemm_grouped_reference(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? TBIK_OK : hip_fail(e);
+}
+
+int tbik_gemm_grouped(const void *X, int64_t ldx, int tokens, const int32_t *rows, const void *W, int64_t ldw, int64_t weight_stride, int groups,
+                      const int32_t *offsets, void *Y, int64_t ldy, tbik_dtype y_dtype, tbik_dtype x_dtype, int R, int N, int K, int leaf, int k_first,
+                      void *hip_stream) {
+    return gemm_grouped(x_dtype, X, ldx, tokens, rows, W, ldw, weight_stride, groups, offsets, Y, ldy, y_dtype, nullptr, false, R, N, K, leaf, k_first, 1, hip_stream);
+}
+
+int tbik_gemm_grouped_swiglu(const void *X, int64_t ldx, int tokens, const int32_t *rows, const void *W_gu, int64_t ldw, int64_t weight_stride, int groups,
+                             const int32_t *offsets, void *act, int64_t lda, tbik_dtype dtype, int R, int I, int K, int leaf, int k_first, void *hip_stream) {
+    if (I < 0 || I > 0x3fffffff || I % 8 != 0) return TBIK_ERR_SHAPE;
+    return gemm_grouped(dtype, X, ldx, tokens, rows, W_gu, ldw, weight_stride, groups, offsets, act, lda, dtype, nullptr, true, R, 2 * I, K, leaf, k_first, 1, hip_stream);
+}
+
+int tbik_gemm_grouped_shard_partials(const void *X, int64_t ldx, int tokens, const int32_t *rows, const void *W, int64_t ldw, int64_t weight_stride, int groups,
+                                     const int32_t *offsets, float *partials, tbik_dtype x_dtype, int R, int N, int K, int leaf, int k_first, int P,
+                                     void *hip_stream) {
+    if (!partials && R > 0 && N > 0) return TBIK_ERR_NULL;
+    return gemm_grouped(x_dtype, X, ldx, tokens, rows, W, ldw, weight_stride, groups, offsets, nullptr, 0, TBIK_F32, partials, false, R, N, K, leaf, k_first, P, hip_stream);
+}
+
+int tbik_combine_experts(const void *Y, int64_t ldy, tbik_dtype y_dtype, int P, int R, const int32_t *slots, const float *weights,
+                         const void *residual, int64_t ldr, void *out, int64_t ldo, tbik_dtype out_dtype, int T, int H, int k, void *hip_stream) {
+    if (T < 0 || H < 0 || k < 1 || R < 0) return TBIK_ERR_SHAPE;
+    if (P < 1 || !is_pow2(P) || P > TBIK_MAX_SHARDS) return TBIK_ERR_SHARDS;
+    if (y_dtype != TBIK_F32 && y_dtype != TBIK_BF16 && y_dtype != TBIK_F16) return TBIK_ERR_DTYPE;
+    if (out_dtype != TBIK_F32 && (y_dtype == TBIK_F32 ? out_dtype != TBIK_BF16 && out_dtype != TBIK_F16 : out_dtype != y_dtype)) return TBIK_ERR_DTYPE;
+    if (y_dtype != TBIK_F32 && P != 1) return TBIK_ERR_SHARDS;
+    if (P > 16 || k > kMaxChoices) return TBIK_ERR_UNSUPPORTED;
+    if (T == 0 || H == 0) return TBIK_OK;
+    if ((!Y && R > 0) || !slots || !weights || !out) return TBIK_ERR_NULL;
+    if (ldo < H || (y_dtype != TBIK_F32 && ldy < H) || (residual && (ldr < H || (residual == out && ldr != ldo)))) return TBIK_ERR_SHAPE;
+    const uintptr_t in = y_dtype == TBIK_F32 ? 4 : 2, to = out_dtype == TBIK_F32 ? 4 : 2;
+    if (!aligned(Y, in) || !aligned(out, to) || !aligned(residual, to) || !aligned(slots, 4) || !aligned(weights, 4)) return TBIK_ERR_ALIGN;
+    const ExpertsSumArgs a{Y, ldy, (int)y_dtype, y_dtype == TBIK_F32 ? P : 0, R, slots, weights, residual, residual ? ldr : 0, out, ldo, (int)out_dtype, T, H, k};
+    hipError_t e = launch_experts_sum(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? TBIK_OK : hip_fail(e);
+}
+
+int tbik_rmsnorm_residual_rmsnorm(const void *y, int64_t ldy, const float *partials, int P, const void *residual, int64_t ldr, float residual_scale,
+                                  const void *post_weight, const void *gate, int64_t gate_row_stride, int gate_column_stride, const void *next_weight, float eps,
+                                  void *hidden, int64_t ldh, void *normed, int64_t ldn, tbik_dtype dtype, int M, int H, void *hip_stream) {
+    if (dtype != TBIK_BF16 && dtype != TBIK_F16) return TBIK_ERR_DTYPE;
+    if (M < 0 || H <= 0 || H % 8 != 0 || H > 65536) return TBIK_ERR_SHAPE;
+    if (partials && (P < 1 || !is_pow2(P) || P > TBIK_MAX_SHARDS)) return TBIK_ERR_SHARDS;
+    if (partials && P > 16) return TBIK_ERR_UNSUPPORTED;
+    if (gate && ((gate_column_stride != 0 && gate_column_stride != 1) || gate_row_stride < 0)) return TBIK_ERR_SHAPE;
+    if (M == 0) return TBIK_OK;
+    if (!y == !partials || !residual || !hidden || !next_weight != !normed) return TBIK_ERR_NULL;
+    if ((y && ldy < H) || ldr < H || ldh < H || (normed && ldn < H)) return TBIK_ERR_SHAPE;
+    if ((hidden == y && ldh != ldy) || (hidden == residual && ldh != ldr)) return TBIK_ERR_SHAPE;
+    if (!aligned(y, 16) || !aligned(partials, 16) || !aligned(residual, 16) || !aligned(hidden, 16) || !aligned(normed, 16) || !aligned(post_weight, 16) ||
+        !aligned(next_weight, 16) || (y && ldy % 8 != 0) || ldr % 8 != 0 || ldh % 8 != 0 || (normed && ldn % 8 != 0))
+        return TBIK_ERR_ALIGN;
+    if (gate && (gate_column_stride ? !aligned(gate, 16) || gate_row_stride % 8 != 0 : !aligned(gate, 2))) return TBIK_ERR_ALIGN;
+    const JoinArgs a{(const uint16_t *)y, ldy, partials, partials ? P : 0, (const uint16_t *)residual, ldr, (const uint16_t *)post_weight, (const uint16_t *)next_weight,
+                     (const uint16_t *)gate, gate ? gate_row_stride : 0, gate ? gate_column_stride : 0, (uint16_t *)hidden, ldh, (uint16_t *)normed, ldn,
+                     residual_scale, eps, M, H, (int)dtype};
+    hipError_t e = launch_rmsnorm_join(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? TBIK_OK : hip_fail(e);
+}
+
+static int gemm_w4(tbik_dtype x_dtype, const void *X, int64_t ldx, const void *Wq, int64_t ldwq, const void *scales, int64_t lds, const void *zeros, int64_t ldz,
+                   int group, void *Y, int64_t ldy, tbik_dtype y_dtype, float *partials, int M, int N, int K, int leaf, int k_first, int P, void *hip_stream) {
+    int sl, ns;
+    int rc = check_tree(M, N, K, leaf, k_first, P, &sl, &ns);
+    if (rc != TBIK_OK) return rc;
+    if (group < 32 || group % 32 != 0 || sl % group != 0) return TBIK_ERR_SHAPE;
+    if (x_dtype != TBIK_BF16 && x_dtype != TBIK_F16) return TBIK_ERR_DTYPE;
+    if (!partials && !legal_y_dtype((int)y_dtype, (int)x_dtype)) return TBIK_ERR_DTYPE;
+    if (ns / P > 128) return TBIK_ERR_UNSUPPORTED;
+    if (M == 0 || N == 0) return TBIK_OK;
+    if (!X || !Wq || !scales || (!Y && !partials)) return TBIK_ERR_NULL;
+    if (ldx < K || ldwq < K / 2 || lds < K / group || (zeros && ldz < K / group) || (Y && ldy < N)) return TBIK_ERR_SHAPE;
+    if (!aligned(X, 16) || ldx % 8 != 0 || !aligned(Wq, 16) || ldwq % 16 != 0 || !aligned(scales, 2) || (Y && !aligned(Y, y_dtype == TBIK_F32 ? 4 : 2)) ||
+        !aligned(partials, 16))
+        return TBIK_ERR_ALIGN;
+    W4Args a;
+    static_cast<GemmArgs &>(a) = GemmArgs{(const uint16_t *)X, ldx, (const uint16_t *)Wq, ldwq, partials, Y, ldy, (int)y_dtype, M, N, K, sl, ns, P, (int)x_dtype, 0};
+    a.scales = (const uint16_t *)scales;
+    a.lds = lds;
+    a.zeros = (const uint8_t *)zeros;
+    a.ldz = ldz;
+    a.group = group;
+    hipError_t e = launch_gemm_w4(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? TBIK_OK : hip_fail(e);
+}
+
+int tbik_gemm_w4(const void *X, int64_t ldx, const void *Wq, int64_t ldwq, const void *scales, int64_t lds, const void *zeros, int64_t ldz, int group,
+                 void *Y, int64_t ldy, tbik_dtype y_dtype, tbik_dtype x_dtype, int M, int N, int K, int leaf, int k_first, void *hip_stream) {
+    return gemm_w4(x_dtype, X, ldx, Wq, ldwq, scales, lds, zeros, ldz, group, Y, ldy, y_dtype, nullptr, M, N, K, leaf, k_first, 1, hip_stream);
+}
+
+int tbik_gemm_shard_partials_w4(const void *X, int64_t ldx, const void *Wq, int64_t ldwq, const void *scales, int64_t lds, const void *zeros, int64_t ldz,
+                                int group, float *partials, tbik_dtype x_dtype, int M, int N, int K, int leaf, int k_first, int P, void *hip_stream) {
+    if (!partials && M > 0 && N > 0) return TBIK_ERR_NULL;
+    return gemm_w4(x_dtype, X, ldx, Wq, ldwq, scales, lds, zeros, ldz, group, nullptr, 0, TBIK_F32, partials, M, N, K, leaf, k_first, P, hip_stream);
+}
+
 int tbik_tree_allreduce(float *bufs, int P, int64_t n, void *hip_stream) {
     if (n < 0) return TBIK_ERR_SHAPE;
     if (P < 1 || !is_pow2(P) || P > TBIK_MAX_SHARDS) return TBIK_ERR_SHARDS;

@@ -122,6 +122,72 @@ size_t mxfp6_retiled_scales_bytes(int M, int N, int K);
 bool gemm_slice_takes(const GemmArgs &a, const Mxfp4Scales *sc);
 hipError_t launch_gemm_slice(const GemmArgs &a, const Mxfp4Scales *sc, hipStream_t s);
 
+// ---- an MLP that is a mixture of experts ----
+constexpr int kMaxGroups = 512;            // experts
+constexpr int kMaxChoices = 32;            // of a token
+size_t route_topk_workspace(int T, int E);
+hipError_t launch_route_topk(const void *logits, int64_t ldl, int dtype, int T, int E, int k, int renormalize, int32_t *experts, float *weights,
+                             int32_t *offsets, int32_t *rows, int32_t *slots, void *workspace, hipStream_t s);
+
+// Products grouped by expert: the GemmArgs of one of them -- M is the rows of the output, W the first weight, 16-bit operands -- and
+struct GroupedArgs : GemmArgs {
+    const int32_t *offsets;                // device, [groups + 1]: group e is rows offsets[e] .. offsets[e + 1] - 1
+    const int32_t *rows;                   // device, [M]: row of X of each row of the output, or nullptr: its own
+    int tokens;                            // rows of X
+    int groups;
+    int64_t weight_stride;                 // elements from one weight to the next
+};
+hipError_t launch_gemm_grouped_reference(const GroupedArgs &a, hipStream_t s);
+// Workgroups that hold all of K, `waves` wavefronts beside each other along it.
+bool gemm_grouped_slice_supports(const GroupedArgs &a);
+hipError_t launch_gemm_grouped_slice(const GroupedArgs &a, hipStream_t s);
+// The tiled kernels; variant: VARIANT_T128, VARIANT_T64 or VARIANT_T32.
+bool gemm_grouped_tiled_supports(const GroupedArgs &a, int variant);
+hipError_t launch_gemm_grouped_tiled(const GroupedArgs &a, int variant, hipStream_t s);
+
+struct ExpertsSumArgs {
+    const void *y;                         // 16-bit [R, ldy] (P == 0), or fp32, dense [P, R, H]
+    int64_t ldy;
+    int y_dtype, P, R;
+    const int32_t *slots;                  // [T, k]
+    const float *weights;
+    const void *residual;                  // [T, ldr] of out_dtype, or nullptr
+    int64_t ldr;
+    void *out;
+    int64_t ldo;
+    int out_dtype, T, H, k;
+};
+hipError_t launch_experts_sum(const ExpertsSumArgs &a, hipStream_t s);
+
+struct JoinArgs {
+    const uint16_t *y;                     // [M, ldy], P == 0
+    int64_t ldy;
+    const float *partials;                 // dense [P, M, H], P > 0
+    int P;
+    const uint16_t *residual;
+    int64_t ldr;
+    const uint16_t *post, *next, *gate;    // each may be nullptr
+    int64_t gate_row;
+    int gate_column;
+    uint16_t *hidden;
+    int64_t ldh;
+    uint16_t *normed;                      // with next
+    int64_t ldn;
+    float residual_scale, eps;
+    int M, H, dtype;
+};
+hipError_t launch_rmsnorm_join(const JoinArgs &a, hipStream_t s);
+
+// 4-bit weights with a scale per group of k and channel, 16-bit rows (x_dtype): W points to [N, ldw] bytes.
+struct W4Args : GemmArgs {
+    const uint16_t *scales;                // x_dtype, [N, lds]
+    int64_t lds;
+    const uint8_t *zeros;                  // [N, ldz], or nullptr: 8
+    int64_t ldz;
+    int group;
+};
+hipError_t launch_gemm_w4(const W4Args &a, hipStream_t s);
+
 // Y = T(partials[0..P)) elementwise + one rounding.
 hipError_t launch_tree_combine(const float *partials, int P, void *Y, int64_t ldy, int y_dtype, int M, int N,
                                hipStream_t s);
