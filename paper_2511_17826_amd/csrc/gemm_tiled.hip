@@ -20,6 +20,7 @@
 #include <type_traits>
 
 #include "tbik_device.hpp"
+#include "grouped.hpp"
 #include "tbik_internal.hpp"
 #include "tile_epilogue.hpp"
 #include "tile_store.hpp"
@@ -73,6 +74,13 @@ struct TiledEpilogueParams : TiledParams {
     int from_ring;              // the epilogue's operands come through the ring (tile_epilogue.hpp), or there are none
     int vector_slots, residual_slots;      // positions of the load stream behind a tile's last stage: 0 or 1 each
 };
+struct TiledGroupedParams : TiledParams {   // M: rows of the output; tiles and work are the device's
+    const int32_t *offsets, *rows;
+    int tokens, groups, shards;
+    int64_t weight_stride;
+};
+template <bool EPI, bool GROUP>
+using TiledParamsOf = std::conditional_t<EPI, TiledEpilogueParams, std::conditional_t<GROUP, TiledGroupedParams, TiledParams>>;
 
 // ---------------------------------------------------------------------------------------------
 // BM = 32*MT*WM rows, BN = 32*NT*WN columns, WM*WN = 4 wavefronts.
@@ -83,9 +91,12 @@ struct TiledEpilogueParams : TiledParams {
 // F16: the operands (and a 16-bit output) are IEEE binary16 instead of bf16; only the MFMA opcode and the output
 // conversion differ.
 // EPI: the output passes through an epilogue (epilogue.hpp); P == 1 then, and no gated activation.
-template <int LEVELS, int WM, int WN, int MT, int NT, int RING, bool F16, bool EPI>
+// GROUP: products grouped by expert (grouped.hpp).  A row tile belongs to one group and its number of rows is what the group leaves
+// it; which tiles there are every workgroup works out from the offsets, in registers.  A tile's rows of X are gathered by the
+// lanes' offsets; reading their indexes waits for the loads in flight once a tile.
+template <int LEVELS, int WM, int WN, int MT, int NT, int RING, bool F16, bool EPI, bool GROUP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
-void gemm_tiled_kernel(const std::conditional_t<EPI, TiledEpilogueParams, TiledParams> p) {
+void gemm_tiled_kernel(const TiledParamsOf<EPI, GROUP> p) {
     constexpr int BM = 32 * MT * WM, BN = 32 * NT * WN;
     static_assert(BN == BN_TILE && WM * WN == 4, "tile shape");
     constexpr int A_LOADS = BM / 32;          // 1 KiB loads per wavefront and stage: BM rows / 8 rows / 4 wavefronts
@@ -93,6 +104,7 @@ void gemm_tiled_kernel(const std::conditional_t<EPI, TiledEpilogueParams, TiledP
     static_assert(B_LOADS == 4 && A_LOADS <= 4, "one W load and at most one X load per K-step");
     constexpr int REGION_BYTES = (A_LOADS + B_LOADS) * 1024;   // stage layout: one region per loading wavefront,
     constexpr int STAGE_BYTES = 4 * REGION_BYTES;               // [8*A_LOADS rows of X | 16 rows of W]
+    constexpr bool ACT_ONLY = GROUP && REGION_BYTES < 32 * 32 * NT * 4;   // a region holds the patch of the gated activation only
 
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
 
@@ -101,6 +113,14 @@ void gemm_tiled_kernel(const std::conditional_t<EPI, TiledEpilogueParams, TiledP
     const int wm = wave / WN, wn = wave % WN;
     const int li = lane & 31, lg = lane >> 5;
     const int stages_per_item = p.ns_per_shard * p.stages_per_superleaf;
+    std::conditional_t<GROUP, GroupMap<BM>, int> map;
+    int tiles = p.tiles, work = p.work;
+    if constexpr (GROUP) {
+        map.read(p.offsets, p.groups, p.M, lane);
+        tiles = map.tiles * p.tiles_n;
+        work = tiles * p.shards;
+        if ((int)blockIdx.x >= work) return;
+    }
 
     // ---- global -> LDS, without passing through registers (global_load_lds_dwordx4) ----
     // One such instruction moves 64 x 16 bytes: lane i's chunk lands at LDS base + 16*i, so a
@@ -127,23 +147,36 @@ void gemm_tiled_kernel(const std::conditional_t<EPI, TiledEpilogueParams, TiledP
 
     int issue_m0 = 0, issue_n0 = 0;            // EPI: the tile whose stages are being loaded
     auto point_loads_at = [&](int item) __attribute__((always_inline)) {
-        const int tile = EPI ? item : item % p.tiles, shard = EPI ? 0 : item / p.tiles;
-        const int m0 = (tile / p.tiles_n) * BM, n0 = (tile % p.tiles_n) * BN;
+        const int tile = EPI ? item : item % tiles, shard = EPI ? 0 : item / tiles;
+        int m0 = (tile / p.tiles_n) * BM, rows_end = p.M;
+        const int n0 = (tile % p.tiles_n) * BN;
         if (EPI) {
             issue_m0 = m0;
             issue_n0 = n0;
         }
         const int64_t kbase = (int64_t)shard * p.k_per_shard;
-        a_ptr = uniform_pointer(reinterpret_cast<const char *>(p.X + (int64_t)m0 * p.ldx + kbase));
+        const uint16_t *weight = p.W, *first_row = p.X + (int64_t)m0 * p.ldx;
+        if constexpr (GROUP) {
+            const GroupRows at = map.at(tile / p.tiles_n);
+            m0 = at.first;
+            rows_end = at.end;
+            weight += at.group * p.weight_stride;
+            first_row = p.rows ? p.X : p.X + (int64_t)m0 * p.ldx;
+        }
+        a_ptr = uniform_pointer(reinterpret_cast<const char *>(first_row + kbase));
         // Gated activation: the 128 columns of a tile are, per wavefront column, 32 gate channels and the same 32 up
         // channels (a lane then holds gate and up of one channel in its two column blocks), taken from the two halves
         // of W; the tile starts at channel n0 / 2.
-        b_ptr = uniform_pointer(reinterpret_cast<const char *>(p.W + kbase * p.ldw + (p.swiglu ? n0 / 2 : n0)) - LANE_BIAS);
+        b_ptr = uniform_pointer(reinterpret_cast<const char *>(weight + kbase * p.ldw + (p.swiglu ? n0 / 2 : n0)) - LANE_BIAS);
 #pragma unroll
         for (int j = 0; j < A_LOADS; ++j) {
             const int r = (wave * A_LOADS + j) * 8 + (lane >> 3);
             const int c = (lane & 7) ^ ((r >> 1) & 7);
-            aoff[j] = (unsigned)(min(r, p.M - 1 - m0) * (int)p.ldx + c * 8) * 2u + (unsigned)((A_LOADS - j) * 1024);
+            int row = min(r, rows_end - 1 - m0);
+            if constexpr (GROUP) {
+                if (p.rows) row = source_row(p.rows, m0 + row, p.tokens);
+            }
+            aoff[j] = (unsigned)(row * (int)p.ldx + c * 8) * 2u + (unsigned)((A_LOADS - j) * 1024);
         }
 #pragma unroll
         for (int j = 0; j < B_LOADS; ++j) {
@@ -174,11 +207,11 @@ void gemm_tiled_kernel(const std::conditional_t<EPI, TiledEpilogueParams, TiledP
                 } else if (behind < p.vector_slots + p.residual_slots) {
                     point_at_residual<MT, NT>(loads, p.epilogue, issue_m0, issue_n0, p.M, p.N, wave_u / WN, wave_u % WN, here);
                 } else {                               // past the end: a tile's stages again (nobody consumes them)
-                    if (issue_item + (int)gridDim.x < p.work) issue_item += gridDim.x;
+                    if (issue_item + (int)gridDim.x < work) issue_item += gridDim.x;
                     point_loads_at(issue_item);
                     issue_stage = 0;
                 }
-            } else if (issue_item + (int)gridDim.x < p.work) {
+            } else if (issue_item + (int)gridDim.x < work) {
                 issue_item += gridDim.x;
                 point_loads_at(issue_item);
                 issue_stage = 0;
@@ -341,14 +374,20 @@ void gemm_tiled_kernel(const std::conditional_t<EPI, TiledEpilogueParams, TiledP
         for (int q = 1; q < p.stages_per_superleaf; ++q) stage(std::false_type{}, a);
     };
 
-    for (int item = blockIdx.x; item < p.work; item += gridDim.x) {
+    for (int item = blockIdx.x; item < work; item += gridDim.x) {
         SubtreeWalker<LEVELS>::run(superleaf, acc, acc2, stash);
 
         // ---- acc holds T(superleaves of this shard) for this tile: store it ----
-        const int tile = EPI ? item : item % p.tiles, shard = EPI ? 0 : item / p.tiles;
-        const int m0 = (tile / p.tiles_n) * BM, n0 = (tile % p.tiles_n) * BN;
+        const int tile = EPI ? item : item % tiles, shard = EPI ? 0 : item / tiles;
+        int m0 = (tile / p.tiles_n) * BM, rows_end = p.M;
+        const int n0 = (tile % p.tiles_n) * BN;
+        if constexpr (GROUP) {
+            const GroupRows at = map.at(tile / p.tiles_n);
+            m0 = at.first;
+            rows_end = at.end;
+        }
         float *part = p.partials ? p.partials + (int64_t)shard * p.M * p.N : nullptr;
-        const bool interior = (m0 + BM <= p.M) && (n0 + BN <= p.N);
+        const bool interior = (m0 + BM <= rows_end) && (n0 + BN <= p.N);
         if constexpr (EPI) {                                // the patch and its barrier as below
             int here = lane;
             asm volatile("" : "+v"(here));             // as above
@@ -382,7 +421,7 @@ void gemm_tiled_kernel(const std::conditional_t<EPI, TiledEpilogueParams, TiledP
                 store_elements_with_epilogue(acc, patch, p.epilogue, p.Y, p.ldy, row0, col0, p.M, p.N, here);
             }
             stores_in_flight = stores;
-            const int behind_it = item + (int)gridDim.x < p.work ? extra : 0;      // the last tile: no more loads
+            const int behind_it = item + (int)gridDim.x < work ? extra : 0;      // the last tile: no more loads
             if (behind_it) {
                 // On to the next tile's first stage: as many positions of the stream are issued as are consumed, the first into the slot of
                 // the last stage (its patch has been read).  With one position the rest is a stage's entry as always: its wait leaves
@@ -413,7 +452,7 @@ void gemm_tiled_kernel(const std::conditional_t<EPI, TiledEpilogueParams, TiledP
             // store instructions is fixed (no lane masks, no branches), which the load accounting above relies on.
             // The patch is the wavefront's own region of the stage slot that was multiplied last: nothing is loaded
             // into that slot before the next stage's barrier, but the other wavefronts may still be reading it.
-            static_assert(REGION_BYTES >= 32 * WCOLS * 4, "the output patch must fit a wavefront's region of a slot");
+            static_assert(ACT_ONLY || REGION_BYTES >= 32 * WCOLS * 4, "the output patch must fit a wavefront's region of a slot");
             const int last_slot = cur == 0 ? RING - 1 : cur - 1;
             float *patch = reinterpret_cast<float *>(smem + last_slot * STAGE_BYTES + wave * REGION_BYTES);
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -422,7 +461,7 @@ void gemm_tiled_kernel(const std::conditional_t<EPI, TiledEpilogueParams, TiledP
             // per store), and a store's address is a wave-uniform base plus a 32-bit lane offset.
             const int wm_u = wave_u / WN, wn_u = wave_u % WN;          // the same numbers as wm, wn, known to be uniform
             const int col0 = n0 + wn_u * WCOLS;
-            if (NT == 2 && p.swiglu) {
+            if (NT == 2 && (ACT_ONLY || p.swiglu)) {
                 // Gate and up of a channel sit in the lane's two column blocks: both are rounded as the 16-bit outputs
                 // of two separate GEMMs would be, the activation is applied, and the 32 x 32 block goes through the patch.
                 constexpr int CPR = 4, RPI = 16, N_IT = 2;
@@ -518,15 +557,15 @@ void gemm_tiled_kernel(const std::conditional_t<EPI, TiledEpilogueParams, TiledP
                     }
                 }
             }
-            stores_in_flight = (NT == 2 && p.swiglu) ? STORES_ACT : to_bf16 ? STORES_BF16 : STORES_F32;
+            stores_in_flight = (NT == 2 && (ACT_ONLY || p.swiglu)) ? STORES_ACT : to_bf16 ? STORES_BF16 : STORES_F32;
         } else if (n0 + BN <= p.N && p.vector_stores) {      // ragged last row tile: the same through the patch, rows clamped
             const int last_slot = cur == 0 ? RING - 1 : cur - 1;
             float *patch = reinterpret_cast<float *>(smem + last_slot * STAGE_BYTES + wave * REGION_BYTES);
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
             const bool to_bf16 = (part == nullptr) && p.y_bf16;
             const int wm_u = wave_u / WN, wn_u = wave_u % WN;
-            const int row0 = m0 + wm_u * MT * 32, last = p.M - 1 - row0;      // the wavefront's rows, the last one that exists
-            if (NT == 2 && p.swiglu) {
+            const int row0 = m0 + wm_u * MT * 32, last = rows_end - 1 - row0;      // the wavefront's rows, the last one that exists
+            if (NT == 2 && (ACT_ONLY || p.swiglu)) {
 #pragma unroll
                 for (int a = 0; a < MT; ++a) {
                     if (last < 32 * a) continue;
@@ -549,15 +588,15 @@ void gemm_tiled_kernel(const std::conditional_t<EPI, TiledEpilogueParams, TiledP
                 float *dst = (part ? part : reinterpret_cast<float *>(p.Y)) + (int64_t)row0 * ld + n0 + wn_u * WCOLS;
                 store_ragged_f32(acc, patch, dst, ld, last, lane, p.stream_stores);
             }
-            stores_in_flight = last < (MT - 1) * 32 ? -1 : (NT == 2 && p.swiglu) ? STORES_ACT : to_bf16 ? STORES_BF16 : STORES_F32;
-        } else if (NT == 2 && p.swiglu) {                    // rows that cannot be stored 16 bytes at a time
+            stores_in_flight = last < (MT - 1) * 32 ? -1 : (NT == 2 && (ACT_ONLY || p.swiglu)) ? STORES_ACT : to_bf16 ? STORES_BF16 : STORES_F32;
+        } else if (NT == 2 && (ACT_ONLY || p.swiglu)) {                    // rows that cannot be stored 16 bytes at a time
             const int col = n0 / 2 + wn * 32 + li;
 #pragma unroll
             for (int a = 0; a < MT; ++a) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int row = m0 + (wm * MT + a) * 32 + 8 * (r >> 2) + 4 * lg + (r & 3);
-                    if (row >= p.M) continue;
+                    if (row >= rows_end) continue;
                     const float v = silu_mul(through_16_bits<F16>(acc.t[a][0][r]), through_16_bits<F16>(acc.t[a][NT - 1][r]));
                     reinterpret_cast<uint16_t *>(p.Y)[(int64_t)row * p.ldy + col] = (uint16_t)f32_to_16_bits<F16>(v);
                 }
@@ -573,7 +612,7 @@ void gemm_tiled_kernel(const std::conditional_t<EPI, TiledEpilogueParams, TiledP
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int row = m0 + (wm * MT + a) * 32 + 8 * (r >> 2) + 4 * lg + (r & 3);
-                        if (row >= p.M) continue;
+                        if (row >= rows_end) continue;
                         const float v = acc.t[a][b][r];
                         if (part) part[(int64_t)row * p.N + col] = v;
                         if (p.Y) {
@@ -597,7 +636,7 @@ static int levels_for(int ns_per_shard) {
     return l;
 }
 
-#ifndef TBIK_EPILOGUE_UNIT
+#if !defined(TBIK_EPILOGUE_UNIT) && !defined(TBIK_GROUPED_UNIT)
 bool gemm_tiled_supports(const GemmArgs &a, int variant) {
     if (variant != VARIANT_T128 && variant != VARIANT_T32 && variant != VARIANT_T64 && variant != VARIANT_T96) return false;
     if (a.N % 8 != 0 || a.superleaf % BK != 0) return false;
@@ -621,10 +660,10 @@ static int compute_units() {
     return cus;
 }
 
-template <int WM, int WN, int MT, int NT, int RING, bool F16, bool EPI>
-static hipError_t launch_shape(const GemmArgs &a, hipStream_t s) {
+template <int WM, int WN, int MT, int NT, int RING, bool F16, bool EPI, bool GROUP = false>
+static hipError_t launch_shape(const std::conditional_t<GROUP, GroupedArgs, GemmArgs> &a, hipStream_t s) {
     constexpr int BM = 32 * MT * WM, BN = 32 * NT * WN;
-    std::conditional_t<EPI, TiledEpilogueParams, TiledParams> p;
+    TiledParamsOf<EPI, GROUP> p;
     if constexpr (EPI) p.epilogue = *a.epilogue;
     p.X = a.X; p.W = a.W; p.partials = a.partials; p.Y = (a.P == 1) ? a.Y : nullptr;
     p.ldx = a.ldx; p.ldw = a.ldw; p.ldy = a.ldy;
@@ -635,7 +674,12 @@ static hipError_t launch_shape(const GemmArgs &a, hipStream_t s) {
     p.ns_per_shard = a.ns / a.P;
     p.k_per_shard = (int64_t)a.K / a.P;
     p.tiles_n = (a.N + BN - 1) / BN;
-    const int64_t tiles = (int64_t)p.tiles_n * ((a.M + BM - 1) / BM);
+    int64_t tiles = (int64_t)p.tiles_n * ((a.M + BM - 1) / BM);
+    if constexpr (GROUP) {
+        p.offsets = a.offsets; p.rows = a.rows; p.tokens = a.tokens;
+        p.groups = a.groups; p.shards = a.P; p.weight_stride = a.weight_stride;
+        tiles = (int64_t)p.tiles_n * grouped_tiles(a, BM);               // an upper bound
+    }
     if (tiles * a.P > 0x7fffffff) return hipErrorInvalidValue;
     p.tiles = (int)tiles;
     p.work = (int)(tiles * a.P);
@@ -662,7 +706,7 @@ static hipError_t launch_shape(const GemmArgs &a, hipStream_t s) {
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 32) dev = 32;   // 32: not remembered, set every time
 #define TBIK_LAUNCH(L)                                                                                   \
     case L: {                                                                                            \
-        auto k = gemm_tiled_kernel<L, WM, WN, MT, NT, RING, F16, EPI>;                                       \
+        auto k = gemm_tiled_kernel<L, WM, WN, MT, NT, RING, F16, EPI, GROUP>;                                      \
         static std::atomic<unsigned> lds_allowed{0};   /* bit d: the attribute is set on device d */     \
         if (dev >= 32 || !((lds_allowed.load(std::memory_order_relaxed) >> dev) & 1u)) {                 \
             hipError_t e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds); \
@@ -684,6 +728,29 @@ static hipError_t launch_shape(const GemmArgs &a, hipStream_t s) {
     return hipGetLastError();
 }
 
+#ifdef TBIK_GROUPED_UNIT
+bool gemm_grouped_tiled_supports(const GroupedArgs &a, int variant) {
+    if (variant != VARIANT_T128 && variant != VARIANT_T64) return false;
+    if (a.N % 8 != 0 || a.superleaf % BK != 0 || levels_for(a.ns / a.P) > 4) return false;
+    if (a.ldx >= (1 << 22) || a.ldw >= (1 << 22)) return false;
+    // Gathered rows are 32-bit offsets (unsigned) from the first row of X.
+    if (a.rows && (int64_t)a.tokens * a.ldx * 2 > 0xffffffffll - 8192) return false;
+    if (a.swiglu && (a.P != 1 || a.partials || a.N % 128 != 0)) return false;
+    return ((int64_t)(a.N + BN_TILE - 1) / BN_TILE) * grouped_tiles(a, 64) * a.P <= 0x7fffffff;
+}
+template <bool F16>
+static hipError_t launch_grouped_variant(const GroupedArgs &a, int variant, hipStream_t s) {
+    if (variant == VARIANT_T128) return launch_shape<2, 2, 2, 2, 5, F16, false, true>(a, s);
+    // Gate and up of a channel in one lane ask for two column blocks in a wavefront's tile.
+    if (a.swiglu) return launch_shape<2, 2, 1, 2, 6, F16, false, true>(a, s);
+    return launch_shape<1, 4, 2, 1, 6, F16, false, true>(a, s);
+}
+hipError_t launch_gemm_grouped_tiled(const GroupedArgs &a, int variant, hipStream_t s) {
+    if (a.M <= 0 || a.N <= 0) return hipSuccess;
+    if (!gemm_grouped_tiled_supports(a, variant)) return hipErrorInvalidValue;
+    return a.x_dtype == TBIK_F16 ? launch_grouped_variant<true>(a, variant, s) : launch_grouped_variant<false>(a, variant, s);
+}
+#else
 template <bool F16, bool EPI>
 static hipError_t launch_variant(const GemmArgs &a, int variant, hipStream_t s) {
     // 128 x 128, wave tile 64 x 64, 5 x 32 KiB stage slots = all of LDS
@@ -708,6 +775,7 @@ hipError_t launch_gemm_tiled(const GemmArgs &a, int variant, hipStream_t s) {
     if (a.epilogue) return launch_gemm_tiled_epilogue(a, variant, s);
     return a.x_dtype == TBIK_F16 ? launch_variant<true, false>(a, variant, s) : launch_variant<false, false>(a, variant, s);
 }
+#endif
 #endif
 
 }  // namespace tbik

@@ -1251,6 +1251,19 @@ int tbik_route_topk(const void *logits, int64_t ldl, tbik_dtype dtype, int T, in
     return e == hipSuccess ? TBIK_OK : hip_fail(e);
 }
 
+// The kernel of a grouped call by the rows that a group has in the mean (the device knows each one's): slices up to 32 rows, else tiles.
+static int grouped_kernel(const GroupedArgs &a) {
+    const bool slices = gemm_grouped_slice_supports(a), tiles64 = gemm_grouped_tiled_supports(a, VARIANT_T64), tiles128 = gemm_grouped_tiled_supports(a, VARIANT_T128);
+    const int64_t mean = a.M / a.groups;
+    int wanted = mean <= 32 ? VARIANT_T32 : mean <= 96 ? VARIANT_T64 : VARIANT_T128;
+    const int forced = g_forced_variant.load();
+    if (forced == VARIANT_REFERENCE) return VARIANT_REFERENCE;
+    if (forced == VARIANT_T32 || forced == VARIANT_T64 || forced == VARIANT_T128) wanted = forced;
+    if (wanted == VARIANT_T32 && slices) return VARIANT_T32;
+    if (wanted != VARIANT_T128 && tiles64) return VARIANT_T64;
+    return tiles128 ? VARIANT_T128 : slices ? VARIANT_T32 : VARIANT_REFERENCE;
+}
+
 // Y: [R, ldy] of y_dtype, or partials: dense [P, R, N]; swiglu: N = 2 I columns of the weights, Y is [R, I].
 static int gemm_grouped(tbik_dtype x_dtype, const void *X, int64_t ldx, int tokens, const int32_t *rows, const void *W, int64_t ldw, int64_t stride, int groups,
                         const int32_t *offsets, void *Y, int64_t ldy, tbik_dtype y_dtype, float *partials, bool swiglu,
@@ -1275,7 +1288,14 @@ static int gemm_grouped(tbik_dtype x_dtype, const void *X, int64_t ldx, int toke
     a.tokens = tokens;
     a.groups = groups;
     a.weight_stride = stride;
-    hipError_t e = launch_gemm_grouped_reference(a, (hipStream_t)hip_stream);
+    hipStream_t s = (hipStream_t)hip_stream;
+    hipError_t e;
+    switch (grouped_kernel(a)) {
+        case VARIANT_T32: e = launch_gemm_grouped_slice(a, s); break;
+        case VARIANT_T64: e = launch_gemm_grouped_tiled(a, VARIANT_T64, s); break;
+        case VARIANT_T128: e = launch_gemm_grouped_tiled(a, VARIANT_T128, s); break;
+        default: e = launch_gemm_grouped_reference(a, s);
+    }
     return e == hipSuccess ? TBIK_OK : hip_fail(e);
 }
 

@@ -137,11 +137,13 @@ struct GroupedArgs : GemmArgs {
     int groups;
     int64_t weight_stride;                 // elements from one weight to the next
 };
+// The most row tiles of `height` rows that any division of the rows into groups has.
+inline int64_t grouped_tiles(const GroupedArgs &a, int height) { return (int64_t)a.M / height + (a.groups < a.M ? a.groups : a.M); }
 hipError_t launch_gemm_grouped_reference(const GroupedArgs &a, hipStream_t s);
-// Workgroups that hold all of K, `waves` wavefronts beside each other along it.
+// Groups of few rows: workgroups that hold a slice of columns and all of K.
 bool gemm_grouped_slice_supports(const GroupedArgs &a);
 hipError_t launch_gemm_grouped_slice(const GroupedArgs &a, hipStream_t s);
-// The tiled kernels; variant: VARIANT_T128, VARIANT_T64 or VARIANT_T32.
+// The tiled kernels; variant: VARIANT_T128 or VARIANT_T64.
 bool gemm_grouped_tiled_supports(const GroupedArgs &a, int variant);
 hipError_t launch_gemm_grouped_tiled(const GroupedArgs &a, int variant, hipStream_t s);
 
