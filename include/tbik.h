@@ -663,11 +663,14 @@ int tbik_combine_experts(const void *Y, int64_t ldy, tbik_dtype y_dtype, int P, 
  *   scales  device, x_dtype, [N, lds], lds >= K / group          zeros   device, bytes (the low four bits count), [N, ldz], or NULL
  *   group   a multiple of 32 that divides leaf * k_first; K / (leaf * k_first) / P <= 128
  *   Y       device, y_dtype (TBIK_F32 or x_dtype), [M, ldy], aligned to its type          partials   device, fp32, dense [P, M, N], 16-byte aligned
- *   No workspace.
+ *   workspace  tbik_gemm_w4_workspace_bytes(M, N, K, leaf, k_first) bytes, 256-byte aligned, are room for the quickest way to cut the work; less (or NULL) gives
+ *           the same bits, more slowly
  * Errors: NULL, SHAPE, SHARDS, DTYPE, UNSUPPORTED, ALIGN, HIP.
  */
+size_t tbik_gemm_w4_workspace_bytes(int M, int N, int K, int leaf, int k_first);
 int tbik_gemm_w4(const void *X, int64_t ldx, const void *Wq, int64_t ldwq, const void *scales, int64_t lds, const void *zeros, int64_t ldz, int group,
-                 void *Y, int64_t ldy, tbik_dtype y_dtype, tbik_dtype x_dtype, int M, int N, int K, int leaf, int k_first, void *hip_stream);
+                 void *Y, int64_t ldy, tbik_dtype y_dtype, tbik_dtype x_dtype, int M, int N, int K, int leaf, int k_first,
+                 void *workspace, size_t workspace_bytes, void *hip_stream);
 int tbik_gemm_shard_partials_w4(const void *X, int64_t ldx, const void *Wq, int64_t ldwq, const void *scales, int64_t lds, const void *zeros, int64_t ldz,
                                 int group, float *partials, tbik_dtype x_dtype, int M, int N, int K, int leaf, int k_first, int P, void *hip_stream);
 

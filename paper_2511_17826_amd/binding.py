@@ -153,7 +153,8 @@ SIGNATURES = {
     "tbik_gemm_grouped_shard_partials": (C.c_int, _GROUPED + [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p]),
     "tbik_combine_experts": (C.c_int, [C.c_void_p, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
                                        C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p]),
-    "tbik_gemm_w4": (C.c_int, _W4 + [C.c_void_p, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p]),
+    "tbik_gemm_w4": (C.c_int, _W4 + [C.c_void_p, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "tbik_gemm_w4_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int, C.c_int, C.c_int]),
     "tbik_gemm_shard_partials_w4": (C.c_int, _W4 + [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p]),
     "tbik_rmsnorm_residual_rmsnorm": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_void_p, C.c_int64, C.c_int,
                                                 C.c_void_p, C.c_float, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_void_p]),
@@ -205,6 +206,14 @@ _NATIVE = {name: (i, *spec) for i, (name, *spec) in enumerate([
     ("tbik_combine_residual_rmsnorm_mxfp8", 19, None, torch.uint8),
     ("tbik_silu_mul_fp8", 20, None, torch.uint8),
     ("tbik_silu_mul_mxfp8", 21, None, torch.uint8),
+    ("tbik_route_topk", 22, "tbik_route_topk_workspace_bytes", torch.float32),
+    ("tbik_gemm_grouped", 23, None, torch.bfloat16),
+    ("tbik_gemm_grouped_swiglu", 24, None, torch.bfloat16),
+    ("tbik_gemm_grouped_shard_partials", 25, None, torch.bfloat16),
+    ("tbik_combine_experts", 26, None, torch.float32),
+    ("tbik_gemm_w4", 27, "tbik_gemm_w4_workspace_bytes", torch.bfloat16),
+    ("tbik_gemm_shard_partials_w4", 28, None, torch.bfloat16),
+    ("tbik_rmsnorm_residual_rmsnorm", 29, None, torch.bfloat16),
 ])}
 _NUMBER = {name: spec[0] for name, spec in _NATIVE.items()}
 
@@ -212,6 +221,7 @@ _NUMBER = {name: spec[0] for name, spec in _NATIVE.items()}
 class _NotLoaded:
     """Stands for the native half until the library is loaded, and where it cannot be loaded: no call is a common one."""
     product = rmsnorm = combine = row_reduce = attention = epilogue = eight_bits = staticmethod(lambda *a: None)
+    route = grouped = experts_sum = w4 = join = product
 
 
 _native = _NotLoaded
@@ -1255,6 +1265,10 @@ def tbik_route_topk(logits: torch.Tensor, k: int, renormalize: bool = True, work
     (float32, bfloat16 or float16): each token's k largest, falling, the lower expert first among equals; their softmax, over the chosen
     ones or (renormalize=False) over all; and the order by expert that tbik_gemm_grouped takes (offsets, rows) and
     tbik_combine_experts undoes (slots)."""
+    if workspace is None:
+        y = _native.route(_NUMBER["tbik_route_topk"], logits, k, renormalize)
+        if y is not None:
+            return _done(y, "tbik_route_topk")
     ldl = _rowmajor(logits, "logits")
     T, E = logits.shape
     L = lib()
@@ -1294,6 +1308,10 @@ def tbik_gemm_grouped(X: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, l
     """Y[i] = X[rows[i]] @ W[e] for offsets[e] <= i < offsets[e + 1], in the tree order: the bits of tbik_gemm on that row and weight.  W
     [groups, K, N]; offsets int32 [groups + 1] and rows int32 [R] on the GPU (tbik_route_topk's); without rows Y[i] = X[i] @ W[e].  Y is
     float32 or (default) X's type; its rows outside every group are left as they were (undefined in a new tensor)."""
+    if out is None:
+        y = _native.grouped(_NUMBER["tbik_gemm_grouped"], X, W, offsets, rows, leaf, k_first, out_dtype, 1)
+        if y is not None:
+            return _done(y, "tbik_gemm_grouped")
     operands, R, N, K = _grouped_operands(X, W, offsets, rows)
     if out is None:
         out = torch.empty((R, N), dtype=out_dtype or X.dtype, device=X.device)
@@ -1308,6 +1326,10 @@ def tbik_gemm_grouped(X: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, l
 def tbik_gemm_grouped_swiglu(X: torch.Tensor, W_gu: torch.Tensor, offsets: torch.Tensor, leaf: int, k_first: int = 1, rows: torch.Tensor | None = None,
                              out: torch.Tensor | None = None) -> torch.Tensor:
     """act[i] = tbik_gemm_swiglu of X[rows[i]] and W_gu[e], bit for bit; W_gu [groups, K, 2 I], gate columns first.  Otherwise as tbik_gemm_grouped."""
+    if out is None:
+        y = _native.grouped(_NUMBER["tbik_gemm_grouped_swiglu"], X, W_gu, offsets, rows, leaf, k_first, None, 1)
+        if y is not None:
+            return _done(y, "tbik_gemm_grouped_swiglu")
     operands, R, N, K = _grouped_operands(X, W_gu, offsets, rows)
     if N % 2 != 0:
         raise ValueError("W_gu holds gate and up columns: an even number, got %d" % N)
@@ -1324,6 +1346,10 @@ def tbik_gemm_grouped_swiglu(X: torch.Tensor, W_gu: torch.Tensor, offsets: torch
 def tbik_gemm_grouped_shard_partials(X: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, leaf: int, k_first: int, P: int,
                                      rows: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """partials [P, R, N] (float32): tbik_gemm_shard_partials of each row and its group's weight."""
+    if out is None:
+        y = _native.grouped(_NUMBER["tbik_gemm_grouped_shard_partials"], X, W, offsets, rows, leaf, k_first, None, P)
+        if y is not None:
+            return _done(y, "tbik_gemm_grouped_shard_partials")
     operands, R, N, K = _grouped_operands(X, W, offsets, rows)
     if out is None:
         out = torch.empty((max(P, 0), R, N), dtype=torch.float32, device=X.device)
@@ -1338,6 +1364,10 @@ def tbik_combine_experts(Y: torch.Tensor, slots: torch.Tensor, weights: torch.Te
                          out: torch.Tensor | None = None) -> torch.Tensor:
     """out[t] = sum_j weights[t, j] * Y[slots[t, j]] (+ residual[t]), j ascending in fp32, rounded once.  Y [R, H] is bfloat16 or float16, or float32
     [R, H] or [P, R, H], the partial sums of P shards.  A slot that is no row of Y adds nothing.  The output's type: residual's, else Y's."""
+    if out is None:
+        y = _native.experts_sum(_NUMBER["tbik_combine_experts"], Y, slots, weights, residual, out_dtype)
+        if y is not None:
+            return _done(y, "tbik_combine_experts")
     if Y.dim() == 3:
         if Y.dtype != torch.float32:
             raise TypeError("shards' partial sums are float32, got %s" % Y.dtype)
@@ -1387,23 +1417,34 @@ def _w4_operands(X, Wq, scales, zeros):
 
 
 def tbik_gemm_w4(X: torch.Tensor, Wq: torch.Tensor, scales: torch.Tensor, leaf: int, k_first: int = 1, zeros: torch.Tensor | None = None, out_dtype=None,
-                 out: torch.Tensor | None = None) -> torch.Tensor:
+                 out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
     """Y = X @ W in the tree order, W[k, n] = scales[n, k / group] * (q[n, k] - zeros[n, k / group]) (8 without zeros).  Wq uint8 [N, K / 2]: two
     4-bit elements a byte, the even k in the low half; scales [N, K / group] of X's type; zeros uint8 likewise.  Y is float32 or (default) X's type."""
+    if out is None and workspace is None:
+        y = _native.w4(_NUMBER["tbik_gemm_w4"], X, Wq, scales, zeros, leaf, k_first, out_dtype, 1)
+        if y is not None:
+            return _done(y, "tbik_gemm_w4")
     operands, M, N, K = _w4_operands(X, Wq, scales, zeros)
     if out is None:
         out = torch.empty((M, N), dtype=out_dtype or X.dtype, device=X.device)
     ldy = _rowmajor(out, "out")
     if out.shape != (M, N):
         raise ValueError("out must have the shape %s" % ((M, N),))
-    _on_current_device(X, Wq, scales, zeros, out)
-    _check(lib().tbik_gemm_w4(*operands, out.data_ptr(), ldy, _dt(out), _dt(X), M, N, K, leaf, k_first, _stream()), "tbik_gemm_w4")
+    _on_current_device(X, Wq, scales, zeros, out, workspace)
+    if workspace is None:
+        workspace = _scratch(int(lib().tbik_gemm_w4_workspace_bytes(M, N, K, leaf, k_first)), X.device)
+    room, room_bytes = _room(workspace)
+    _check(lib().tbik_gemm_w4(*operands, out.data_ptr(), ldy, _dt(out), _dt(X), M, N, K, leaf, k_first, room, room_bytes, _stream()), "tbik_gemm_w4")
     return out
 
 
 def tbik_gemm_shard_partials_w4(X: torch.Tensor, Wq: torch.Tensor, scales: torch.Tensor, leaf: int, k_first: int, P: int, zeros: torch.Tensor | None = None,
                                 out: torch.Tensor | None = None) -> torch.Tensor:
     """partials [P, M, N] (float32) of the same product, for tbik_tree_combine."""
+    if out is None:
+        y = _native.w4(_NUMBER["tbik_gemm_shard_partials_w4"], X, Wq, scales, zeros, leaf, k_first, None, P)
+        if y is not None:
+            return _done(y, "tbik_gemm_shard_partials_w4")
     operands, M, N, K = _w4_operands(X, Wq, scales, zeros)
     if out is None:
         out = torch.empty((max(P, 0), M, N), dtype=torch.float32, device=X.device)
@@ -1420,6 +1461,10 @@ def tbik_rmsnorm_residual_rmsnorm(y: torch.Tensor, residual: torch.Tensor, post_
     """(hidden, normed): hidden = residual * residual_scale + gate * RMSNorm(y; post_weight), rounded to residual's type; normed = RMSNorm(hidden;
     next_weight).  y [M, H] of that type, or float32 [P, M, H], shards' partial sums, which are combined and rounded first.  gate: [H] or [1, H],
     [M, 1] or [M, H].  Without post_weight y is taken as it is; without next_weight normed is None.  `hidden` may be residual or y."""
+    if hidden is None and normed is None:
+        out = _native.join(_NUMBER["tbik_rmsnorm_residual_rmsnorm"], y, residual, post_weight, next_weight, eps, residual_scale, gate)
+        if out is not None:
+            return _done(out, "tbik_rmsnorm_residual_rmsnorm")
     ldr = _rowmajor(residual, "residual")
     M, H = residual.shape
     dtype = residual.dtype

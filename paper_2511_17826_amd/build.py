@@ -105,6 +105,8 @@ def build(save_temps: bool = True, jobs: int = 8, defines=(), lib_path: str = LI
         check_generated_code(os.path.join(BUILD, "gemm_tiled_epilogue-hip-amdgcn-amd-amdhsa-gfx950.s"), "gemm_tiled_kernel")
         check_generated_code(os.path.join(BUILD, "gemm_tiled_grouped-hip-amdgcn-amd-amdhsa-gfx950.s"), "gemm_tiled_kernel")
         check_generated_code(os.path.join(BUILD, "gemm_grouped_slice-hip-amdgcn-amd-amdhsa-gfx950.s"), "gemm_grouped_slice_kernel")
+        for kernel in ("gemm_w4_slice_kernel", "gemm_w4_tiled_kernel"):
+            check_generated_code(os.path.join(BUILD, "gemm_w4-hip-amdgcn-amd-amdhsa-gfx950.s"), kernel)
         for unit in ("gemm_fp8_epilogue", "gemm_mxfp8_epilogue"):
             check_generated_code(os.path.join(BUILD, unit + "-hip-amdgcn-amd-amdhsa-gfx950.s"), "gemm_fp8_tiled_kernel")
         check_generated_code(os.path.join(BUILD, "attention-hip-amdgcn-amd-amdhsa-gfx950.s"), "attention_")

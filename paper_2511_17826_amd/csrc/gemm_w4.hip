@@ -1,21 +1,28 @@
-// Tree-Based MatMul of 16-bit rows on a 4-bit weight with a scale per group of consecutive k and channel (decode batches).
+// Tree-Based MatMul of 16-bit rows on a 4-bit weight with a scale per group of consecutive k and channel.
 //
 //   Y[m,n] = T over superleaves of  sum over groups g of the superleaf, ascending:  acc = fma(scale[n,g], S_g, acc), acc from +0
 //   S_g    = sum over k of the group of  x[m,k] (q[n,k] - zero[n,g])     chained matrix instructions from +0
 // q - zero is a whole number of -15 .. 15 and exact in either 16-bit format, so the weight is never rounded: the scale multiplies a
-// group's fp32 sum, once per group, row and channel.
+// group's fp32 sum, once per group, row and channel.  An element becomes a float with one conversion of the hardware (v_cvt_off_f32_i4, the
+// 4-bit two's complement number over 16, which the scale takes back exactly) and two of them a pair of 16-bit values with one more.
 //
-// What bounds it is the weight's bytes (half a byte an element) and, of more rows, the batch's, which every workgroup reads.  A workgroup
-// takes 32 channels, up to 32 rows and all of a shard's K in one launch: its wavefronts take consecutive superleaves each, whole and in order
-// (Sec. 4.2, App. D.1), and the upper levels of the tree run over their sums in LDS (App. C).  An instruction multiplies 16 k of 32
-// channels; which 16 of a unit of 64 (or 32, for groups that no 64 divides) it takes is chosen so that a lane's elements of the
-// whole unit are 16 (8) consecutive bytes: half a lane's 32 channels at the unit's first half, the other at its second.  Operands go
-// from memory to registers, DEPTH units ahead; an element becomes a float with one conversion of the hardware (v_cvt_off_f32_i4, the 4-bit two's
-// complement number over 16, which the scale takes back exactly) and two of them a pair of 16-bit values with one more.
+// An instruction multiplies 16 k of 32 channels; which 16 of a unit of 64 (or 32, for groups that no 64 divides) it takes is chosen so that a
+// lane's elements of the whole unit are 16 (8) consecutive bytes: half of the lanes take the unit's first half, the others its second.  The three
+// kernels below share that map, the chains and the tree, so they give the same bits:
+//   slices   up to 16 rows in one launch: a workgroup takes 32 channels and all of a shard's K, its eight wavefronts consecutive superleaves each (whole and in
+//            order: Sec. 4.2, App. D.1); each streams its part of the weight, of the rows and of the scales through a ring of stages in
+//            LDS of its own (direct global->LDS loads, no barrier until the sums are there), and the upper levels of the tree run over their sums (App. C)
+//   tiles    more rows: a workgroup takes 128 channels and 32, 64 or 128 rows, which its four wavefronts share; few tiles split K (fp32 planes, combined by
+//            the same tree), which the rows' traffic decides: a slice would read all of X for every 32 channels
+//   general  any legal shape, operands straight from memory to registers
+#include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "tbik_device.hpp"
 #include "tbik_internal.hpp"
+#include "tile_store.hpp"
+#include "tree_walk.hpp"
 
 namespace tbik {
 
@@ -33,6 +40,7 @@ struct W4Params {
     int y_f32;
     int group, superleaf;
     int leaves_per_wave, active_waves, leaves_per_shard;
+    int vector_stores;
 };
 
 typedef uint32_t w4_u32x4 __attribute__((ext_vector_type(4)));
@@ -64,8 +72,354 @@ __device__ __forceinline__ bf16x8 widened_levels(uint32_t w, float zero) {
 template <bool F16>
 __device__ __forceinline__ float widened_16(uint16_t h) { return F16 ? (float)__builtin_bit_cast(_Float16, h) : bf16_bits_to_f32(h); }
 
-constexpr int W4_WAVES = 8;
 
+
+constexpr int W4_WAVES = 8;                // of a slice, and of the general kernel's workgroup
+
+// ---- stages in LDS (slices and tiles) ----
+// A stage is 64 k.  Of one wavefront it holds rows of X (128 bytes; chunk c of 16 bytes of row r at c ^ (r / 2 % 8), so that the rows of a read meet
+// different banks), the 32 bytes of each of 32 channels in the order of the lanes, and a dword per lane with the scale (and one with
+// the zero point) of the group that the lane's unit belongs to: lanes 0 .. 31 the first unit of 32 k, lanes 32 .. 63 the second.
+constexpr int W4_STAGE_K = 64;
+
+template <int N>
+__device__ __forceinline__ void w4_wait_loads() {
+    static_assert(N >= 0 && N < 64, "vmcnt range");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void w4_wait_loads_and_barrier() {
+    static_assert(N >= 0 && N < 64, "vmcnt range");
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// The group of one unit after another.
+struct GroupWalk {
+    int g, left;
+    int units;                             // of a group
+    __device__ __forceinline__ explicit GroupWalk(int units_per_group) : g(0), left(units_per_group), units(units_per_group) {}
+    __device__ __forceinline__ bool next() {       // true: the unit was the group's last
+        if (--left != 0) return false;
+        left = units;
+        ++g;
+        return true;
+    }
+};
+
+// One wavefront's stream of weight, scales and zero points: 32 channels from n0 on, k from k0 on.
+template <int UNIT, bool ZEROS>
+struct W4Stream {
+    const char *w_ptr, *s_ptr, *z_ptr;     // w_ptr: less a bias that the instruction offset takes back
+    unsigned w_off, s_off, z_off;          // of the lane; s_off and z_off count from an aligned dword
+    GroupWalk walk;                        // of the stream's next unit
+    static constexpr int LOADS = 2 + (ZEROS ? 1 : 0);
+    static constexpr int BYTES = 1024 + 256 * (1 + (ZEROS ? 1 : 0));
+
+    __device__ __forceinline__ W4Stream(const W4Params &p, int n0, int64_t k0, int lane) : walk(p.group / UNIT) {
+        const uint8_t *w = p.W + n0 * p.ldw + k0 / 2;
+        const uint16_t *sc = p.scales + n0 * p.lds + k0 / p.group;
+        w_ptr = uniform_pointer(reinterpret_cast<const char *>(w));
+        w_off = (unsigned)(min(lane >> 1, p.N - 1 - n0) * (int)p.ldw + (lane & 1) * 16);
+        const int channel = min(lane & 31, p.N - 1 - n0);
+        const unsigned s_low = (unsigned)(reinterpret_cast<uintptr_t>(sc) & 3);
+        s_ptr = uniform_pointer(reinterpret_cast<const char *>(sc) - s_low);
+        s_off = s_low + (unsigned)(channel * (int)p.lds) * 2u;
+        z_ptr = nullptr;
+        z_off = 0;
+        if constexpr (ZEROS) {
+            const uint8_t *z = p.zeros + n0 * p.ldz + k0 / p.group;
+            const unsigned z_low = (unsigned)(reinterpret_cast<uintptr_t>(z) & 3);
+            z_ptr = uniform_pointer(reinterpret_cast<const char *>(z) - z_low);
+            z_off = z_low + (unsigned)(channel * (int)p.ldz);
+        }
+    }
+    // The next stage's loads to LDS address `at` (uniform): weight, scales, zero points.  A scale's dword holds its neighbour too.
+    // `more`: there is a stage behind it; else the next issue loads it again.
+    __device__ __forceinline__ void issue(unsigned at, int lane, bool more) {
+        load_16B_per_lane_to_lds<0, true>(w_ptr, w_off, at);
+        GroupWalk behind = walk;
+        int g = behind.g;
+        behind.next();
+        if constexpr (UNIT == 32) {
+            if (lane >= 32) g = behind.g;
+            behind.next();
+        }
+        load_4B_per_lane_to_lds<0, true>(s_ptr, (s_off + 2u * g) & ~3u, at + 1024);
+        if constexpr (ZEROS) load_4B_per_lane_to_lds<256, false>(z_ptr - 256, (z_off + g) & ~3u, at + 1024);
+        if (more) {
+            walk = behind;
+            w_ptr += W4_STAGE_K / 2;
+        }
+    }
+    // From the stage at `st` in LDS, for unit u of it, which is group g's.
+    __device__ __forceinline__ float zero(const unsigned char *st, int u, int g, int li) const {
+        const unsigned z = *reinterpret_cast<const unsigned *>(st + 1280 + (u * 32 + li) * 4);
+        return (float)((int)((z >> (8u * ((z_off + g) & 3u))) & 15u) - 8) * 0.0625f;
+    }
+    template <bool F16>
+    __device__ __forceinline__ float scale(const unsigned char *st, int u, int g, int li) const {
+        const unsigned s = *reinterpret_cast<const unsigned *>(st + 1024 + (u * 32 + li) * 4);
+        return widened_16<F16>((uint16_t)(s >> (8u * ((s_off + 2u * g) & 2u)))) * 16.0f;
+    }
+};
+
+// Multiplies a stage: rows x_rows[a] (LDS addresses of the lane's row of X in the stage) times the stage's weight at st.  sum: the running group's; a group
+// that ends goes through its scale into acc.
+template <int UNIT, bool F16, bool ZEROS, int MT>
+__device__ __forceinline__ void multiply_stage(const W4Stream<UNIT, ZEROS> &stream, const unsigned char *st, const unsigned char *const (&x_rows)[MT], int x_sw,
+                                               GroupWalk &walk, Acc<MT, 1> &sum, Acc<MT, 1> &acc, int li, int lg) {
+    w4_u32x4 words;
+    if constexpr (UNIT == 64) {
+        words = *reinterpret_cast<const w4_u32x4 *>(st + (li * 2 + lg) * 16);
+    } else {
+        const w4_u32x2 a = *reinterpret_cast<const w4_u32x2 *>(st + li * 32 + lg * 8), b = *reinterpret_cast<const w4_u32x2 *>(st + li * 32 + 16 + lg * 8);
+        words = w4_u32x4{a[0], a[1], b[0], b[1]};
+    }
+    bf16x8 x[4][MT];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int chunk = UNIT == 64 ? lg * 4 + i : (i >> 1) * 4 + lg * 2 + (i & 1);
+#pragma unroll
+        for (int a = 0; a < MT; ++a) x[i][a] = *reinterpret_cast<const bf16x8 *>(x_rows[a] + ((chunk ^ x_sw) << 4));
+    }
+    constexpr int UNITS = W4_STAGE_K / UNIT;
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+        float zero = 0.0f;
+        if constexpr (ZEROS) zero = stream.zero(st, u, walk.g, li);
+        const float scale = stream.template scale<F16>(st, u, walk.g, li);
+#pragma unroll
+        for (int i = u * (4 / UNITS); i < (u + 1) * (4 / UNITS); ++i) {
+            const bf16x8 w = widened_levels<F16, ZEROS>(words[i], zero);
+#pragma unroll
+            for (int a = 0; a < MT; ++a) sum.t[a][0] = mfma_32x32x16<F16>(x[i][a], w, sum.t[a][0]);
+        }
+        if (walk.next()) {
+#pragma unroll
+            for (int a = 0; a < MT; ++a)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    acc.t[a][0][r] = __builtin_fmaf(scale, sum.t[a][0][r], acc.t[a][0][r]);
+                    sum.t[a][0][r] = 0.0f;
+                }
+        }
+    }
+}
+
+template <int MT>
+__device__ __forceinline__ void clear(Acc<MT, 1> &acc) {
+#pragma unroll
+    for (int a = 0; a < MT; ++a)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc.t[a][0][r] = 0.0f;
+}
+
+// The wavefronts' sums in LDS (32 x 32 each), four wavefronts or eight: T over them for element `at`.
+__device__ __forceinline__ float tree_of_waves(const float *red, int active, int at) {
+    float v[W4_WAVES];
+#pragma unroll
+    for (int w = 0; w < W4_WAVES; ++w) v[w] = red[w < active ? w * 1024 + at : at];
+#pragma unroll
+    for (int s = 1; s < W4_WAVES; s *= 2)
+#pragma unroll
+        for (int r = 0; r < W4_WAVES; r += 2 * s)
+            if (r + s < active) v[r] = v[r] + v[r + s];
+    return v[0];
+}
+template <bool F16>
+__device__ __forceinline__ void store_sum(const W4Params &p, int shard, int row, int col, float v) {
+    if (p.partials) p.partials[((int64_t)shard * p.M + row) * p.N + col] = v;
+    else if (p.y_f32) reinterpret_cast<float *>(p.Y)[(int64_t)row * p.ldy + col] = v;
+    else reinterpret_cast<uint16_t *>(p.Y)[(int64_t)row * p.ldy + col] = (uint16_t)f32_to_16_bits<F16>(v);
+}
+
+template <int REST, class Consume>
+__device__ __forceinline__ void w4_last_stages(int stages, Consume &consume) {
+    if (stages > REST) consume(std::integral_constant<int, REST>{}, std::false_type{});
+    if constexpr (REST > 0) w4_last_stages<REST - 1>(stages, consume);
+}
+
+// XR: rows of X in a stage, 8 or 16; LEVELS: of the tree in a wavefront.
+template <int UNIT, bool F16, bool ZEROS, int XR, int RING, int LEVELS>
+__global__ __launch_bounds__(64 * W4_WAVES, XR == 8 && LEVELS <= 1 ? 4 : 2) void gemm_w4_slice_kernel(const W4Params p) {
+    using Stream = W4Stream<UNIT, ZEROS>;
+    constexpr int X_LOADS = XR / 8, X_BYTES = X_LOADS * 1024, STAGE = X_BYTES + Stream::BYTES, LOADS = X_LOADS + Stream::LOADS;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int li = lane & 31, lg = lane >> 5;
+    const int n0 = blockIdx.x * 32;
+    Acc<1, 1> acc;
+    if (wave < p.active_waves) {
+        const int64_t k0 = (int64_t)(blockIdx.z * p.leaves_per_shard + wave * p.leaves_per_wave) * p.superleaf;
+        const int stages_per_leaf = p.superleaf / W4_STAGE_K, stages = p.leaves_per_wave * stages_per_leaf;
+        Stream stream(p, n0, k0, lane);
+        const char *x_ptr = uniform_pointer(reinterpret_cast<const char *>(p.X + k0));
+        unsigned x_off[X_LOADS];
+#pragma unroll
+        for (int j = 0; j < X_LOADS; ++j) {            // rows behind the last one read it once more; they are not stored
+            const int r = 8 * j + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
+            x_off[j] = (unsigned)(min(r, p.M - 1) * (int)p.ldx + c * 8) * 2u;
+        }
+        const unsigned ring = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem + wave * RING * STAGE;
+        auto issue = [&](int slot) __attribute__((always_inline)) {
+            const unsigned at = ring + slot * STAGE;
+#pragma unroll
+            for (int j = 0; j < X_LOADS; ++j) load_16B_per_lane_to_lds<0, true>(x_ptr, x_off[j], at + j * 1024);
+            x_ptr += W4_STAGE_K * 2;
+            stream.issue(at + X_BYTES, lane, true);
+        };
+        const unsigned char *const mine = smem + wave * RING * STAGE;
+        const int xr = li & (XR - 1), x_sw = (xr >> 1) & 7;
+        GroupWalk walk(p.group / UNIT);
+        Acc<1, 1> sum;
+        f32x16 stash[LEVELS > 0 ? LEVELS : 1];
+        int left = stages_per_leaf, leaf = 0, slot = 0;
+        clear(acc);
+        clear(sum);
+        auto consume = [&](auto rest, auto again) __attribute__((always_inline)) {
+            w4_wait_loads<decltype(rest)::value * LOADS>();
+            const unsigned char *const st = mine + slot * STAGE;
+            const unsigned char *const x_rows[1] = {st + xr * 128};
+            multiply_stage<UNIT, F16, ZEROS, 1>(stream, st + X_BYTES, x_rows, x_sw, walk, sum, acc, li, lg);
+            if constexpr (decltype(again)::value) {    // the stage's bytes are in registers before its slot is filled again
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                issue(slot);
+            }
+            slot = slot + 1 == RING ? 0 : slot + 1;
+            if (--left == 0) {                         // a superleaf ends: the carry-over step of the tree
+                left = stages_per_leaf;
+                const int t = __builtin_ctz(~leaf);
+#pragma unroll
+                for (int l = 0; l < LEVELS; ++l)
+                    if (l < t) {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc.t[0][0][r] = stash[l][r] + acc.t[0][0][r];
+                    }
+                if (++leaf < p.leaves_per_wave) {
+#pragma unroll
+                    for (int l = 0; l < LEVELS; ++l)
+                        if (l == t) stash[l] = acc.t[0][0];
+                    clear(acc);
+                }
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < RING; ++i)
+            if (i < stages) issue(i);
+        for (int s = RING; s < stages; ++s) consume(std::integral_constant<int, RING - 1>{}, std::true_type{});
+        w4_last_stages<RING - 1>(stages, consume);
+    }
+    __syncthreads();                                   // the rings have been read: the sums take their place
+    float *const red = reinterpret_cast<float *>(smem);
+    if (wave < p.active_waves) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) red[wave * 1024 + (8 * (r >> 2) + 4 * lg + (r & 3)) * 32 + li] = acc.t[0][0][r];
+    }
+    __syncthreads();
+    const int row = threadIdx.x / 32, col = n0 + threadIdx.x % 32;                 // 16 rows of 32
+    if (row < p.M && col < p.N) store_sum<F16>(p, blockIdx.z, row, col, tree_of_waves(red, p.active_waves, threadIdx.x));
+}
+
+// 32 MT rows times 128 channels; the wavefronts share the rows of X in LDS.  blockIdx.z: the shard or the part of a split K.
+template <int UNIT, bool F16, bool ZEROS, int MT, int RING>
+__global__ __launch_bounds__(256, MT == 4 ? 1 : 2) void gemm_w4_tiled_kernel(const W4Params p) {
+    using Stream = W4Stream<UNIT, ZEROS>;
+    constexpr int REGION = MT * 1024 + Stream::BYTES, STAGE = 4 * REGION, LOADS = MT + Stream::LOADS;      // a region is what one wavefront loads
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int li = lane & 31, lg = lane >> 5;
+    const int m0 = blockIdx.y * 32 * MT, n0 = blockIdx.x * 128 + wave * 32;
+    const int64_t k0 = (int64_t)blockIdx.z * p.leaves_per_shard * p.superleaf;
+    const int stages_per_leaf = p.superleaf / W4_STAGE_K, stages = p.leaves_per_shard * stages_per_leaf;
+    Stream stream(p, min(n0, p.N - 1), k0, lane);
+    const char *x_ptr = uniform_pointer(reinterpret_cast<const char *>(p.X + (int64_t)m0 * p.ldx + k0));
+    unsigned x_off[MT];
+#pragma unroll
+    for (int j = 0; j < MT; ++j) {                     // 8 rows each; rows behind the last one read it once more
+        const int r = (wave * MT + j) * 8 + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
+        x_off[j] = (unsigned)(min(r, p.M - 1 - m0) * (int)p.ldx + c * 8) * 2u;
+    }
+    const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem + wave * REGION;
+    int to_issue = stages;                             // stages that are not yet on their way
+    auto issue = [&](int slot) __attribute__((always_inline)) {
+        const unsigned at = lds + slot * STAGE;
+#pragma unroll
+        for (int j = 0; j < MT; ++j) load_16B_per_lane_to_lds<0, true>(x_ptr, x_off[j], at + j * 1024);
+        const bool more = --to_issue > 0;              // the last stage is loaded again behind itself (nobody consumes it)
+        stream.issue(at + MT * 1024, lane, more);
+        if (more) x_ptr += W4_STAGE_K * 2;
+    };
+    int x_at[MT];
+#pragma unroll
+    for (int a = 0; a < MT; ++a) {
+        const int r = a * 32 + li;
+        x_at[a] = (r / (8 * MT)) * REGION + (r % (8 * MT)) * 128;
+    }
+    const int x_sw = (li >> 1) & 7;
+    GroupWalk walk(p.group / UNIT);
+    int cur = 0;
+    Acc<MT, 1> acc, sum;
+    f32x16 stash[MT][4];                               // finished subtrees of up to 16 superleaves
+    clear(sum);
+    clear(acc);
+#pragma unroll
+    for (int i = 0; i < RING - 1; ++i) issue(i);
+    for (int leaf = 0; leaf < p.leaves_per_shard; ++leaf) {
+#pragma nounroll
+        for (int s = 0; s < stages_per_leaf; ++s) {
+            // Own loads of this stage have landed, and behind the barrier everybody's; the slot of the stage before has been read.
+            w4_wait_loads_and_barrier<LOADS * (RING - 2)>();
+            issue(cur == 0 ? RING - 1 : cur - 1);
+            const unsigned char *const st = smem + cur * STAGE;
+            const unsigned char *x_rows[MT];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) x_rows[i] = st + x_at[i];
+            multiply_stage<UNIT, F16, ZEROS, MT>(stream, st + wave * REGION + MT * 1024, x_rows, x_sw, walk, sum, acc, li, lg);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            cur = cur + 1 == RING ? 0 : cur + 1;
+        }
+        const int t = __builtin_ctz(~leaf);            // a superleaf ends: the carry-over step of the tree
+        const bool more = leaf + 1 < p.leaves_per_shard;
+#pragma unroll
+        for (int a = 0; a < MT; ++a) {
+#pragma unroll
+            for (int l = 0; l < 4; ++l)
+                if (l < t) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc.t[a][0][r] = stash[a][l][r] + acc.t[a][0][r];
+                }
+        }
+        if (more) {
+#pragma unroll
+            for (int a = 0; a < MT; ++a) {
+#pragma unroll
+                for (int l = 0; l < 4; ++l)
+                    if (l == t) stash[a][l] = acc.t[a][0];
+            }
+            clear(acc);
+        }
+    }
+    w4_wait_loads_and_barrier<0>();                    // no load may still be writing LDS; all stages have been read
+    const int last = min(p.M - 1 - m0, 32 * MT - 1);
+    if (n0 >= p.N) return;
+    float *const patch = reinterpret_cast<float *>(smem) + wave * 1024;
+    if (p.vector_stores && n0 + 32 <= p.N) {
+        if (p.partials) store_ragged_f32(acc, patch, p.partials + ((int64_t)blockIdx.z * p.M + m0) * p.N + n0, p.N, last, lane, false);
+        else if (p.y_f32) store_ragged_f32(acc, patch, reinterpret_cast<float *>(p.Y) + (int64_t)m0 * p.ldy + n0, p.ldy, last, lane, false);
+        else store_ragged_16bit<F16>(acc, patch, reinterpret_cast<uint16_t *>(p.Y) + (int64_t)m0 * p.ldy + n0, p.ldy, last, lane);
+        return;
+    }
+    if (n0 + li >= p.N) return;
+#pragma unroll
+    for (int a = 0; a < MT; ++a)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int row = a * 32 + 8 * (r >> 2) + 4 * lg + (r & 3);
+            if (row <= last) store_sum<F16>(p, blockIdx.z, m0 + row, n0 + li, acc.t[a][0][r]);
+        }
+}
+
+// ---- any legal shape ----
 // UNIT: k of a lane pair's unit, 64 or 32.
 template <int UNIT, bool F16, bool ZEROS>
 __global__ __launch_bounds__(64 * W4_WAVES, 2) void gemm_w4_kernel(const W4Params p) {
@@ -165,7 +519,84 @@ __global__ __launch_bounds__(64 * W4_WAVES, 2) void gemm_w4_kernel(const W4Param
     }
 }
 
+template <class Kernel>
+hipError_t allow_lds(Kernel k, int lds, std::atomic<unsigned> &allowed) {
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 32) dev = 32;      // 32: not remembered, set every time
+    if (dev >= 32 || !((allowed.load(std::memory_order_relaxed) >> dev) & 1u)) { // bit d: the attribute is set on device d
+        const hipError_t e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+        if (dev < 32) allowed.fetch_or(1u << dev, std::memory_order_relaxed);
+    }
+    return hipSuccess;
+}
+
+template <int UNIT, bool F16, bool ZEROS, int XR, int RING, int LEVELS>
+hipError_t launch_slice(const W4Params &p, int shards, hipStream_t s) {
+    constexpr int lds = W4_WAVES * RING * (XR / 8 * 1024 + W4Stream<UNIT, ZEROS>::BYTES);
+    static_assert(lds <= 160 * 1024 && lds >= W4_WAVES * 4096, "LDS of a compute unit; room for the sums");
+    auto k = gemm_w4_slice_kernel<UNIT, F16, ZEROS, XR, RING, LEVELS>;
+    static std::atomic<unsigned> allowed{0};
+    const hipError_t e = allow_lds(k, lds, allowed);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(k, dim3((unsigned)((p.N + 31) / 32), 1, (unsigned)shards), dim3(64 * W4_WAVES), lds, s, p);
+    return hipGetLastError();
+}
+template <int UNIT, bool F16, bool ZEROS, int MT, int RING>
+hipError_t launch_tile(const W4Params &p, int shards, hipStream_t s) {
+    constexpr int lds = RING * 4 * (MT * 1024 + W4Stream<UNIT, ZEROS>::BYTES);
+    static_assert(lds <= 160 * 1024 && lds >= 4 * 4096, "LDS of a compute unit; room for the patches");
+    auto k = gemm_w4_tiled_kernel<UNIT, F16, ZEROS, MT, RING>;
+    static std::atomic<unsigned> allowed{0};
+    const hipError_t e = allow_lds(k, lds, allowed);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(k, dim3((unsigned)((p.N + 127) / 128), (unsigned)((p.M + 32 * MT - 1) / (32 * MT)), (unsigned)shards), dim3(256), lds, s, p);
+    return hipGetLastError();
+}
+
+template <int UNIT, bool F16, bool ZEROS>
+hipError_t launch_w4_of(const W4Args &a, const W4Params &all, hipStream_t s) {
+    W4Params p = all;
+    const int ns = a.ns / a.P;                         // superleaves of a shard
+    switch (w4_kernel(a)) {
+        case W4_SLICES: {
+            p.leaves_per_wave = ns > W4_WAVES ? ns / W4_WAVES : 1;
+            p.active_waves = ns > W4_WAVES ? W4_WAVES : ns;
+            if (a.M <= 8) return p.leaves_per_wave <= 2 ? launch_slice<UNIT, F16, ZEROS, 8, 4, 1>(p, a.P, s) : launch_slice<UNIT, F16, ZEROS, 8, 4, 4>(p, a.P, s);
+            return p.leaves_per_wave <= 2 ? launch_slice<UNIT, F16, ZEROS, 16, 4, 1>(p, a.P, s) : launch_slice<UNIT, F16, ZEROS, 16, 4, 4>(p, a.P, s);
+        }
+        case W4_TILES: {
+            if (a.M <= 32) return launch_tile<UNIT, F16, ZEROS, 1, 8>(p, a.P, s);
+            if (a.M <= 64) return launch_tile<UNIT, F16, ZEROS, 2, 5>(p, a.P, s);
+            return launch_tile<UNIT, F16, ZEROS, 4, 7>(p, a.P, s);
+        }
+        default: {
+            p.leaves_per_wave = ns > W4_WAVES ? ns / W4_WAVES : 1;
+            p.active_waves = ns > W4_WAVES ? W4_WAVES : ns;
+            if (p.leaves_per_wave > 16) return hipErrorInvalidValue;
+            for (int64_t m0 = 0; m0 < a.M; m0 += 32 * 4096) {          // 4096 row tiles a launch
+                W4Params q = p;
+                q.M = (int)(a.M - m0 < 32 * 4096 ? a.M - m0 : 32 * 4096);
+                q.X += m0 * a.ldx;
+                if (q.Y) q.Y = static_cast<char *>(q.Y) + m0 * a.ldy * (p.y_f32 ? 4 : 2);
+                if (q.partials) q.partials += m0 * a.N;
+                hipLaunchKernelGGL((gemm_w4_kernel<UNIT, F16, ZEROS>), dim3((unsigned)((a.N + 31) / 32), (unsigned)((q.M + 31) / 32), (unsigned)a.P), dim3(64 * W4_WAVES), 0, s, q);
+            }
+            return hipGetLastError();
+        }
+    }
+}
+
 }  // namespace
+
+// Slices up to 16 rows, tiles beyond; `a.P`: shards, or the parts of a split K.
+int w4_kernel(const W4Args &a) {
+    const int ns = a.ns / a.P;
+    const bool ring = a.superleaf % W4_STAGE_K == 0 && a.ldx < (1 << 22) && a.ldw < (1 << 22) && a.lds < (1 << 22) && a.ldz < (1 << 22);      // 32-bit lane offsets
+    if (!ring) return W4_GENERAL;
+    if (a.M <= 16) return W4_SLICES;
+    return ns <= 16 && (int64_t)a.M <= 32 * 65535 ? W4_TILES : W4_GENERAL;
+}
 
 hipError_t launch_gemm_w4(const W4Args &a, hipStream_t s) {
     if (a.M <= 0 || a.N <= 0) return hipSuccess;
@@ -177,27 +608,17 @@ hipError_t launch_gemm_w4(const W4Args &a, hipStream_t s) {
     p.y_f32 = a.y_dtype == TBIK_F32;
     p.group = a.group; p.superleaf = a.superleaf;
     p.leaves_per_shard = a.ns / a.P;
-    p.leaves_per_wave = p.leaves_per_shard > W4_WAVES ? p.leaves_per_shard / W4_WAVES : 1;
-    p.active_waves = p.leaves_per_shard > W4_WAVES ? W4_WAVES : p.leaves_per_shard;
-    if (p.leaves_per_wave > 16) return hipErrorInvalidValue;
-    auto launch = [&](auto kernel) {
-        for (int64_t m0 = 0; m0 < a.M; m0 += 32 * 4096) {              // 4096 row tiles a launch
-            W4Params q = p;
-            q.M = (int)(a.M - m0 < 32 * 4096 ? a.M - m0 : 32 * 4096);
-            q.X += m0 * a.ldx;
-            if (q.Y) q.Y = static_cast<char *>(q.Y) + m0 * a.ldy * (p.y_f32 ? 4 : 2);
-            hipLaunchKernelGGL(kernel, dim3((unsigned)((a.N + 31) / 32), (unsigned)((q.M + 31) / 32), (unsigned)a.P), dim3(64 * W4_WAVES), 0, s, q);
-        }
-    };
+    p.leaves_per_wave = p.active_waves = 0;
+    const void *out = a.partials ? (const void *)a.partials : a.Y;
+    const int64_t ld_bytes = a.partials ? (int64_t)a.N * 4 : a.ldy * (p.y_f32 ? 4 : 2);
+    p.vector_stores = (reinterpret_cast<uintptr_t>(out) & 15) == 0 && ld_bytes % 16 == 0 && ld_bytes < kMaxVectorRowBytes;
     const bool f16 = a.x_dtype == TBIK_F16, zeros = a.zeros != nullptr;
     if (a.group % 64 == 0) {
-        if (zeros) launch(f16 ? gemm_w4_kernel<64, true, true> : gemm_w4_kernel<64, false, true>);
-        else launch(f16 ? gemm_w4_kernel<64, true, false> : gemm_w4_kernel<64, false, false>);
-    } else {
-        if (zeros) launch(f16 ? gemm_w4_kernel<32, true, true> : gemm_w4_kernel<32, false, true>);
-        else launch(f16 ? gemm_w4_kernel<32, true, false> : gemm_w4_kernel<32, false, false>);
+        if (zeros) return f16 ? launch_w4_of<64, true, true>(a, p, s) : launch_w4_of<64, false, true>(a, p, s);
+        return f16 ? launch_w4_of<64, true, false>(a, p, s) : launch_w4_of<64, false, false>(a, p, s);
     }
-    return hipGetLastError();
+    if (zeros) return f16 ? launch_w4_of<32, true, true>(a, p, s) : launch_w4_of<32, false, true>(a, p, s);
+    return f16 ? launch_w4_of<32, true, false>(a, p, s) : launch_w4_of<32, false, false>(a, p, s);
 }
 
 }  // namespace tbik

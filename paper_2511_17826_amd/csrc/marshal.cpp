@@ -16,6 +16,7 @@
 
 #include <ATen/ATen.h>
 #include <c10/hip/HIPFunctions.h>
+#include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -25,13 +26,14 @@
 namespace {
 
 enum Kind { GEMM, GEMM_F32, PARTIALS, PARTIALS_F32, SWIGLU, FP8, MX, MXFP4, RMSNORM, COMBINE, ROWS, ATTENTION,
-            EPILOGUE, EPILOGUE_FP8, EPILOGUE_MX, EPILOGUE_COMBINE, NORM8, NORM8_MX, TAIL8, TAIL8_MX, SILU8, SILU8_MX, KINDS };
+            EPILOGUE, EPILOGUE_FP8, EPILOGUE_MX, EPILOGUE_COMBINE, NORM8, NORM8_MX, TAIL8, TAIL8_MX, SILU8, SILU8_MX,
+            ROUTE, GROUPED, GROUPED_SWIGLU, GROUPED_PARTIALS, EXPERTS_SUM, W4, W4_PARTIALS, JOIN, KINDS };
 struct Entry {
     int kind = -1;
     void *call = nullptr, *need = nullptr;      // the C entry point and its workspace query
     at::ScalarType dtype = at::kFloat;          // of its operands
 };
-constexpr int MAX_ENTRIES = 32;
+constexpr int MAX_ENTRIES = 48;
 Entry entries[MAX_ENTRIES];                     // written while the library is loaded, under the interpreter lock
 PyObject *workspaces = nullptr;                 // the binding's dict: (device index, stream) -> uint8 tensor
 PyObject *make_workspace = nullptr;             // the binding's function that fills it
@@ -510,6 +512,245 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     }
 }
 
+// ---- an MLP that is a mixture of experts, 4-bit weights, norms around a block ----
+bool here(const at::Tensor &t) { return t.device().index() == c10::hip::current_device(); }
+// A contiguous int32 vector or matrix.
+const at::Tensor *indexes(PyObject *o, int dim) {
+    const at::Tensor *t = plain(o, dim);
+    return t && t->scalar_type() == at::kInt && t->is_contiguous() ? t : nullptr;
+}
+bool sixteen_bits(const at::Tensor &t) { return t.scalar_type() == at::kBFloat16 || t.scalar_type() == at::kHalf; }
+tbik_dtype code_of(const at::Tensor &t) { return (tbik_dtype)type_code(t.scalar_type()); }
+template <int N>
+PyObject *tuple_of(at::Tensor (&t)[N], int status) {
+    if (status) return PyLong_FromLong(status);
+    PyObject *all = PyTuple_New(N);
+    if (!all) return nullptr;
+    for (int i = 0; i < N; ++i) {
+        PyObject *o = t[i].defined() ? THPVariable_Wrap(std::move(t[i])) : Py_NewRef(Py_None);
+        if (!o) {
+            Py_DECREF(all);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(all, i, o);
+    }
+    return all;
+}
+
+// route(entry, logits, k, renormalize) -> (experts, weights, offsets, rows, slots)
+PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 4) UNCOMMON;
+    const Entry *e = entry_of(a[0], ROUTE, ROUTE);
+    int k;
+    if (!e || !integer(a[2], &k) || !PyBool_Check(a[3])) UNCOMMON;
+    try {
+        const at::Tensor *l = plain(a[1], 2);
+        if (!l || l->stride(1) != 1 || type_code(l->scalar_type()) < 0 || l->size(0) > (1 << 26) || l->size(1) > 512 || k < 1 || k > l->size(1) || l->size(0) * k > INT_MAX || !here(*l)) UNCOMMON;
+        const int T = (int)l->size(0), E = (int)l->size(1);
+        void *stream = current_stream();
+        Room ws;
+        const size_t need = NEED(tbik_route_topk_workspace_bytes)(T, E);
+        if (need && c10::hip::currentStreamCaptureStatusMayInitCtx() != c10::hip::CaptureStatus::None) UNCOMMON;      // a workspace of the graph's own
+        if (!room_for(need, a[1], *l, stream, &ws)) return nullptr;
+        at::Tensor out[5] = {output({T, k}, *l, at::kInt), output({T, k}, *l, at::kFloat), output({E + 1}, *l, at::kInt), output({(L)T * k}, *l, at::kInt), output({T, k}, *l, at::kInt)};
+        for (const at::Tensor &t : out)
+            if (!t.defined()) UNCOMMON;
+        P at[5], logits = l->data_ptr();
+        for (int i = 0; i < 5; ++i) at[i] = out[i].data_ptr();
+        const L ldl = l->stride(0);
+        const tbik_dtype type = code_of(*l);
+        const int renormalize = a[3] == Py_True;
+        int st;
+        Py_BEGIN_ALLOW_THREADS
+        st = CALL(tbik_route_topk)(logits, ldl, type, T, E, k, renormalize, (int32_t *)at[0], (float *)at[1], (int32_t *)at[2], (int32_t *)at[3], (int32_t *)at[4], ws.at, ws.bytes, stream);
+        Py_END_ALLOW_THREADS
+        return tuple_of(out, st);
+    } catch (const std::exception &) {
+        if (PyErr_Occurred()) return nullptr;
+        UNCOMMON;
+    }
+}
+
+// grouped(entry, X, W, offsets, rows or None, leaf, k_first, out dtype or None, shards)
+PyObject *grouped(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 9) UNCOMMON;
+    const Entry *e = entry_of(a[0], GROUPED, GROUPED_PARTIALS);
+    int leaf, k_first, shards;
+    if (!e || !integer(a[5], &leaf) || !integer(a[6], &k_first) || !integer(a[8], &shards)) UNCOMMON;
+    const int kind = e->kind;
+    try {
+        const at::Tensor *X = plain(a[1], 2), *W = plain(a[2], 3), *offsets = indexes(a[3], 1), *rows = nullptr;
+        if (a[4] != Py_None && !(rows = indexes(a[4], 1))) UNCOMMON;
+        if (!X || !W || !offsets || !sixteen_bits(*X) || W->scalar_type() != X->scalar_type() || X->stride(1) != 1 || W->stride(2) != 1 || X->size(0) > INT_MAX || X->size(1) > INT_MAX ||
+            W->size(0) > 512 || W->size(1) != X->size(1) || W->size(2) > INT_MAX || offsets->size(0) != W->size(0) + 1 || (rows && rows->size(0) > INT_MAX) || !here(*X) || elsewhere(W, *X) ||
+            elsewhere(offsets, *X) || elsewhere(rows, *X))
+            UNCOMMON;
+        at::ScalarType type = X->scalar_type();
+        if (a[7] != Py_None) {
+            if (!THPDtype_Check(a[7])) UNCOMMON;
+            type = ((THPDtype *)a[7])->scalar_type;
+            if (type_code(type) < 0) UNCOMMON;
+        }
+        const int tokens = (int)X->size(0), K = (int)X->size(1), groups = (int)W->size(0), N = (int)W->size(2), R = rows ? (int)rows->size(0) : tokens;
+        if ((kind == GROUPED_SWIGLU && N % 2) || shards < 1) UNCOMMON;
+        at::Tensor y = kind == GROUPED_PARTIALS ? output({shards, R, N}, *X, at::kFloat) : output({R, kind == GROUPED_SWIGLU ? N / 2 : N}, *X, type);
+        if (!y.defined()) UNCOMMON;
+        P px = X->data_ptr(), pw = W->data_ptr(), po = offsets->data_ptr(), pr = rows ? rows->data_ptr() : nullptr, py = y.data_ptr(), stream = current_stream();
+        const L ldx = X->stride(0), ldw = W->stride(1), stride = W->stride(0), ldy = kind == GROUPED_PARTIALS ? 0 : y.stride(0);
+        const tbik_dtype xt = code_of(*X), yt = code_of(y);
+        int st;
+        Py_BEGIN_ALLOW_THREADS
+        if (kind == GROUPED)
+            st = CALL(tbik_gemm_grouped)(px, ldx, tokens, (const int32_t *)pr, pw, ldw, stride, groups, (const int32_t *)po, py, ldy, yt, xt, R, N, K, leaf, k_first, stream);
+        else if (kind == GROUPED_SWIGLU)
+            st = CALL(tbik_gemm_grouped_swiglu)(px, ldx, tokens, (const int32_t *)pr, pw, ldw, stride, groups, (const int32_t *)po, py, ldy, xt, R, N / 2, K, leaf, k_first, stream);
+        else
+            st = CALL(tbik_gemm_grouped_shard_partials)(px, ldx, tokens, (const int32_t *)pr, pw, ldw, stride, groups, (const int32_t *)po, (float *)py, xt, R, N, K, leaf, k_first, shards, stream);
+        Py_END_ALLOW_THREADS
+        return wrapped(std::move(y), st);
+    } catch (const std::exception &) {
+        if (PyErr_Occurred()) return nullptr;
+        UNCOMMON;
+    }
+}
+
+// experts_sum(entry, Y, slots, weights, residual or None, out dtype or None)
+PyObject *experts_sum(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 6) UNCOMMON;
+    const Entry *e = entry_of(a[0], EXPERTS_SUM, EXPERTS_SUM);
+    if (!e) UNCOMMON;
+    try {
+        const at::Tensor *y = plain(a[1], 3), *slots = indexes(a[2], 2), *w = plain(a[3], 2), *r = nullptr;
+        const bool sums = y != nullptr;
+        if (!sums) y = plain(a[1], 2);
+        if (a[4] != Py_None && !(r = plain(a[4], 2))) UNCOMMON;
+        if (!y || !slots || !w || type_code(y->scalar_type()) < 0 || (sums && y->scalar_type() != at::kFloat) || w->scalar_type() != at::kFloat || !w->is_contiguous() || w->sizes() != slots->sizes()) UNCOMMON;
+        if (y->scalar_type() == at::kFloat ? !y->is_contiguous() : y->stride(1) != 1) UNCOMMON;
+        at::ScalarType type = r ? r->scalar_type() : y->scalar_type();
+        if (a[5] != Py_None) {
+            if (!THPDtype_Check(a[5])) UNCOMMON;
+            type = ((THPDtype *)a[5])->scalar_type;
+        }
+        const int d = sums ? 1 : 0;
+        if (type_code(type) < 0 || y->size(0) > INT_MAX || y->size(d) > INT_MAX || y->size(d + 1) > INT_MAX || slots->size(0) > INT_MAX || slots->size(1) > INT_MAX || !here(*y) ||
+            elsewhere(slots, *y) || elsewhere(w, *y) || elsewhere(r, *y))
+            UNCOMMON;
+        const int shards = sums ? (int)y->size(0) : 1, R = (int)y->size(d), H = (int)y->size(d + 1), T = (int)slots->size(0), k = (int)slots->size(1);
+        if (r && (r->scalar_type() != type || r->size(0) != T || r->size(1) != H || r->stride(1) != 1)) UNCOMMON;
+        at::Tensor out = output({T, H}, *y, type);
+        if (!out.defined()) UNCOMMON;
+        P py = y->data_ptr(), ps = slots->data_ptr(), pw = w->data_ptr(), pr = r ? r->data_ptr() : nullptr, po = out.data_ptr(), stream = current_stream();
+        const L ldy = y->stride(d), ldr = r ? r->stride(0) : 0, ldo = out.stride(0);
+        const tbik_dtype yt = code_of(*y), ot = code_of(out);
+        int st;
+        Py_BEGIN_ALLOW_THREADS
+        st = CALL(tbik_combine_experts)(py, ldy, yt, shards, R, (const int32_t *)ps, (const float *)pw, pr, ldr, po, ldo, ot, T, H, k, stream);
+        Py_END_ALLOW_THREADS
+        return wrapped(std::move(out), st);
+    } catch (const std::exception &) {
+        if (PyErr_Occurred()) return nullptr;
+        UNCOMMON;
+    }
+}
+
+// w4(entry, X, Wq, scales, zeros or None, leaf, k_first, out dtype or None, shards)
+PyObject *w4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 9) UNCOMMON;
+    const Entry *e = entry_of(a[0], W4, W4_PARTIALS);
+    int leaf, k_first, shards;
+    if (!e || !integer(a[5], &leaf) || !integer(a[6], &k_first) || !integer(a[8], &shards) || shards < 1) UNCOMMON;
+    try {
+        const at::Tensor *X = plain(a[1], 2), *W = matrix(a[2], at::kByte), *z = nullptr;
+        if (!X || !W || !sixteen_bits(*X) || X->stride(1) != 1 || X->size(0) > INT_MAX || X->size(1) > INT_MAX) UNCOMMON;
+        const at::Tensor *sc = matrix(a[3], X->scalar_type());
+        if (!sc || (a[4] != Py_None && !(z = matrix(a[4], at::kByte)))) UNCOMMON;
+        at::ScalarType type = X->scalar_type();
+        if (a[7] != Py_None) {
+            if (!THPDtype_Check(a[7])) UNCOMMON;
+            type = ((THPDtype *)a[7])->scalar_type;
+            if (type_code(type) < 0) UNCOMMON;
+        }
+        const int M = (int)X->size(0), K = (int)X->size(1), N = (int)W->size(0), groups = (int)sc->size(1);
+        if (K % 2 || W->size(1) != K / 2 || sc->size(0) != N || groups < 1 || K % groups || (z && z->sizes() != sc->sizes()) || !here(*X) || elsewhere(W, *X) || elsewhere(sc, *X) || elsewhere(z, *X)) UNCOMMON;
+        const bool partials = e->kind == W4_PARTIALS;
+        void *stream = current_stream();
+        Room ws;
+        const size_t need = partials ? 0 : NEED(tbik_gemm_w4_workspace_bytes)(M, N, K, leaf, k_first);
+        if (need && c10::hip::currentStreamCaptureStatusMayInitCtx() != c10::hip::CaptureStatus::None) UNCOMMON;      // a workspace of the graph's own
+        if (!room_for(need, a[1], *X, stream, &ws)) return nullptr;
+        at::Tensor y = partials ? output({shards, M, N}, *X, at::kFloat) : output({M, N}, *X, type);
+        if (!y.defined()) UNCOMMON;
+        P px = X->data_ptr(), pw = W->data_ptr(), ps = sc->data_ptr(), pz = z ? z->data_ptr() : nullptr, py = y.data_ptr();
+        const L ldx = X->stride(0), ldw = W->stride(0), lds = sc->stride(0), ldz = z ? z->stride(0) : 0, ldy = partials ? 0 : y.stride(0);
+        const tbik_dtype xt = code_of(*X), yt = code_of(y);
+        int st;
+        Py_BEGIN_ALLOW_THREADS
+        if (partials) st = CALL(tbik_gemm_shard_partials_w4)(px, ldx, pw, ldw, ps, lds, pz, ldz, K / groups, (float *)py, xt, M, N, K, leaf, k_first, shards, stream);
+        else st = CALL(tbik_gemm_w4)(px, ldx, pw, ldw, ps, lds, pz, ldz, K / groups, py, ldy, yt, xt, M, N, K, leaf, k_first, ws.at, ws.bytes, stream);
+        Py_END_ALLOW_THREADS
+        return wrapped(std::move(y), st);
+    } catch (const std::exception &) {
+        if (PyErr_Occurred()) return nullptr;
+        UNCOMMON;
+    }
+}
+
+// join(entry, y, residual, post_weight or None, next_weight or None, eps, residual_scale, gate or None) -> (hidden, normed or None)
+PyObject *join(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 8) UNCOMMON;
+    const Entry *e = entry_of(a[0], JOIN, JOIN);
+    float eps, scale;
+    if (!e || !number(a[5], &eps) || !number(a[6], &scale)) UNCOMMON;
+    try {
+        const at::Tensor *r = plain(a[2], 2);
+        if (!r || !sixteen_bits(*r) || r->stride(1) != 1 || r->size(0) > INT_MAX || r->size(1) > INT_MAX) UNCOMMON;
+        const at::ScalarType type = r->scalar_type();
+        const int M = (int)r->size(0), H = (int)r->size(1);
+        const at::Tensor *y = plain(a[1], 3), *w[2] = {nullptr, nullptr}, *gate = nullptr;
+        const bool sums = y != nullptr;
+        if (sums ? y->scalar_type() != at::kFloat || !y->is_contiguous() || y->size(0) > INT_MAX || y->size(1) != M || y->size(2) != H
+                 : !(y = matrix(a[1], type)) || y->size(0) != M || y->size(1) != H)
+            UNCOMMON;
+        for (int i = 0; i < 2; ++i) {
+            if (a[3 + i] == Py_None) continue;
+            w[i] = plain(a[3 + i], 1);
+            if (!w[i] || w[i]->scalar_type() != type || w[i]->size(0) != H || !w[i]->is_contiguous()) UNCOMMON;
+        }
+        L gate_row = 0;
+        int gate_column = 0;
+        if (a[7] != Py_None) {
+            if ((gate = plain(a[7], 1))) {
+                if (gate->size(0) != H) UNCOMMON;
+            } else {
+                gate = plain(a[7], 2);
+                if (!gate || (gate->size(0) != 1 && gate->size(0) != M) || (gate->size(1) != 1 && gate->size(1) != H)) UNCOMMON;
+                if (gate->size(0) == M && M > 1) gate_row = gate->stride(0);
+            }
+            const int last = (int)gate->dim() - 1;
+            gate_column = gate->size(last) == H && H > 1;
+            if (gate->scalar_type() != type || (gate_column && gate->stride(last) != 1)) UNCOMMON;
+        }
+        if (!here(*r) || elsewhere(y, *r) || elsewhere(w[0], *r) || elsewhere(w[1], *r) || elsewhere(gate, *r)) UNCOMMON;
+        at::Tensor out[2] = {output({M, H}, *r, type), at::Tensor()};
+        if (w[1]) out[1] = output({M, H}, *r, type);
+        if (!out[0].defined() || (w[1] && !out[1].defined())) UNCOMMON;
+        P py = y->data_ptr(), pr = r->data_ptr(), pw[2] = {w[0] ? w[0]->data_ptr() : nullptr, w[1] ? w[1]->data_ptr() : nullptr}, pg = gate ? gate->data_ptr() : nullptr,
+          ph = out[0].data_ptr(), pn = w[1] ? out[1].data_ptr() : nullptr, stream = current_stream();
+        const L ldy = sums ? 0 : y->stride(0), ldr = r->stride(0), ldh = out[0].stride(0);
+        const int shards = sums ? (int)y->size(0) : 1;
+        const tbik_dtype t = code_of(*r);
+        int st;
+        Py_BEGIN_ALLOW_THREADS
+        st = CALL(tbik_rmsnorm_residual_rmsnorm)(sums ? nullptr : py, ldy, sums ? (const float *)py : nullptr, shards, pr, ldr, scale, pw[0], pg, gate_row, gate_column, pw[1], eps, ph, ldh, pn,
+                                                 pn ? ldh : 0, t, M, H, stream);
+        Py_END_ALLOW_THREADS
+        return tuple_of(out, st);
+    } catch (const std::exception &) {
+        if (PyErr_Occurred()) return nullptr;
+        UNCOMMON;
+    }
+}
+
 // register(entry, kind, address, address of the workspace query or 0, operand dtype)
 PyObject *register_entry(PyObject *, PyObject *args) {
     int i, kind;
@@ -548,6 +789,11 @@ PyMethodDef methods[] = {
     {"attention", (PyCFunction)(void (*)(void))attention, METH_FASTCALL, nullptr},
     {"epilogue", (PyCFunction)(void (*)(void))epilogue, METH_FASTCALL, nullptr},
     {"eight_bits", (PyCFunction)(void (*)(void))eight_bits, METH_FASTCALL, nullptr},
+    {"route", (PyCFunction)(void (*)(void))route, METH_FASTCALL, nullptr},
+    {"grouped", (PyCFunction)(void (*)(void))grouped, METH_FASTCALL, nullptr},
+    {"experts_sum", (PyCFunction)(void (*)(void))experts_sum, METH_FASTCALL, nullptr},
+    {"w4", (PyCFunction)(void (*)(void))w4, METH_FASTCALL, nullptr},
+    {"join", (PyCFunction)(void (*)(void))join, METH_FASTCALL, nullptr},
     {"register", register_entry, METH_VARARGS, nullptr},
     {"use", use, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};

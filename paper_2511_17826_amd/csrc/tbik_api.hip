@@ -1359,8 +1359,22 @@ int tbik_rmsnorm_residual_rmsnorm(const void *y, int64_t ldy, const float *parti
     return e == hipSuccess ? TBIK_OK : hip_fail(e);
 }
 
+// Parts that K is split into where the tiles of a 4-bit product leave compute units idle: until there is a workgroup for each (and a tile
+// walks at most 16 superleaves).  Up to 16 rows are slices, which split K among their wavefronts.
+static int w4_split(int M, int N, int K, int ns) {
+    (void)K;
+    if (M <= 16) return 1;
+    const int rows = M <= 32 ? 32 : M <= 64 ? 64 : 128;
+    const int64_t tiles = ((int64_t)N + 127) / 128 * (((int64_t)M + rows - 1) / rows);
+    int split = 1;
+    while (ns > 16 * split) split *= 2;
+    while (split < ns && split < 16 && tiles * split < 256) split *= 2;
+    return split;
+}
+
 static int gemm_w4(tbik_dtype x_dtype, const void *X, int64_t ldx, const void *Wq, int64_t ldwq, const void *scales, int64_t lds, const void *zeros, int64_t ldz,
-                   int group, void *Y, int64_t ldy, tbik_dtype y_dtype, float *partials, int M, int N, int K, int leaf, int k_first, int P, void *hip_stream) {
+                   int group, void *Y, int64_t ldy, tbik_dtype y_dtype, float *partials, int M, int N, int K, int leaf, int k_first, int P,
+                   void *workspace, size_t workspace_bytes, void *hip_stream) {
     int sl, ns;
     int rc = check_tree(M, N, K, leaf, k_first, P, &sl, &ns);
     if (rc != TBIK_OK) return rc;
@@ -1381,19 +1395,39 @@ static int gemm_w4(tbik_dtype x_dtype, const void *X, int64_t ldx, const void *W
     a.zeros = (const uint8_t *)zeros;
     a.ldz = ldz;
     a.group = group;
-    hipError_t e = launch_gemm_w4(a, (hipStream_t)hip_stream);
+    hipStream_t s = (hipStream_t)hip_stream;
+    if (workspace && !aligned(workspace, 256)) return TBIK_ERR_ALIGN;
+    hipError_t e;
+    int split = partials ? 1 : w4_split(M, N, K, ns);
+    while (split > 1 && split_planes_bytes(M, N, split) > (workspace ? workspace_bytes : 0)) split /= 2;      // less room: the same bits with less of a split
+    if (split > 1 && w4_kernel(a) != W4_SLICES) {
+        a.partials = reinterpret_cast<float *>(workspace);
+        a.Y = nullptr;
+        a.P = split;
+        e = launch_gemm_w4(a, s);
+        if (e == hipSuccess) e = launch_tree_combine(a.partials, split, Y, ldy, (int)y_dtype, M, N, s);
+    } else {
+        e = launch_gemm_w4(a, s);
+    }
     return e == hipSuccess ? TBIK_OK : hip_fail(e);
 }
 
+size_t tbik_gemm_w4_workspace_bytes(int M, int N, int K, int leaf, int k_first) {
+    int sl, ns;
+    if (check_tree(M, N, K, leaf, k_first, 1, &sl, &ns) != TBIK_OK) return 0;
+    return split_planes_bytes(M, N, w4_split(M, N, K, ns));
+}
+
 int tbik_gemm_w4(const void *X, int64_t ldx, const void *Wq, int64_t ldwq, const void *scales, int64_t lds, const void *zeros, int64_t ldz, int group,
-                 void *Y, int64_t ldy, tbik_dtype y_dtype, tbik_dtype x_dtype, int M, int N, int K, int leaf, int k_first, void *hip_stream) {
-    return gemm_w4(x_dtype, X, ldx, Wq, ldwq, scales, lds, zeros, ldz, group, Y, ldy, y_dtype, nullptr, M, N, K, leaf, k_first, 1, hip_stream);
+                 void *Y, int64_t ldy, tbik_dtype y_dtype, tbik_dtype x_dtype, int M, int N, int K, int leaf, int k_first,
+                 void *workspace, size_t workspace_bytes, void *hip_stream) {
+    return gemm_w4(x_dtype, X, ldx, Wq, ldwq, scales, lds, zeros, ldz, group, Y, ldy, y_dtype, nullptr, M, N, K, leaf, k_first, 1, workspace, workspace_bytes, hip_stream);
 }
 
 int tbik_gemm_shard_partials_w4(const void *X, int64_t ldx, const void *Wq, int64_t ldwq, const void *scales, int64_t lds, const void *zeros, int64_t ldz,
                                 int group, float *partials, tbik_dtype x_dtype, int M, int N, int K, int leaf, int k_first, int P, void *hip_stream) {
     if (!partials && M > 0 && N > 0) return TBIK_ERR_NULL;
-    return gemm_w4(x_dtype, X, ldx, Wq, ldwq, scales, lds, zeros, ldz, group, nullptr, 0, TBIK_F32, partials, M, N, K, leaf, k_first, P, hip_stream);
+    return gemm_w4(x_dtype, X, ldx, Wq, ldwq, scales, lds, zeros, ldz, group, nullptr, 0, TBIK_F32, partials, M, N, K, leaf, k_first, P, nullptr, 0, hip_stream);
 }
 
 int tbik_tree_allreduce(float *bufs, int P, int64_t n, void *hip_stream) {

@@ -188,6 +188,8 @@ struct W4Args : GemmArgs {
     int64_t ldz;
     int group;
 };
+enum { W4_GENERAL, W4_SLICES, W4_TILES };
+int w4_kernel(const W4Args &a);            // what a call launches
 hipError_t launch_gemm_w4(const W4Args &a, hipStream_t s);
 
 // Y = T(partials[0..P)) elementwise + one rounding.

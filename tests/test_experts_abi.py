@@ -27,7 +27,7 @@ PARTIALS = dict(X=A, ldx=512, tokens=10, rows=A, W=A, ldw=256, stride=512 * 256,
                 K=512, leaf=64, k_first=1, P=2, stream=None)
 SUM = dict(Y=A, ldy=64, y_dtype=BF16, P=1, R=20, slots=A, weights=A, residual=A, ldr=64, out=A, ldo=64, out_dtype=BF16, T=10, H=64, k=2, stream=None)
 W4 = dict(X=A, ldx=512, Wq=A, ldwq=256, scales=A, lds=8, zeros=A, ldz=8, group=64, Y=A, ldy=128, y_dtype=BF16, x_dtype=BF16, M=3, N=128, K=512, leaf=64,
-          k_first=1, stream=None)
+          k_first=1, ws=None, ws_bytes=0, stream=None)
 W4P = dict(X=A, ldx=512, Wq=A, ldwq=256, scales=A, lds=8, zeros=None, ldz=0, group=64, partials=A, x_dtype=BF16, M=3, N=128, K=512, leaf=64, k_first=1, P=2,
            stream=None)
 JOIN = dict(y=A, ldy=64, partials=None, P=1, residual=A, ldr=64, scale=1.0, post=A, gate=A, gate_row=0, gate_col=1, next=A, eps=1e-6, hidden=2 * A, ldh=64, normed=A,
@@ -88,7 +88,7 @@ def test_combine_refuses(L, changes, status):
     (dict(ldwq=240), SHAPE), (dict(lds=7), SHAPE), (dict(ldz=7), SHAPE), (dict(ldy=127), SHAPE), (dict(x_dtype=F32, y_dtype=F32), DTYPE), (dict(y_dtype=F16), DTYPE),
     (dict(X=None), NULL), (dict(Wq=None), NULL), (dict(scales=None), NULL), (dict(Y=None), NULL), (dict(X=A + 8), ALIGN), (dict(Wq=A + 8), ALIGN), (dict(ldwq=264), ALIGN),
     (dict(ldx=516), ALIGN), (dict(scales=A + 1), ALIGN), (dict(Y=A + 1), ALIGN), (dict(K=64 * 256, ldx=64 * 256, ldwq=32 * 256, lds=256, ldz=256), UNSUPPORTED),
-    (dict(M=0), OK), (dict(N=0), OK)])
+    (dict(ws=A + 64, ws_bytes=1 << 20), ALIGN), (dict(M=0), OK), (dict(N=0), OK)])
 def test_w4_refuses(L, changes, status):
     assert call(L, "tbik_gemm_w4", W4, **changes) == status
 

@@ -100,6 +100,20 @@ def test_batch_and_shards(K, leaf, k_first, group, dtype, zeros):
         assert torch.equal(bits(tb.tbik_tree_combine(torch.stack(halves), out_dtype=torch.float32)), bits(want))
 
 
+def test_less_workspace_and_the_general_kernel():
+    """The split of K follows the room; operands too far apart for the kernels with direct loads go another way: the same bits."""
+    X, Wq, scales, z = operands(40, 256, 4096, 64, torch.bfloat16, True, 7)
+    want = tb.tbik_gemm_w4(X, Wq, scales, 256, 1, zeros=z)
+    need = tb.lib().tbik_gemm_w4_workspace_bytes(40, 256, 4096, 256, 1)
+    assert need > 0
+    for room in (0, 256, need // 2, need // 4 + 1, need):
+        assert torch.equal(bits(tb.tbik_gemm_w4(X, Wq, scales, 256, 1, zeros=z, workspace=torch.empty(room, dtype=torch.uint8, device=DEV))), bits(want))
+    far = torch.empty_strided((40, 4096), (1 << 22, 1), dtype=torch.bfloat16, device=DEV)
+    far.copy_(X)
+    for rows in (3, 40):
+        assert torch.equal(bits(tb.tbik_gemm_w4(far[:rows], Wq, scales, 256, 1, zeros=z)), bits(want[:rows]))
+
+
 def test_strides():
     X, Wq, scales, z = operands(9, 70, 512, 64, torch.bfloat16, True, 4)
     want = tb.tbik_gemm_w4(X, Wq, scales, 64, 1, zeros=z)
