@@ -20,7 +20,7 @@ LIB = os.path.join(HERE, "libtbik.so")
 SOURCES = ["gemm_mxfp8_epilogue.hip", "gemm_fp8_epilogue.hip", "gemm_tiled_epilogue.hip", "gemm_fp8.hip", "gemm_tiled.hip", "gemm_tiled_grouped.hip", "tbik_api.hip", "gemm_reference.hip", "gemm_f32.hip", "gemm_mxfp4.hip",
            "gemm_mxfp6.hip", "gemm_slice.hip", "combine.hip", "combine_epilogue.hip", "activation.hip", "activation_8bit.hip",
            "rmsnorm.hip", "rmsnorm_8bit.hip", "row_reduce.hip",
-           "attention.hip", "attention_decode.hip", "route.hip", "gemm_grouped.hip", "gemm_grouped_slice.hip", "experts_sum.hip", "gemm_w4.hip", "rmsnorm_join.hip"]
+           "attention.hip", "attention_decode.hip", "route.hip", "gemm_grouped.hip", "gemm_grouped_slice.hip", "experts_sum.hip", "gemm_w4.hip", "gemm_w4_f16.hip", "rmsnorm_join.hip"]
 
 # -ffp-contract=off: a tree addition or an RMSNorm multiply must never be fused into an FMA.
 # packed-fp32 ops are switched off for the device pass (known-bad forms on the test machines).
@@ -105,8 +105,9 @@ def build(save_temps: bool = True, jobs: int = 8, defines=(), lib_path: str = LI
         check_generated_code(os.path.join(BUILD, "gemm_tiled_epilogue-hip-amdgcn-amd-amdhsa-gfx950.s"), "gemm_tiled_kernel")
         check_generated_code(os.path.join(BUILD, "gemm_tiled_grouped-hip-amdgcn-amd-amdhsa-gfx950.s"), "gemm_tiled_kernel")
         check_generated_code(os.path.join(BUILD, "gemm_grouped_slice-hip-amdgcn-amd-amdhsa-gfx950.s"), "gemm_grouped_slice_kernel")
-        for kernel in ("gemm_w4_slice_kernel", "gemm_w4_tiled_kernel"):
-            check_generated_code(os.path.join(BUILD, "gemm_w4-hip-amdgcn-amd-amdhsa-gfx950.s"), kernel)
+        for unit in ("gemm_w4", "gemm_w4_f16"):
+            for kernel in ("gemm_w4_slice_kernel", "gemm_w4_tiled_kernel"):
+                check_generated_code(os.path.join(BUILD, unit + "-hip-amdgcn-amd-amdhsa-gfx950.s"), kernel)
         for unit in ("gemm_fp8_epilogue", "gemm_mxfp8_epilogue"):
             check_generated_code(os.path.join(BUILD, unit + "-hip-amdgcn-amd-amdhsa-gfx950.s"), "gemm_fp8_tiled_kernel")
         check_generated_code(os.path.join(BUILD, "attention-hip-amdgcn-amd-amdhsa-gfx950.s"), "attention_")

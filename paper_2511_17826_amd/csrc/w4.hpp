@@ -1,0 +1,381 @@
+// The parts of the products on 4-bit weights: an element's widening, and stages in LDS.  See gemm_w4.hip.
+#pragma once
+
+#include <algorithm>
+#include <atomic>
+#include <type_traits>
+
+#include "tbik_device.hpp"
+#include "tbik_internal.hpp"
+#include "tile_store.hpp"
+
+namespace tbik {
+
+struct W4Params {
+    const uint16_t *X;
+    const uint8_t *W;
+    const uint16_t *scales;
+    const uint8_t *zeros;
+    float *partials;
+    void *Y;
+    int64_t ldx, ldw, lds, ldz, ldy;
+    int M, N;
+    int y_f32;
+    int superleaf, groups_per_leaf;
+    int units_per_group;                   // of the call's UNIT
+    int stages_per_leaf;                   // of the call's stage
+    int leaves_per_wave, active_waves, leaves_per_shard;
+    int vector_stores;
+    int row_bytes;                         // slices of one row: LDS for the row's part of a wavefront's k, whole loads
+};
+
+constexpr int W4_WAVES = 8;                // of a slice, and of the general kernel's workgroup
+
+// Eight elements of one dword, element i in bits 4 i .. 4 i + 3, as 16-bit floats of (q - zero) / 16 in order.  `zero`: ZeroPoint of the channel's group.
+// bf16: a float per element (v_cvt_off_f32_i4 of the 4-bit two's complement number q - 8, whose byte selection costs nothing; with zero points the bytes q - zero
+// through v_cvt_f32_i32), then the upper halves of two as one register: exact.  14 instructions (19 with zero points).
+// fp16: 1024 + q has q in its low bits; one packed subtraction of 1024 + zero for two of them, exact.  13 instructions.
+template <bool F16, bool ZEROS>
+struct ZeroPoint {
+    uint32_t v;
+    __device__ __forceinline__ explicit ZeroPoint(int zero = 8) {
+        if constexpr (F16) {
+            const uint32_t h = 0xe400u + (uint32_t)zero;             // -(1024 + zero)
+            v = h | (h << 16);
+        } else {
+            v = (uint32_t)(128 - zero) * 0x01010101u;
+        }
+    }
+};
+typedef _Float16 w4_f16x2 __attribute__((ext_vector_type(2)));
+// Two elements a byte: byte B of `even` holds element 2 B in its low bits, of `odd` element 2 B + 1.
+template <int B>
+__device__ __forceinline__ uint32_t byte_of(uint32_t v) { return B == 3 ? v >> 24 : (v >> (8 * B)) & 0xffu; }
+template <bool F16, bool ZEROS>
+__device__ __forceinline__ bf16x8 widened_levels(uint32_t w, const ZeroPoint<F16, ZEROS> &zero) {
+    union { uint32_t u[4]; w4_f16x2 h[4]; bf16x8 v; } out;
+    if constexpr (F16) {
+        const uint32_t odd = w >> 4;
+        const w4_f16x2 less = __builtin_bit_cast(w4_f16x2, zero.v);
+        out.u[0] = __builtin_amdgcn_perm(odd, w, 0x0c040c00u);       // bytes B of w and of odd, one in each half
+        out.u[1] = __builtin_amdgcn_perm(odd, w, 0x0c050c01u);
+        out.u[2] = __builtin_amdgcn_perm(odd, w, 0x0c060c02u);
+        out.u[3] = __builtin_amdgcn_perm(odd, w, 0x0c070c03u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(out.u[i]) : "v"(out.u[i]), "s"(0x000f000fu), "v"(0x64006400u));      // (left to the compiler it is two instructions)
+            out.h[i] = out.h[i] + less;
+        }
+    } else {
+        float v[8];
+        if constexpr (ZEROS) {
+            const uint32_t even = ((w & 0x0f0f0f0fu) + zero.v) ^ 0x80808080u, odd = (((w >> 4) & 0x0f0f0f0fu) + zero.v) ^ 0x80808080u;      // signed bytes q - zero
+            v[0] = (float)(int8_t)even; v[2] = (float)(int8_t)(even >> 8); v[4] = (float)(int8_t)(even >> 16); v[6] = (float)(int8_t)(even >> 24);
+            v[1] = (float)(int8_t)odd; v[3] = (float)(int8_t)(odd >> 8); v[5] = (float)(int8_t)(odd >> 16); v[7] = (float)(int8_t)(odd >> 24);
+        } else {
+            const uint32_t even = w ^ 0x88888888u;
+            uint32_t odd = even >> 4;
+            asm("" : "+v"(odd));                                     // a register of its own, whose bytes the conversions select
+            v[0] = __builtin_amdgcn_cvt_off_f32_i4(even); v[2] = __builtin_amdgcn_cvt_off_f32_i4(byte_of<1>(even));
+            v[4] = __builtin_amdgcn_cvt_off_f32_i4(byte_of<2>(even)); v[6] = __builtin_amdgcn_cvt_off_f32_i4(byte_of<3>(even));
+            v[1] = __builtin_amdgcn_cvt_off_f32_i4(odd); v[3] = __builtin_amdgcn_cvt_off_f32_i4(byte_of<1>(odd));
+            v[5] = __builtin_amdgcn_cvt_off_f32_i4(byte_of<2>(odd)); v[7] = __builtin_amdgcn_cvt_off_f32_i4(byte_of<3>(odd));
+        }
+#pragma unroll
+        for (int b = 0; b < 4; ++b) out.u[b] = __builtin_amdgcn_perm(__float_as_uint(v[2 * b + 1]), __float_as_uint(v[2 * b]), 0x07060302u);
+    }
+    return out.v;
+}
+// What the scale is multiplied by: the bf16 elements without zero points come as sixteenths.
+template <bool F16, bool ZEROS>
+constexpr float kLevelUnit = F16 || ZEROS ? 1.0f : 16.0f;
+
+template <bool F16>
+__device__ __forceinline__ float widened_16(uint16_t h) { return F16 ? (float)__builtin_bit_cast(_Float16, h) : bf16_bits_to_f32(h); }
+
+template <bool F16>
+__device__ __forceinline__ f32x4 mfma_16x16x32(bf16x8 a, bf16x8 b, f32x4 c) {
+    if constexpr (F16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// The sums of 16 MR rows and 16 NB channels: block (a, b) is 16 x 16, the lane has rows 4 (lane / 16) .. + 3 of channel lane % 16.
+template <int MR, int NB = 2>
+struct W4Sums {
+    f32x4 t[MR][NB];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int a = 0; a < MR; ++a)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) t[a][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+};
+// Finished subtrees of up to 2^LEVELS superleaves (the carry-over scheme of App. D.1): `leaf`, counted from 0, has ended in acc.
+template <int MR, int NB, int LEVELS>
+struct W4Stash {
+    f32x4 s[MR][NB][LEVELS];
+    __device__ __forceinline__ void push(W4Sums<MR, NB> &acc, int leaf, bool more) {
+        const int t = __builtin_ctz(~leaf);
+#pragma unroll
+        for (int a = 0; a < MR; ++a)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+#pragma unroll
+                for (int l = 0; l < LEVELS; ++l)
+                    if (l < t) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc.t[a][b][r] = s[a][b][l][r] + acc.t[a][b][r];
+                    }
+            }
+        if (!more) return;
+#pragma unroll
+        for (int a = 0; a < MR; ++a)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+#pragma unroll
+                for (int l = 0; l < LEVELS; ++l)
+                    if (LEVELS == 1 || l == t) s[a][b][l] = acc.t[a][b];
+            }
+        acc.clear();
+    }
+};
+
+// T over 2^levels superleaves, levels <= L: a nest of loops, each of two trips or (above `levels`) one, whose first trip parks its subtree's sum in a slot of
+// its own.  (With the stash above, whose slot is chosen when it is used, tiles of 64 and 128 rows spill.)
+template <int L>
+struct W4Walk {
+    template <class Leaf, int MR, int SLOTS>
+    __device__ __forceinline__ static void run(Leaf &leaf, W4Sums<MR> &acc, W4Sums<MR> (&slots)[SLOTS], int levels) {
+        const int trips = L <= levels ? 2 : 1;
+#pragma nounroll
+        for (int half = 0; half < trips; ++half) {
+            W4Walk<L - 1>::run(leaf, acc, slots, levels);
+            if (half + 1 < trips) {
+                slots[L - 1] = acc;
+            } else if (half == 1) {
+#pragma unroll
+                for (int a = 0; a < MR; ++a)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc.t[a][b][r] = slots[L - 1].t[a][b][r] + acc.t[a][b][r];
+            }
+        }
+    }
+};
+template <>
+struct W4Walk<0> {
+    template <class Leaf, int MR, int SLOTS>
+    __device__ __forceinline__ static void run(Leaf &leaf, W4Sums<MR> &acc, W4Sums<MR> (&)[SLOTS], int) { leaf(acc); }
+};
+
+// ---- stages in LDS (slices and tiles) ----
+// A stage is 64 S k.  Of one wavefront it holds rows of X (128 S bytes), the 32 S bytes of each of 32 channels, and a dword per lane and pair of units with the
+// scale (and one with the zero point) of the unit's group: lanes 0 .. 31 the even unit, lanes 32 .. 63 the odd one.  Chunks of 16 bytes are swapped
+// about within a row so that the rows of a read meet different banks.
+// S = 2 where superleaves are whole stages of 128 k: with 64, whose 32 bytes of a channel are a quarter of a cache line, the weight alone came in at
+// 1.6 TB/s (27 rows, K = 12288, N = 4096 without the loads of X and the scales 16.6 us; so 7.3).
+template <int N>
+__device__ __forceinline__ void w4_wait_loads() {
+    static_assert(N >= 0 && N < 64, "vmcnt range");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void w4_wait_loads_and_barrier() {
+    static_assert(N >= 0 && N < 64, "vmcnt range");
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// What a chunk's number is XORed with in row r of X and in channel r of the weight.
+template <int S>
+__device__ __forceinline__ int x_swizzle(int r) { return S == 1 ? (r >> 1) & 7 : r & 15; }
+template <int S>
+__device__ __forceinline__ int w_swizzle(int r) { return S == 1 ? 0 : S == 2 ? (r >> 2) & 3 : (r >> 1) & 7; }
+
+// The group of one unit after another.
+struct GroupWalk {
+    int g, left;
+    int units;                             // of a group
+    __device__ __forceinline__ explicit GroupWalk(int units_per_group) : g(0), left(units_per_group), units(units_per_group) {}
+    __device__ __forceinline__ bool next() {       // true: the unit was the group's last
+        if (--left != 0) return false;
+        left = units;
+        ++g;
+        return true;
+    }
+};
+
+// One wavefront's stream of weight, scales and zero points: 16 NB channels from n0 on, superleaves from `leaf` on.
+template <int UNIT, bool ZEROS, int S, int NB = 2>
+struct W4Stream {
+    static constexpr int UNITS = 64 * S / UNIT, PAIRS = (UNITS + 1) / 2, W_LOADS = S * NB / 2;
+    static_assert(W_LOADS >= 1, "whole loads");
+    static constexpr int LOADS = W_LOADS + PAIRS * (ZEROS ? 2 : 1);
+    static constexpr int SCALES = W_LOADS * 1024, ZERO_POINTS = SCALES + PAIRS * 256, BYTES = ZERO_POINTS + (ZEROS ? PAIRS * 256 : 0);
+    const char *w_ptr, *s_ptr, *z_ptr;
+    unsigned w_off[W_LOADS], s_off, z_off;       // of the lane; s_off and z_off count from an aligned dword
+    GroupWalk walk;                        // of the stream's next unit
+
+    __device__ __forceinline__ W4Stream(const W4Params &p, int n0, int leaf, int lane) : walk(p.units_per_group) {
+        const uint8_t *w = p.W + n0 * p.ldw + (int64_t)leaf * p.superleaf / 2;
+        const uint16_t *sc = p.scales + n0 * p.lds + (int64_t)leaf * p.groups_per_leaf;
+        w_ptr = uniform_pointer(reinterpret_cast<const char *>(w));
+#pragma unroll
+        for (int j = 0; j < W_LOADS; ++j) {      // 64 chunks each, 2 S of a channel
+            const int r = j * (32 / S) + lane / (2 * S), c = (lane % (2 * S)) ^ w_swizzle<S>(r);
+            w_off[j] = (unsigned)(min(r, p.N - 1 - n0) * (int)p.ldw + c * 16);
+        }
+        const int channel = min(lane & 31 & (16 * NB - 1), p.N - 1 - n0);
+        const unsigned s_low = (unsigned)(reinterpret_cast<uintptr_t>(sc) & 3);
+        s_ptr = uniform_pointer(reinterpret_cast<const char *>(sc) - s_low);
+        s_off = s_low + (unsigned)(channel * (int)p.lds) * 2u;
+        z_ptr = nullptr;
+        z_off = 0;
+        if constexpr (ZEROS) {
+            const uint8_t *z = p.zeros + n0 * p.ldz + (int64_t)leaf * p.groups_per_leaf;
+            const unsigned z_low = (unsigned)(reinterpret_cast<uintptr_t>(z) & 3);
+            z_ptr = uniform_pointer(reinterpret_cast<const char *>(z) - z_low);
+            z_off = z_low + (unsigned)(channel * (int)p.ldz);
+        }
+    }
+    // The next stage's loads to LDS address `at` (uniform): weight, scales, zero points.  A scale's dword holds its neighbour too.
+    // `more`: there is a stage behind it; else the next issue loads it again.
+    __device__ __forceinline__ void issue(unsigned at, int lane, bool more) {
+#pragma unroll
+        for (int j = 0; j < W_LOADS; ++j) load_16B_per_lane_to_lds<0, true>(w_ptr, w_off[j], at + j * 1024);
+        GroupWalk behind = walk;
+#pragma unroll
+        for (int q = 0; q < PAIRS; ++q) {
+            int g = behind.g;
+            behind.next();
+            if constexpr (UNITS > 1) {
+                if (lane >= 32) g = behind.g;
+                behind.next();
+            }
+            load_4B_per_lane_to_lds<0, true>(s_ptr, (s_off + 2u * g) & ~3u, at + SCALES + q * 256);
+            if constexpr (ZEROS) load_4B_per_lane_to_lds<0, true>(z_ptr, (z_off + g) & ~3u, at + ZERO_POINTS + q * 256);
+        }
+        if (more) {
+            walk = behind;
+            w_ptr += 32 * S;
+        }
+    }
+    // From the stage at `st` in LDS, for unit u of it, which is group g's.  low: where in its dword the channel's first one lies, s_off or z_off of lane `channel`.
+    template <bool F16>
+    __device__ __forceinline__ ZeroPoint<F16, ZEROS> zero(const unsigned char *st, int u, int g, int channel, unsigned low) const {
+        const unsigned z = *reinterpret_cast<const unsigned *>(st + ZERO_POINTS + (u * 32 + channel) * 4);
+        return ZeroPoint<F16, ZEROS>((int)((z >> (8u * ((low + g) & 3u))) & 15u));
+    }
+    template <bool F16>
+    __device__ __forceinline__ float scale(const unsigned char *st, int u, int g, int channel, unsigned low) const {
+        const unsigned s = *reinterpret_cast<const unsigned *>(st + SCALES + (u * 32 + channel) * 4);
+        return widened_16<F16>((uint16_t)(s >> (8u * ((low + 2u * g) & 2u)))) * kLevelUnit<F16, ZEROS>;
+    }
+};
+
+// Multiplies a stage: rows x_rows[a] (the lane's row of X of block a in the stage, in LDS) times the stage's weight at st.  sum: the running group's; a group that ends
+// goes through its scale into acc.  lane % 16: the row of X and the channel of a block; quarter: lane / 16.
+template <int UNIT, bool F16, bool ZEROS, int S, int MR, int NB = 2>
+struct W4Multiplier {
+    using Stream = W4Stream<UNIT, ZEROS, S, NB>;
+    static constexpr int UNITS = 64 * S / UNIT, STEPS = UNIT / 32;      // units of a stage, instructions of a unit
+    unsigned s_low[NB], z_low[NB];
+    int w_at[NB], w_sw, l16, quarter;
+    GroupWalk walk;
+    W4Sums<MR, NB> sum;
+
+    // All 64 lanes of the wavefront.
+    __device__ __forceinline__ W4Multiplier(const W4Params &p, const Stream &stream, int lane) : walk(p.units_per_group) {
+        l16 = lane & 15;
+        quarter = lane >> 4;
+        w_sw = w_swizzle<S>(l16);                          // of both of the lane's channels
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            s_low[b] = __shfl(stream.s_off, b * 16 + l16);
+            z_low[b] = ZEROS ? __shfl(stream.z_off, b * 16 + l16) : 0u;
+            w_at[b] = (b * 16 + l16) * (32 * S);
+        }
+        sum.clear();
+    }
+    __device__ __forceinline__ void stage(const Stream &stream, const unsigned char *st, const unsigned char *const (&x_rows)[MR], int x_sw, W4Sums<MR, NB> &acc) {
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            uint32_t words[NB][STEPS];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                if constexpr (UNIT == 128) {               // chunk `quarter` of the unit's four
+                    const uint4 v = *reinterpret_cast<const uint4 *>(st + w_at[b] + (((4 * u + quarter) ^ w_sw) << 4));
+                    words[b][0] = v.x; words[b][1] = v.y; words[b][2] = v.z; words[b][3] = v.w;
+                } else if constexpr (UNIT == 64) {         // half a chunk
+                    const uint2 v = *reinterpret_cast<const uint2 *>(st + w_at[b] + (((2 * u + (quarter >> 1)) ^ w_sw) << 4) + (quarter & 1) * 8);
+                    words[b][0] = v.x; words[b][1] = v.y;
+                } else {
+                    words[b][0] = *reinterpret_cast<const uint32_t *>(st + w_at[b] + ((u ^ w_sw) << 4) + quarter * 4);
+                }
+            }
+            // The rows' fragments of all the unit's instructions at once; of many rows an instruction or two at a time, or they would not fit the registers.
+            constexpr int AHEAD = MR <= 2 ? STEPS : MR == 4 ? 1 : STEPS > 2 ? 2 : STEPS;
+            bf16x8 x[AHEAD][MR];
+            auto read_x = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+                for (int a = 0; a < MR; ++a) x[i % AHEAD][a] = *reinterpret_cast<const bf16x8 *>(x_rows[a] + (((u * (UNIT / 8) + quarter * STEPS + i) ^ x_sw) << 4));
+            };
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) read_x(i);
+            ZeroPoint<F16, ZEROS> zero[NB];
+            if constexpr (ZEROS) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b) zero[b] = stream.template zero<F16>(st, u, walk.g, b * 16 + l16, z_low[b]);
+            }
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    const bf16x8 w = widened_levels<F16, ZEROS>(words[b][i], zero[b]);
+#pragma unroll
+                    for (int a = 0; a < MR; ++a) sum.t[a][b] = mfma_16x16x32<F16>(x[i % AHEAD][a], w, sum.t[a][b]);
+                }
+                if constexpr (AHEAD < STEPS) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (i + AHEAD < STEPS) read_x(i + AHEAD);
+                }
+            }
+            const int g = walk.g;
+            if (walk.next()) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    const float scale = stream.template scale<F16>(st, u, g, b * 16 + l16, s_low[b]);
+#pragma unroll
+                    for (int a = 0; a < MR; ++a)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc.t[a][b][r] = __builtin_fmaf(scale, sum.t[a][b][r], acc.t[a][b][r]);
+                }
+                sum.clear();
+            }
+        }
+    }
+};
+
+template <bool F16>
+__device__ __forceinline__ void w4_store(const W4Params &p, int shard, int row, int col, float v) {
+    if (p.partials) p.partials[((int64_t)shard * p.M + row) * p.N + col] = v;
+    else if (p.y_f32) reinterpret_cast<float *>(p.Y)[(int64_t)row * p.ldy + col] = v;
+    else reinterpret_cast<uint16_t *>(p.Y)[(int64_t)row * p.ldy + col] = (uint16_t)f32_to_16_bits<F16>(v);
+}
+// T over the wavefronts' sums in LDS, STRIDE floats apart.
+template <int STRIDE>
+__device__ __forceinline__ float tree_of_waves(const float *red, int active, int at) {
+    float v[W4_WAVES];
+#pragma unroll
+    for (int w = 0; w < W4_WAVES; ++w) v[w] = red[w < active ? w * STRIDE + at : at];
+#pragma unroll
+    for (int s = 1; s < W4_WAVES; s *= 2)
+#pragma unroll
+        for (int r = 0; r < W4_WAVES; r += 2 * s)
+            if (r + s < active) v[r] = v[r] + v[r + s];
+    return v[0];
+}
+
+}  // namespace tbik
