@@ -39,7 +39,7 @@ template <int UNIT, bool F16, bool ZEROS, int S, int XR, int RING, int LEVELS>
 __global__ __launch_bounds__(64 * W4_WAVES, XR == 1 ? (LEVELS == 1 && RING == 2 ? 6 : 4) : RING == 2 ? 4 : 2) void gemm_w4_slice_kernel(const W4Params p) {
     constexpr bool ONE = XR == 1;
     constexpr int NB = ONE ? 1 : 2;
-    using Stream = W4Stream<UNIT, ZEROS, S, NB>;
+    using Stream = W4Stream<ZEROS, S, NB>;
     constexpr int X_LOADS = ONE ? 0 : XR * S / 8, X_BYTES = X_LOADS * 1024, STAGE = X_BYTES + Stream::BYTES, LOADS = X_LOADS + Stream::LOADS;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -47,7 +47,11 @@ __global__ __launch_bounds__(64 * W4_WAVES, XR == 1 ? (LEVELS == 1 && RING == 2 
     W4Sums<1, NB> acc;
     if (wave < p.active_waves) {
         const int first_leaf = blockIdx.z * p.leaves_per_shard + wave * p.leaves_per_wave, stages = p.leaves_per_wave * p.stages_per_leaf;
-        Stream stream(p, n0, first_leaf, lane);
+        const int row_at = RING * STAGE, groups_at = row_at + (ONE ? p.row_bytes : 0), wave_bytes = groups_at + p.group_bytes;
+        const unsigned ring = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem + wave * wave_bytes;
+        const unsigned char *const mine = smem + wave * wave_bytes;
+        Stream stream(p, n0, first_leaf, p.leaves_per_wave, lane, ring + groups_at, mine + groups_at);
+        stream.issue_groups(0, lane);
         const char *x_ptr = uniform_pointer(reinterpret_cast<const char *>(p.X + (int64_t)first_leaf * p.superleaf));
         unsigned x_off[ONE ? 1 : X_LOADS];
 #pragma unroll
@@ -55,31 +59,29 @@ __global__ __launch_bounds__(64 * W4_WAVES, XR == 1 ? (LEVELS == 1 && RING == 2 
             const int r = j * (8 / S) + lane / (8 * S), c = (lane % (8 * S)) ^ x_swizzle<S>(r);
             x_off[j] = (unsigned)(min(r, p.M - 1) * (int)p.ldx + c * 8) * 2u;
         }
-        const int wave_bytes = RING * STAGE + (ONE ? p.row_bytes : 0);
-        const unsigned ring = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem + wave * wave_bytes;
         if constexpr (ONE) {                           // 512 k a load; behind the part's end its last chunk
             for (int j = 0; j * 1024 < p.row_bytes; ++j)
-                load_16B_per_lane_to_lds<0, true>(x_ptr, (unsigned)min(j * 1024 + lane * 16, stages * (128 * S) - 16), ring + RING * STAGE + j * 1024);
+                load_16B_per_lane_to_lds<0, true>(x_ptr, (unsigned)min(j * 1024 + lane * 16, stages * (128 * S) - 16), ring + row_at + j * 1024);
         }
         auto issue = [&](int slot) __attribute__((always_inline)) {
             const unsigned at = ring + slot * STAGE;
 #pragma unroll
             for (int j = 0; j < X_LOADS; ++j) load_16B_per_lane_to_lds<0, true>(x_ptr, x_off[j], at + j * 1024);
             x_ptr += 128 * S;
-            stream.issue(at + X_BYTES, lane, true);
+            stream.issue(at + X_BYTES, true);
         };
 #pragma unroll
         for (int i = 0; i < RING; ++i)
             if (i < stages) issue(i);
-        const unsigned char *const mine = smem + wave * wave_bytes;
         const int xr = lane & 15 & (XR - 1), x_sw = ONE ? 0 : x_swizzle<S>(xr);
-        const unsigned char *row = mine + RING * STAGE;
+        const unsigned char *row = mine + row_at;
         W4Multiplier<UNIT, F16, ZEROS, S, 1, NB> multiplier(p, stream, lane);
         W4Stash<1, NB, LEVELS> stash;
         int left = p.stages_per_leaf, leaf = 0, slot = 0;
         acc.clear();
         auto consume = [&](auto rest, auto again) __attribute__((always_inline)) {
             w4_wait_loads<decltype(rest)::value * LOADS>();
+            multiplier.prefetch_groups(stream, lane);
             const unsigned char *const st = mine + slot * STAGE;
             const unsigned char *const x_rows[1] = {ONE ? row : st + xr * (128 * S)};
             row += 128 * S;
@@ -116,7 +118,7 @@ __global__ __launch_bounds__(64 * W4_WAVES, XR == 1 ? (LEVELS == 1 && RING == 2 
 // and its matrix instructions take turns, and a second one on its vector unit fills the gaps.
 template <int UNIT, bool F16, bool ZEROS, int S, int MT, int RING, int KG>
 __global__ __launch_bounds__(256 * KG, MT == 4 ? 1 : 2) void gemm_w4_tiled_kernel(const W4Params p) {
-    using Stream = W4Stream<UNIT, ZEROS, S>;
+    using Stream = W4Stream<ZEROS, S>;
     constexpr int MR = 2 * MT;
     constexpr int X_LOADS = MT * S, REGION = X_LOADS * 1024 + Stream::BYTES, STAGE = 4 * REGION, LOADS = X_LOADS + Stream::LOADS;      // a region is what one wavefront loads
     extern __shared__ __attribute__((aligned(16))) unsigned char all_smem[];
@@ -126,7 +128,10 @@ __global__ __launch_bounds__(256 * KG, MT == 4 ? 1 : 2) void gemm_w4_tiled_kerne
     const int m0 = blockIdx.y * 32 * MT, n0 = blockIdx.x * 128 + wave * 32;
     const int leaves = p.leaves_per_shard / KG, stages = leaves * p.stages_per_leaf;
     const int first_leaf = blockIdx.z * p.leaves_per_shard + part * leaves;
-    Stream stream(p, min(n0, p.N - 1), first_leaf, lane);
+    const unsigned all_lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)all_smem;
+    const int groups_at = KG * RING * STAGE + every_wave * p.group_bytes;
+    Stream stream(p, min(n0, p.N - 1), first_leaf, leaves, lane, all_lds + groups_at, all_smem + groups_at);
+    stream.issue_groups(0, lane);
     const char *x_ptr = uniform_pointer(reinterpret_cast<const char *>(p.X + (int64_t)m0 * p.ldx + (int64_t)first_leaf * p.superleaf));
     unsigned x_off[X_LOADS];
 #pragma unroll
@@ -134,14 +139,14 @@ __global__ __launch_bounds__(256 * KG, MT == 4 ? 1 : 2) void gemm_w4_tiled_kerne
         const int r = wave * 8 * MT + j * (8 / S) + lane / (8 * S), c = (lane % (8 * S)) ^ x_swizzle<S>(r);
         x_off[j] = (unsigned)(min(r, p.M - 1 - m0) * (int)p.ldx + c * 8) * 2u;
     }
-    const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem + wave * REGION;
+    const unsigned lds = all_lds + part * (RING * STAGE) + wave * REGION;
     int to_issue = stages;                             // stages that are not yet on their way
     auto issue = [&](int slot) __attribute__((always_inline)) {
         const unsigned at = lds + slot * STAGE;
 #pragma unroll
         for (int j = 0; j < X_LOADS; ++j) load_16B_per_lane_to_lds<0, true>(x_ptr, x_off[j], at + j * 1024);
         const bool more = --to_issue > 0;              // the last stage is loaded again behind itself (nobody consumes it)
-        stream.issue(at + X_LOADS * 1024, lane, more);
+        stream.issue(at + X_LOADS * 1024, more);
         if (more) x_ptr += 128 * S;
     };
 #pragma unroll
@@ -166,6 +171,7 @@ __global__ __launch_bounds__(256 * KG, MT == 4 ? 1 : 2) void gemm_w4_tiled_kerne
             // Own loads of this stage have landed, and behind the barrier everybody's; the slot of the stage before has been read.
             w4_wait_loads_and_barrier<LOADS * (RING - 2)>();
             issue(cur == 0 ? RING - 1 : cur - 1);
+            multiplier.prefetch_groups(stream, lane);
             const unsigned char *const st = smem + cur * STAGE;
             const unsigned char *x_rows[MR];
 #pragma unroll
@@ -352,15 +358,30 @@ hipError_t allow_lds(Kernel k, int lds, std::atomic<unsigned> &allowed) {
     return hipSuccess;
 }
 
+// The chunks of scales and zero points of a wavefront that walks `leaves` superleaves of `channels`.
+void chunks_of(W4Params &p, int channels, int leaves, bool zeros) {
+    const int groups = leaves * p.groups_per_leaf, most = std::min(groups, W4_CHUNK), buffers = w4_chunk_buffers(groups);
+    p.s_dwords = (2 * most + 5) / 4;                   // the first element may lie 2 bytes into its dword, a zero point 3
+    p.z_dwords = (most + 6) / 4;
+    p.s_inverse = 65536 / p.s_dwords + 1;
+    p.z_inverse = 65536 / p.z_dwords + 1;
+    p.group_bytes = buffers * (w4_chunk_bytes(channels, p.s_dwords) + (zeros ? w4_chunk_bytes(channels, p.z_dwords) : 0));
+}
+constexpr int most_group_bytes(int channels, bool zeros) {
+    return 2 * (w4_chunk_bytes(channels, (2 * W4_CHUNK + 5) / 4) + (zeros ? w4_chunk_bytes(channels, (W4_CHUNK + 6) / 4) : 0));
+}
+
 template <int UNIT, bool F16, bool ZEROS, int S, int XR, int RING, int LEVELS>
-hipError_t launch_slice_of(const W4Params &p, int shards, hipStream_t s) {
+hipError_t launch_slice_of(const W4Params &all, int shards, hipStream_t s) {
     constexpr int NB = XR == 1 ? 1 : 2, row = XR == 1 ? 8192 : 0;
-    constexpr int ring = RING * ((XR == 1 ? 0 : XR * S * 128) + W4Stream<UNIT, ZEROS, S, NB>::BYTES);
-    static_assert(W4_WAVES * (ring + row) <= 160 * 1024 && ring >= 2048, "LDS of a compute unit; room for the sums");
-    const int lds = W4_WAVES * (ring + (XR == 1 ? p.row_bytes : 0));
+    constexpr int ring = RING * ((XR == 1 ? 0 : XR * S * 128) + W4Stream<ZEROS, S, NB>::BYTES), most = W4_WAVES * (ring + row + most_group_bytes(16 * NB, ZEROS));
+    static_assert(most <= 160 * 1024 && ring >= 2048, "LDS of a compute unit; room for the sums");
+    W4Params p = all;
+    chunks_of(p, 16 * NB, p.leaves_per_wave, ZEROS);
+    const int lds = W4_WAVES * (ring + (XR == 1 ? p.row_bytes : 0) + p.group_bytes);
     auto k = gemm_w4_slice_kernel<UNIT, F16, ZEROS, S, XR, RING, LEVELS>;
     static std::atomic<unsigned> allowed{0};
-    const hipError_t e = allow_lds(k, W4_WAVES * (ring + row), allowed);
+    const hipError_t e = allow_lds(k, most, allowed);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(k, dim3((unsigned)((p.N + 16 * NB - 1) / (16 * NB)), 1, (unsigned)shards), dim3(64 * W4_WAVES), lds, s, p);
     return hipGetLastError();
@@ -370,12 +391,15 @@ hipError_t launch_slice(const W4Params &p, int shards, hipStream_t s) {
     return p.leaves_per_wave <= 2 ? launch_slice_of<UNIT, F16, ZEROS, S, XR, RING, 1>(p, shards, s) : launch_slice_of<UNIT, F16, ZEROS, S, XR, RING, 4>(p, shards, s);
 }
 template <int UNIT, bool F16, bool ZEROS, int S, int MT, int RING, int KG = 1>
-hipError_t launch_tile(const W4Params &p, int shards, hipStream_t s) {
-    constexpr int lds = KG * RING * 4 * (MT * S * 1024 + W4Stream<UNIT, ZEROS, S>::BYTES);
-    static_assert(lds <= 160 * 1024 && lds >= 4 * MT * 4096, "LDS of a compute unit; room for the sums and the patches");
+hipError_t launch_tile(const W4Params &all, int shards, hipStream_t s) {
+    constexpr int rings = KG * RING * 4 * (MT * S * 1024 + W4Stream<ZEROS, S>::BYTES), most = rings + 4 * KG * most_group_bytes(32, ZEROS);
+    static_assert(most <= 160 * 1024 && rings >= 4 * MT * 4096, "LDS of a compute unit; room for the sums and the patches");
+    W4Params p = all;
+    chunks_of(p, 32, p.leaves_per_shard / KG, ZEROS);
+    const int lds = rings + 4 * KG * p.group_bytes;
     auto k = gemm_w4_tiled_kernel<UNIT, F16, ZEROS, S, MT, RING, KG>;
     static std::atomic<unsigned> allowed{0};
-    const hipError_t e = allow_lds(k, lds, allowed);
+    const hipError_t e = allow_lds(k, most, allowed);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(k, dim3((unsigned)((p.N + 127) / 128), (unsigned)((p.M + 32 * MT - 1) / (32 * MT)), (unsigned)shards), dim3(256 * KG), lds, s, p);
     return hipGetLastError();
@@ -406,8 +430,8 @@ hipError_t launch_slice_rows(const W4Params &all, int shards, hipStream_t s) {
 template <int UNIT, bool F16, bool ZEROS, int S>
 hipError_t launch_tile_rows(const W4Params &p, int shards, hipStream_t s) {
     const bool halves = p.leaves_per_shard % 2 == 0;   // a power of two: or one
-    if (p.M <= 32) return halves ? launch_tile<UNIT, F16, ZEROS, S, 1, S == 1 ? 6 : 4, 2>(p, shards, s) : launch_tile<UNIT, F16, ZEROS, S, 1, S == 1 ? 6 : 4>(p, shards, s);
-    if (p.M <= 64) return halves ? launch_tile<UNIT, F16, ZEROS, S, 2, S == 1 ? 5 : 2, 2>(p, shards, s) : launch_tile<UNIT, F16, ZEROS, S, 2, S == 1 ? 5 : 3>(p, shards, s);
+    if (p.M <= 32) return halves ? launch_tile<UNIT, F16, ZEROS, S, 1, S == 1 ? 6 : 3, 2>(p, shards, s) : launch_tile<UNIT, F16, ZEROS, S, 1, S == 1 ? 6 : 4>(p, shards, s);
+    if (p.M <= 64) return halves ? launch_tile<UNIT, F16, ZEROS, S, 2, S == 1 ? 4 : 2, 2>(p, shards, s) : launch_tile<UNIT, F16, ZEROS, S, 2, S == 1 ? 5 : 3>(p, shards, s);
     return launch_tile<UNIT, F16, ZEROS, S, 4, S == 1 ? 6 : 3>(p, shards, s);
 }
 template <int UNIT, bool F16, bool ZEROS>

@@ -27,6 +27,9 @@ struct W4Params {
     int leaves_per_wave, active_waves, leaves_per_shard;
     int vector_stores;
     int row_bytes;                         // slices of one row: LDS for the row's part of a wavefront's k, whole loads
+    int s_dwords, z_dwords;                // of a channel in a chunk of scales, of zero points
+    int s_inverse, z_inverse;              // 65536 over them, rounded up: quotients of numbers below 1024
+    int group_bytes;                       // LDS of a wavefront for its chunks of both
 };
 
 constexpr int W4_WAVES = 8;                // of a slice, and of the general kernel's workgroup
@@ -172,11 +175,12 @@ struct W4Walk<0> {
 };
 
 // ---- stages in LDS (slices and tiles) ----
-// A stage is 64 S k.  Of one wavefront it holds rows of X (128 S bytes), the 32 S bytes of each of 32 channels, and a dword per lane and pair of units with the
-// scale (and one with the zero point) of the unit's group: lanes 0 .. 31 the even unit, lanes 32 .. 63 the odd one.  Chunks of 16 bytes are swapped
+// A stage is 64 S k.  Of one wavefront it holds rows of X (128 S bytes) and the 32 S bytes of each of its channels.  Chunks of 16 bytes are swapped
 // about within a row so that the rows of a read meet different banks.
 // S = 2 where superleaves are whole stages of 128 k: with 64, whose 32 bytes of a channel are a quarter of a cache line, the weight alone came in at
 // 1.6 TB/s (27 rows, K = 12288, N = 4096 without the loads of X and the scales 16.6 us; so 7.3).
+// Scales and zero points come in chunks of up to 32 groups, the next one on its way while one is used: a load for every stage touched a cache line of every channel
+// and was more than half of all requests to the caches (same shape, 2.0 million).
 template <int N>
 __device__ __forceinline__ void w4_wait_loads() {
     static_assert(N >= 0 && N < 64, "vmcnt range");
@@ -207,71 +211,84 @@ struct GroupWalk {
     }
 };
 
-// One wavefront's stream of weight, scales and zero points: 16 NB channels from n0 on, superleaves from `leaf` on.
-template <int UNIT, bool ZEROS, int S, int NB = 2>
-struct W4Stream {
-    static constexpr int UNITS = 64 * S / UNIT, PAIRS = (UNITS + 1) / 2, W_LOADS = S * NB / 2;
-    static_assert(W_LOADS >= 1, "whole loads");
-    static constexpr int LOADS = W_LOADS + PAIRS * (ZEROS ? 2 : 1);
-    static constexpr int SCALES = W_LOADS * 1024, ZERO_POINTS = SCALES + PAIRS * 256, BYTES = ZERO_POINTS + (ZEROS ? PAIRS * 256 : 0);
-    const char *w_ptr, *s_ptr, *z_ptr;
-    unsigned w_off[W_LOADS], s_off, z_off;       // of the lane; s_off and z_off count from an aligned dword
-    GroupWalk walk;                        // of the stream's next unit
+constexpr int W4_CHUNK = 32;               // groups
+// LDS of a chunk of `dwords` for each of `channels`: whole loads.
+__host__ __device__ constexpr int w4_chunk_bytes(int channels, int dwords) { return (channels * dwords * 4 + 255) & ~255; }
+__host__ __device__ constexpr int w4_chunk_buffers(int groups) { return groups > W4_CHUNK ? 2 : 1; }
 
-    __device__ __forceinline__ W4Stream(const W4Params &p, int n0, int leaf, int lane) : walk(p.units_per_group) {
-        const uint8_t *w = p.W + n0 * p.ldw + (int64_t)leaf * p.superleaf / 2;
-        const uint16_t *sc = p.scales + n0 * p.lds + (int64_t)leaf * p.groups_per_leaf;
-        w_ptr = uniform_pointer(reinterpret_cast<const char *>(w));
+// The scales (ELEMENT == 2) or zero points (ELEMENT == 1) of CHANNELS channels from n0 on, groups from g0 on, `groups` of them: dwords, each channel's from the aligned
+// one that holds its first element, so a channel's last dword may hold bytes behind its row.
+template <int ELEMENT, int CHANNELS>
+struct W4Groups {
+    const char *ptr;                       // aligned
+    unsigned low;                          // of the first channel's first element from there
+    int pitch, last_channel, groups, dwords, inverse;
+    unsigned at;                           // in LDS
+    int bytes;                             // of a chunk there
+
+    __device__ __forceinline__ W4Groups(const void *first, int64_t ld, int channels_left, int n, int d, int inv, unsigned where) {
+        low = (unsigned)(reinterpret_cast<uintptr_t>(first) & 3);
+        ptr = uniform_pointer(reinterpret_cast<const char *>(first) - low);
+        pitch = (int)ld * ELEMENT;
+        last_channel = channels_left - 1;
+        groups = n;
+        dwords = d;
+        inverse = inv;
+        at = where;
+        bytes = w4_chunk_bytes(CHANNELS, d);
+    }
+    // Byte of channel c's first element from ptr.
+    __device__ __forceinline__ unsigned start(int c) const { return low + (unsigned)(min(c, last_channel) * pitch); }
+    __device__ __forceinline__ void issue(int chunk, int lane) const {
+        const unsigned first = chunk * W4_CHUNK * ELEMENT;
+        for (int j = 0; j * 64 < CHANNELS * dwords; ++j) {
+            const int i = min(j * 64 + lane, CHANNELS * dwords - 1), c = (i * inverse) >> 16, d = i - c * dwords;
+            const unsigned s = start(c), end = (s + groups * ELEMENT - 1) & ~3u;               // the dword of the last element
+            load_4B_per_lane_to_lds<0, true>(ptr, min(((s + first) & ~3u) + d * 4, end), at + (chunk & 1) * bytes + j * 256);
+        }
+    }
+    // Element of group g (uniform) of channel c, whose start is s: its dword, shifted down.
+    __device__ __forceinline__ unsigned read(const unsigned char *chunks, int g, int c, unsigned s) const {
+        const int chunk = g / W4_CHUNK;
+        const unsigned byte = (s & 3) + (g % W4_CHUNK) * ELEMENT;                              // a chunk's bytes are a multiple of four
+        return *reinterpret_cast<const unsigned *>(chunks + (chunk & 1) * bytes + (c * dwords + (byte >> 2)) * 4) >> (8 * (byte & 3));
+    }
+};
+
+// One wavefront's stream: the weight of 16 NB channels from n0 on, superleaves from `leaf` on, `leaves` of them; their scales and zero points.
+template <bool ZEROS, int S, int NB = 2>
+struct W4Stream {
+    static constexpr int LOADS = S * NB / 2, BYTES = LOADS * 1024;             // of a stage
+    static_assert(LOADS >= 1, "whole loads");
+    const char *w_ptr;
+    unsigned w_off[LOADS];                 // of the lane
+    W4Groups<2, 16 * NB> scales;
+    W4Groups<1, 16 * NB> zeros;
+    const unsigned char *group_at;         // both in LDS, the zero points behind the scales
+
+    static __device__ __forceinline__ int scale_bytes(const W4Params &p, int leaves) { return w4_chunk_buffers(leaves * p.groups_per_leaf) * w4_chunk_bytes(16 * NB, p.s_dwords); }
+    // group_lds, group_at: LDS for the chunks, p.group_bytes.
+    __device__ __forceinline__ W4Stream(const W4Params &p, int n0, int leaf, int leaves, int lane, unsigned group_lds, const unsigned char *groups)
+        : scales(p.scales + n0 * p.lds + (int64_t)leaf * p.groups_per_leaf, p.lds, p.N - n0, leaves * p.groups_per_leaf, p.s_dwords, p.s_inverse, group_lds),
+          zeros(ZEROS ? p.zeros + n0 * p.ldz + (int64_t)leaf * p.groups_per_leaf : nullptr, p.ldz, p.N - n0, leaves * p.groups_per_leaf, p.z_dwords, p.z_inverse,
+                group_lds + scale_bytes(p, leaves)),
+          group_at(groups) {
+        w_ptr = uniform_pointer(reinterpret_cast<const char *>(p.W + n0 * p.ldw + (int64_t)leaf * p.superleaf / 2));
 #pragma unroll
-        for (int j = 0; j < W_LOADS; ++j) {      // 64 chunks each, 2 S of a channel
+        for (int j = 0; j < LOADS; ++j) {  // 64 chunks each, 2 S of a channel
             const int r = j * (32 / S) + lane / (2 * S), c = (lane % (2 * S)) ^ w_swizzle<S>(r);
             w_off[j] = (unsigned)(min(r, p.N - 1 - n0) * (int)p.ldw + c * 16);
         }
-        const int channel = min(lane & 31 & (16 * NB - 1), p.N - 1 - n0);
-        const unsigned s_low = (unsigned)(reinterpret_cast<uintptr_t>(sc) & 3);
-        s_ptr = uniform_pointer(reinterpret_cast<const char *>(sc) - s_low);
-        s_off = s_low + (unsigned)(channel * (int)p.lds) * 2u;
-        z_ptr = nullptr;
-        z_off = 0;
-        if constexpr (ZEROS) {
-            const uint8_t *z = p.zeros + n0 * p.ldz + (int64_t)leaf * p.groups_per_leaf;
-            const unsigned z_low = (unsigned)(reinterpret_cast<uintptr_t>(z) & 3);
-            z_ptr = uniform_pointer(reinterpret_cast<const char *>(z) - z_low);
-            z_off = z_low + (unsigned)(channel * (int)p.ldz);
-        }
     }
-    // The next stage's loads to LDS address `at` (uniform): weight, scales, zero points.  A scale's dword holds its neighbour too.
-    // `more`: there is a stage behind it; else the next issue loads it again.
-    __device__ __forceinline__ void issue(unsigned at, int lane, bool more) {
+    __device__ __forceinline__ void issue_groups(int chunk, int lane) const {
+        scales.issue(chunk, lane);
+        if constexpr (ZEROS) zeros.issue(chunk, lane);
+    }
+    // The next stage's loads to LDS address `where` (uniform).  `more`: there is a stage behind it; else the next issue loads it again.
+    __device__ __forceinline__ void issue(unsigned where, bool more) {
 #pragma unroll
-        for (int j = 0; j < W_LOADS; ++j) load_16B_per_lane_to_lds<0, true>(w_ptr, w_off[j], at + j * 1024);
-        GroupWalk behind = walk;
-#pragma unroll
-        for (int q = 0; q < PAIRS; ++q) {
-            int g = behind.g;
-            behind.next();
-            if constexpr (UNITS > 1) {
-                if (lane >= 32) g = behind.g;
-                behind.next();
-            }
-            load_4B_per_lane_to_lds<0, true>(s_ptr, (s_off + 2u * g) & ~3u, at + SCALES + q * 256);
-            if constexpr (ZEROS) load_4B_per_lane_to_lds<0, true>(z_ptr, (z_off + g) & ~3u, at + ZERO_POINTS + q * 256);
-        }
-        if (more) {
-            walk = behind;
-            w_ptr += 32 * S;
-        }
-    }
-    // From the stage at `st` in LDS, for unit u of it, which is group g's.  low: where in its dword the channel's first one lies, s_off or z_off of lane `channel`.
-    template <bool F16>
-    __device__ __forceinline__ ZeroPoint<F16, ZEROS> zero(const unsigned char *st, int u, int g, int channel, unsigned low) const {
-        const unsigned z = *reinterpret_cast<const unsigned *>(st + ZERO_POINTS + (u * 32 + channel) * 4);
-        return ZeroPoint<F16, ZEROS>((int)((z >> (8u * ((low + g) & 3u))) & 15u));
-    }
-    template <bool F16>
-    __device__ __forceinline__ float scale(const unsigned char *st, int u, int g, int channel, unsigned low) const {
-        const unsigned s = *reinterpret_cast<const unsigned *>(st + SCALES + (u * 32 + channel) * 4);
-        return widened_16<F16>((uint16_t)(s >> (8u * ((low + 2u * g) & 2u)))) * kLevelUnit<F16, ZEROS>;
+        for (int j = 0; j < LOADS; ++j) load_16B_per_lane_to_lds<0, true>(w_ptr, w_off[j], where + j * 1024);
+        if (more) w_ptr += 32 * S;
     }
 };
 
@@ -279,25 +296,33 @@ struct W4Stream {
 // goes through its scale into acc.  lane % 16: the row of X and the channel of a block; quarter: lane / 16.
 template <int UNIT, bool F16, bool ZEROS, int S, int MR, int NB = 2>
 struct W4Multiplier {
-    using Stream = W4Stream<UNIT, ZEROS, S, NB>;
+    using Stream = W4Stream<ZEROS, S, NB>;
     static constexpr int UNITS = 64 * S / UNIT, STEPS = UNIT / 32;      // units of a stage, instructions of a unit
-    unsigned s_low[NB], z_low[NB];
+    unsigned s_start[NB], z_start[NB];
     int w_at[NB], w_sw, l16, quarter;
+    const unsigned char *scales, *zeros;   // in LDS
+    int asked;                             // chunks of them
     GroupWalk walk;
     W4Sums<MR, NB> sum;
 
-    // All 64 lanes of the wavefront.
     __device__ __forceinline__ W4Multiplier(const W4Params &p, const Stream &stream, int lane) : walk(p.units_per_group) {
         l16 = lane & 15;
         quarter = lane >> 4;
         w_sw = w_swizzle<S>(l16);                          // of both of the lane's channels
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            s_low[b] = __shfl(stream.s_off, b * 16 + l16);
-            z_low[b] = ZEROS ? __shfl(stream.z_off, b * 16 + l16) : 0u;
+            s_start[b] = stream.scales.start(b * 16 + l16);
+            z_start[b] = ZEROS ? stream.zeros.start(b * 16 + l16) : 0u;
             w_at[b] = (b * 16 + l16) * (32 * S);
         }
+        scales = stream.group_at;
+        zeros = stream.group_at + (stream.zeros.at - stream.scales.at);
+        asked = 1;
         sum.clear();
+    }
+    // Ahead of a stage: asks for the chunk behind the one in use, whose place the chunk before that has left.
+    __device__ __forceinline__ void prefetch_groups(const Stream &stream, int lane) {
+        if (asked < walk.g / W4_CHUNK + 2 && asked * W4_CHUNK < stream.scales.groups) stream.issue_groups(asked++, lane);
     }
     __device__ __forceinline__ void stage(const Stream &stream, const unsigned char *st, const unsigned char *const (&x_rows)[MR], int x_sw, W4Sums<MR, NB> &acc) {
 #pragma unroll
@@ -327,7 +352,7 @@ struct W4Multiplier {
             ZeroPoint<F16, ZEROS> zero[NB];
             if constexpr (ZEROS) {
 #pragma unroll
-                for (int b = 0; b < NB; ++b) zero[b] = stream.template zero<F16>(st, u, walk.g, b * 16 + l16, z_low[b]);
+                for (int b = 0; b < NB; ++b) zero[b] = ZeroPoint<F16, ZEROS>((int)(stream.zeros.read(zeros, walk.g, b * 16 + l16, z_start[b]) & 15u));
             }
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
@@ -346,7 +371,7 @@ struct W4Multiplier {
             if (walk.next()) {
 #pragma unroll
                 for (int b = 0; b < NB; ++b) {
-                    const float scale = stream.template scale<F16>(st, u, g, b * 16 + l16, s_low[b]);
+                    const float scale = widened_16<F16>((uint16_t)stream.scales.read(scales, g, b * 16 + l16, s_start[b])) * kLevelUnit<F16, ZEROS>;
 #pragma unroll
                     for (int a = 0; a < MR; ++a)
 #pragma unroll

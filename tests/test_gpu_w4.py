@@ -100,6 +100,26 @@ def test_batch_and_shards(K, leaf, k_first, group, dtype, zeros):
         assert torch.equal(bits(tb.tbik_tree_combine(torch.stack(halves), out_dtype=torch.float32)), bits(want))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("K,leaf,k_first,group", [(12288, 256, 3, 32), (8192, 64, 1, 32), (6144, 64, 3, 96), (14336, 256, 7, 64)])
+def test_more_groups_than_a_chunk_of_scales(K, leaf, k_first, group, dtype, zeros):
+    """Every wavefront walks more groups than are held at once; scales and zero points at odd addresses; one row to many, one shard."""
+    X, Wq, scales, z = operands(150, 40, K, group, dtype, zeros, K + group)
+    sw = torch.zeros((40, K // group + 3), dtype=dtype, device=DEV)
+    sw[:, 1:-2] = scales
+    zw = torch.zeros((40, K // group + 6), dtype=torch.uint8, device=DEV)
+    if zeros:
+        zw[:, 3:-3] = z
+        z = zw[:, 3:-3]
+    W = weight(Wq, scales, z)
+    want = tb.tbik_gemm_shard_partials_w4(X, Wq, sw[:, 1:-2], leaf, k_first, 1, zeros=z)[0]
+    check(want, X, W, K)
+    for rows in (1, 7, 16, 20, 50, 100):
+        assert torch.equal(bits(tb.tbik_gemm_shard_partials_w4(X[:rows], Wq, scales, leaf, k_first, 1, zeros=z)[0]), bits(want[:rows])), rows
+        assert torch.equal(bits(tb.tbik_gemm_w4(X[:rows], Wq, sw[:, 1:-2], leaf, k_first, zeros=z, out_dtype=torch.float32)), bits(want[:rows])), rows
+
+
 def test_less_workspace_and_the_general_kernel():
     """The split of K follows the room; operands too far apart for the kernels with direct loads go another way: the same bits."""
     X, Wq, scales, z = operands(40, 256, 4096, 64, torch.bfloat16, True, 7)
