@@ -61,11 +61,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_grouped_slice_kernel(const
     const int li = lane & 31, lg = lane >> 5;
     GroupMap<SLICE_ROWS> map;
     map.read(p.offsets, p.groups, p.M, lane);
-    const int tile = blockIdx.x / p.slices;
+    // With the activation a slice takes half a cache line of gate columns and half of one of up columns: two neighbours, which read the same lines, run on one
+    // XCD (workgroups go to the eight in turn), or each fetches them for itself.
+    int block = blockIdx.x;
+    if (p.swiglu && (block | 15) < (int)gridDim.x) block = (block & ~15) + (block & 7) * 2 + ((block >> 3) & 1);
+    const int tile = block / p.slices;
     if (tile >= map.tiles) return;                                     // the grid is for any division of the rows
     const GroupRows at = map.at(tile);
     const int tile_rows = min(at.end - at.first, SLICE_ROWS);
-    const int c0 = (blockIdx.x % p.slices) * (p.swiglu ? SLICE_COLUMNS / 2 : SLICE_COLUMNS);      // first column of the output
+    const int c0 = (block % p.slices) * (p.swiglu ? SLICE_COLUMNS / 2 : SLICE_COLUMNS);      // first column of the output
     const int64_t kbase = blockIdx.y * p.k_per_shard;
 
     f32x16 acc[2];
@@ -264,8 +268,10 @@ hipError_t launch_gemm_grouped_slice(const GroupedArgs &a, hipStream_t s) {
     if (!gemm_grouped_slice_supports(a)) return hipErrorInvalidValue;
     const int ns = a.ns / a.P;
     const int64_t blocks = slices_of(a) * grouped_tiles(a, SLICE_ROWS);
-    // Eight wavefronts along K, one workgroup to a compute unit, while there are no more workgroups than compute units; else four, two workgroups.
-    const int waves = blocks * a.P <= 256 && ns > 4 ? 8 : 4;
+    // While there are no more workgroups than compute units, one has all of LDS: eight wavefronts along K, or with few superleaves four and a ring twice as deep;
+    // else four, two workgroups to a compute unit.
+    const bool alone = blocks * a.P <= 256;
+    const int waves = alone && ns > 4 ? 8 : 4;
     SliceParams p;
     p.X = a.X; p.W = a.W; p.offsets = a.offsets; p.rows = a.rows;
     p.partials = a.partials; p.Y = a.Y;
@@ -284,6 +290,7 @@ hipError_t launch_gemm_grouped_slice(const GroupedArgs &a, hipStream_t s) {
     const int bytes = a.partials || p.y_f32 ? 16 : 8;                            // of four columns
     p.vector_stores = (reinterpret_cast<uintptr_t>(out) & (bytes - 1)) == 0 && ld % 4 == 0;
     if (waves == 8) return a.x_dtype == TBIK_F16 ? launch_slices<8, 3, true>(a, p, (unsigned)blocks, s) : launch_slices<8, 3, false>(a, p, (unsigned)blocks, s);
+    if (alone) return a.x_dtype == TBIK_F16 ? launch_slices<4, 6, true>(a, p, (unsigned)blocks, s) : launch_slices<4, 6, false>(a, p, (unsigned)blocks, s);
     return a.x_dtype == TBIK_F16 ? launch_slices<4, 3, true>(a, p, (unsigned)blocks, s) : launch_slices<4, 3, false>(a, p, (unsigned)blocks, s);
 }
 

@@ -1251,11 +1251,15 @@ int tbik_route_topk(const void *logits, int64_t ldl, tbik_dtype dtype, int T, in
     return e == hipSuccess ? TBIK_OK : hip_fail(e);
 }
 
-// The kernel of a grouped call by the rows that a group has in the mean (the device knows each one's): slices up to 32 rows, else tiles.
+// The kernel of a grouped call, by the tiles of 64 rows and 128 columns that the call may have (the device knows each group's rows): less than compute units,
+// slices, which divide a group's columns further and K among wavefronts; up to two for each, tiles of 64 rows; more, tiles of 128.  What decides is the weights'
+// stream up to about 64 rows a group, and the matrix instructions beyond.  Slices / 64 / 128 rows, us, one token on 8 of 128 experts: gate/up 2048 x 1536 13.7 /
+// 14.7 / 17.8, second product 768 x 2048 8.3 / 9.7 / 10.8; on 8 of 64: gate/up 4096 x 4096 69.5 / 55.6 / 60.8, second product 2048 x 4096 30.5 / 29.7 / 35.4.  64 tokens
+// on 4 of 64 experts each: 413 / 348 / 333, 172 / 158 / 156; 1024: 1205 / 555 / 502, 358 / 257 / 242; 1500 on 4 of 16: 766 / 397 / 310.
 static int grouped_kernel(const GroupedArgs &a) {
     const bool slices = gemm_grouped_slice_supports(a), tiles64 = gemm_grouped_tiled_supports(a, VARIANT_T64), tiles128 = gemm_grouped_tiled_supports(a, VARIANT_T128);
-    const int64_t mean = a.M / a.groups;
-    int wanted = mean <= 32 ? VARIANT_T32 : mean <= 96 ? VARIANT_T64 : VARIANT_T128;
+    const int64_t items = ((int64_t)a.N + 127) / 128 * grouped_tiles(a, 64) * a.P;
+    int wanted = items < 256 ? VARIANT_T32 : items <= 512 ? VARIANT_T64 : VARIANT_T128;
     const int forced = g_forced_variant.load();
     if (forced == VARIANT_REFERENCE) return VARIANT_REFERENCE;
     if (forced == VARIANT_T32 || forced == VARIANT_T64 || forced == VARIANT_T128) wanted = forced;
