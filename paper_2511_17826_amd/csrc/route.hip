@@ -1,14 +1,14 @@
 // The router of a mixture of experts: the k largest logits of each token, their weights, and the order in which products grouped
 // by expert take the tokens.
 //
-// A token is one wavefront's work whatever the batch: each lane holds every 64th logit as a key that orders like it (NaN lowest), and
-// k times the largest key is found with the row's data-parallel moves and the lowest index among its owners with ballots.  The
-// order needs no sort: a token chooses an expert at most once, so a block of 64 tokens is one 64-bit mask per expert, and a
+// A token is one wavefront's work whatever the batch: each lane holds every 64th logit as a key that orders like it (NaN lowest), largest first, and
+// k times the largest of the lanes' first keys is found with data-parallel moves and its owner with a ballot.  The
+// order needs no sort: a token chooses an expert at most once, so a block of up to 64 tokens is one 64-bit mask per expert, and a
 // choice's place is the expert's first row + what earlier blocks have + the bits below the token's in the mask.  Masks are
 // joined with integer "or", counts are sums of integers: nothing depends on the order in which wavefronts run.
 //
 // Bound by launches and latency: 8191 tokens of 128 experts read 2 MB.  Up to 64 tokens are one workgroup and one launch; more are
-// two launches, a block of 64 tokens each (select), then every block adds up the blocks' counts (a byte per expert and block) for itself (place).
+// two launches, a block of 32 tokens each (select), then every block adds up the blocks' counts (a byte per expert and block) for itself (place).
 #include "tbik_device.hpp"
 #include "tbik_internal.hpp"
 
@@ -16,8 +16,9 @@ namespace tbik {
 
 namespace {
 
-constexpr int ROUTE_TOKENS = 64;           // of a block: bits of a mask
-constexpr int ROUTE_WAVES = 16;
+constexpr int ROUTE_ALONE = 64;            // tokens of a block that is the whole batch: bits of a mask
+constexpr int ROUTE_TOKENS = 32;           // of a block of many: 8192 tokens are a block for each compute unit
+constexpr int TOKENS_PER_WAVE = 4;
 
 // Orders like the float; NaN below everything else, the two zeros equal.  0 is no float's key: a logit that has been chosen, or a lane
 // without one.
@@ -31,17 +32,29 @@ __device__ __forceinline__ float logit_of(uint32_t key) {
     return __uint_as_float((key & 0x80000000u) ? key & 0x7fffffffu : ~key);
 }
 
+// The largest of 64 lanes' values: within rows of 16 by shifts, then from row to row; lane 63 has it.  Six instructions and a move to a scalar register.
 template <int CTRL>
-__device__ __forceinline__ uint32_t from_lane_in_row_u32(uint32_t v) {
-    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false);
-}
+__device__ __forceinline__ uint32_t max_with(uint32_t v) { return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false)); }
 __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
-    v = max(v, from_lane_in_row_u32<0xB1>(v));
-    v = max(v, from_lane_in_row_u32<0x4E>(v));
-    v = max(v, from_lane_in_row_u32<0x141>(v));
-    v = max(v, from_lane_in_row_u32<0x140>(v));
-    const uint32_t r0 = __builtin_amdgcn_readlane(v, 0), r1 = __builtin_amdgcn_readlane(v, 16), r2 = __builtin_amdgcn_readlane(v, 32), r3 = __builtin_amdgcn_readlane(v, 48);
-    return max(max(r0, r1), max(r2, r3));
+    v = max_with<0x111>(v);                            // row_shr 1, 2, 4, 8
+    v = max_with<0x112>(v);
+    v = max_with<0x114>(v);
+    v = max_with<0x118>(v);
+    v = max_with<0x142>(v);                            // row_bcast 15, 31
+    v = max_with<0x143>(v);
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+
+// Sums up to and with each lane's, and of all 64 in lane 63.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int plus(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int wave_scan(int v) {
+    v = plus<0x111, 0xf>(v);                           // within rows of 16: row_shr 1, 2, 4, 8
+    v = plus<0x112, 0xf>(v);
+    v = plus<0x114, 0xf>(v);
+    v = plus<0x118, 0xf>(v);
+    v = plus<0x142, 0xa>(v);                           // row_bcast 15 to rows 1 and 3, 31 to rows 2 and 3
+    return plus<0x143, 0xc>(v);
 }
 
 struct RouteParams {
@@ -58,89 +71,155 @@ struct RouteParams {
     int pitch, blocks;
 };
 
-__device__ __forceinline__ float logit_at(const RouteParams &p, int64_t i) {
-    if (p.dtype == TBIK_F32) return reinterpret_cast<const float *>(p.logits)[i];
-    const uint16_t h = reinterpret_cast<const uint16_t *>(p.logits)[i];
-    return p.dtype == TBIK_F16 ? (float)__builtin_bit_cast(_Float16, h) : bf16_bits_to_f32(h);
+__device__ __forceinline__ uint32_t raw_logit(const RouteParams &p, int64_t i) {
+    return p.dtype == TBIK_F32 ? reinterpret_cast<const uint32_t *>(p.logits)[i] : reinterpret_cast<const uint16_t *>(p.logits)[i];
+}
+__device__ __forceinline__ float logit_of_raw(uint32_t raw, int dtype) {
+    return dtype == TBIK_F32 ? __uint_as_float(raw) : dtype == TBIK_F16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)raw) : bf16_bits_to_f32(raw);
 }
 
-// A token's choices: lane j (j < k) gets expert and weight of choice j.  The weights: e^(l_j - l_0) over the sum of the chosen, ascending j, or
-// over the sum of all experts (lane-wise chains in ascending expert order, then the tree over the lanes).
-template <int PER_LANE>
-__device__ __forceinline__ void choose(const RouteParams &p, int t, int lane, int *expert, float *weight) {
-    uint32_t key[PER_LANE];
+// The choices of TOKENS tokens, t[i] of them below p.T (the others repeat one): lane j (j < k) gets expert and weight of choice j.  The weights: e^(l_j - l_0)
+// over the sum of the chosen, ascending j, or over the sum of all experts (lane-wise chains in ascending expert order, then the tree over the lanes).
+// A token's rounds wait for each other, of the moves and ballots that each consists of; four tokens at once fill the gaps.
+template <int PER_LANE, int TOKENS>
+__device__ __forceinline__ void choose(const RouteParams &p, const int (&t)[TOKENS], int lane, int (&expert)[TOKENS], float (&weight)[TOKENS]) {
+    // A lane's logits in falling order, the lower expert first among equals: a round looks at the lanes' first ones alone.
+    uint32_t key[TOKENS][PER_LANE];
+    int index[TOKENS][PER_LANE];
+    // All loads before the first use (one branch by type around them; behind the last expert it is read once more).
+    if (p.dtype == TBIK_F32) {
 #pragma unroll
-    for (int j = 0; j < PER_LANE; ++j) {
-        const int e = j * 64 + lane;
-        key[j] = e < p.E ? key_of(logit_at(p, (int64_t)t * p.ldl + e)) : 0u;
+        for (int i = 0; i < TOKENS; ++i)
+#pragma unroll
+            for (int j = 0; j < PER_LANE; ++j) key[i][j] = reinterpret_cast<const uint32_t *>(p.logits)[(int64_t)t[i] * p.ldl + min(j * 64 + lane, p.E - 1)];
+    } else {
+#pragma unroll
+        for (int i = 0; i < TOKENS; ++i)
+#pragma unroll
+            for (int j = 0; j < PER_LANE; ++j) key[i][j] = reinterpret_cast<const uint16_t *>(p.logits)[(int64_t)t[i] * p.ldl + min(j * 64 + lane, p.E - 1)];
     }
-    float all = 0.0f;
-    uint32_t first = 0, mine = 0;
-    int chosen = 0;
-    for (int i = 0; i < p.k; ++i) {
-        uint32_t best = key[0];
 #pragma unroll
-        for (int j = 1; j < PER_LANE; ++j) best = max(best, key[j]);
-        best = wave_max_u32(best);
-        if (i == 0) {
-            first = best;
-            if (!p.renormalize) {
-#pragma unroll
-                for (int j = 0; j < PER_LANE; ++j)
-                    if (j * 64 + lane < p.E) all = all + expf(logit_of(key[j]) - logit_of(first));
-                all = wave_tree_sum(all);
-            }
-        }
-        int winner = -1;
+    for (int i = 0; i < TOKENS; ++i)
 #pragma unroll
         for (int j = 0; j < PER_LANE; ++j) {
-            const uint64_t owners = __builtin_amdgcn_ballot_w64(key[j] == best);
-            if (winner < 0 && owners) {
-                const int at = __builtin_ctzll(owners);
-                winner = j * 64 + at;
-                if (lane == at) key[j] = 0u;
+            const int e = j * 64 + lane;
+            key[i][j] = e < p.E ? key_of(logit_of_raw(key[i][j], p.dtype)) : 0u;
+            index[i][j] = e;
+        }
+#pragma unroll
+    for (int i = 0; i < TOKENS; ++i)
+#pragma unroll
+        for (int n = 1; n < PER_LANE; ++n)
+#pragma unroll
+            for (int j = n; j > 0; --j) {              // into its place among the n before it
+                const bool swap = key[i][j] > key[i][j - 1];
+                const uint32_t high = swap ? key[i][j] : key[i][j - 1], low = swap ? key[i][j - 1] : key[i][j];
+                const int first = swap ? index[i][j] : index[i][j - 1], second = swap ? index[i][j - 1] : index[i][j];
+                key[i][j - 1] = high;
+                key[i][j] = low;
+                index[i][j - 1] = first;
+                index[i][j] = second;
+            }
+    float all[TOKENS];
+    uint32_t first[TOKENS], mine[TOKENS];
+#pragma unroll
+    for (int i = 0; i < TOKENS; ++i) {
+        all[i] = 0.0f;
+        first[i] = mine[i] = 0u;
+        expert[i] = 0;
+    }
+    if (!p.renormalize) {                              // in ascending expert order, from memory once more
+#pragma unroll
+        for (int i = 0; i < TOKENS; ++i) {
+            const float top = logit_of(wave_max_u32(key[i][0]));
+#pragma unroll
+            for (int j = 0; j < PER_LANE; ++j)
+                if (j * 64 + lane < p.E) all[i] = all[i] + expf(logit_of_raw(raw_logit(p, (int64_t)t[i] * p.ldl + j * 64 + lane), p.dtype) - top);
+            all[i] = wave_tree_sum(all[i]);
+        }
+    }
+    for (int round = 0; round < p.k; ++round) {
+        uint32_t best[TOKENS];
+#pragma unroll
+        for (int i = 0; i < TOKENS; ++i) best[i] = wave_max_u32(key[i][0]);
+#pragma unroll
+        for (int i = 0; i < TOKENS; ++i) {
+            if (round == 0) first[i] = best[i];
+            const uint64_t owners = __builtin_amdgcn_ballot_w64(key[i][0] == best[i]);
+            uint64_t lowest = owners;                              // of several, those of the first block of 64 experts that has one
+#pragma unroll
+            for (int j = PER_LANE - 1; j > 0; --j) {
+                const uint64_t low = owners & __builtin_amdgcn_ballot_w64(index[i][0] < 64 * j);
+                lowest = low ? low : lowest;
+            }
+            const int at = __builtin_ctzll(lowest);
+            const int winner = __builtin_amdgcn_readlane(index[i][0], at);
+            if (lane == round) {
+                mine[i] = best[i];
+                expert[i] = winner;
+            }
+            const bool taken = lane == at;
+#pragma unroll
+            for (int j = 0; j < PER_LANE; ++j) {
+                key[i][j] = taken ? (j + 1 < PER_LANE ? key[i][j + 1] : 0u) : key[i][j];
+                if (j + 1 < PER_LANE) index[i][j] = taken ? index[i][j + 1] : index[i][j];
             }
         }
-        if (lane == i) {
-            mine = best;
-            chosen = winner;
+    }
+#pragma unroll
+    for (int i = 0; i < TOKENS; ++i) {
+        const float top = logit_of(first[i]);
+        const float e = lane < p.k ? expf(logit_of(mine[i]) - top) : 0.0f;
+        float sum = all[i];
+        if (p.renormalize) {
+            sum = 0.0f;
+            for (int j = 0; j < p.k; ++j) sum = sum + __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, e), j));
         }
+        weight[i] = top == -__builtin_inff() ? 0.0f : e / sum;       // nothing to choose from: no weight
     }
-    const float top = logit_of(first);
-    const float e = lane < p.k ? expf(logit_of(mine) - top) : 0.0f;
-    float sum = all;
-    if (p.renormalize) {
-        sum = 0.0f;
-        for (int i = 0; i < p.k; ++i) sum = sum + __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, e), i));
-    }
-    *weight = top == -__builtin_inff() ? 0.0f : e / sum;       // nothing to choose from: no weight
-    *expert = chosen;
 }
 
 // ALONE: one block is the whole batch, and places its choices itself.
 template <int PER_LANE, bool ALONE>
-__global__ __launch_bounds__(64 * ROUTE_WAVES) void route_select_kernel(const RouteParams p) {
+__global__ __launch_bounds__(64 * (ALONE ? ROUTE_ALONE : ROUTE_TOKENS) / TOKENS_PER_WAVE) void route_select_kernel(const RouteParams p) {
+    constexpr int BLOCK_TOKENS = ALONE ? ROUTE_ALONE : ROUTE_TOKENS, WAVES = BLOCK_TOKENS / TOKENS_PER_WAVE;
     __shared__ uint64_t mask[PER_LANE * 64];
     __shared__ int32_t first_row[ALONE ? PER_LANE * 64 : 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int t0 = blockIdx.x * ROUTE_TOKENS;
-    const int tokens = min(ROUTE_TOKENS, p.T - t0);
-    for (int e = threadIdx.x; e < PER_LANE * 64; e += 64 * ROUTE_WAVES) mask[e] = 0;
+    const int t0 = blockIdx.x * BLOCK_TOKENS;
+    const int tokens = min(BLOCK_TOKENS, p.T - t0);
+    for (int e = threadIdx.x; e < PER_LANE * 64; e += 64 * WAVES) mask[e] = 0;
     __syncthreads();
-    for (int i = wave; i < tokens; i += ROUTE_WAVES) {
-        int expert;
-        float weight;
-        choose<PER_LANE>(p, t0 + i, lane, &expert, &weight);
-        if (lane < p.k) {
+    auto keep = [&](int i, int expert, float weight) __attribute__((always_inline)) {
+        if (lane < p.k && i < tokens) {
             const int64_t at = (int64_t)(t0 + i) * p.k + lane;
             p.experts[at] = expert;
             p.weights[at] = weight;
             atomicOr(reinterpret_cast<unsigned long long *>(&mask[expert]), 1ull << i);
         }
+    };
+    if (tokens <= WAVES) {                             // one each: no gaps to fill
+        if (wave < tokens) {
+            int expert[1];
+            float weight[1];
+            choose<PER_LANE, 1>(p, {t0 + wave}, lane, expert, weight);
+            keep(wave, expert[0], weight[0]);
+        }
+    } else {
+        constexpr int TOKENS = PER_LANE < 8 ? TOKENS_PER_WAVE : ALONE ? 1 : 2;              // at once: what the registers hold
+        for (int from = wave; from < tokens; from += TOKENS * WAVES) {
+            int t[TOKENS], expert[TOKENS];
+            float weight[TOKENS];
+#pragma unroll
+            for (int i = 0; i < TOKENS; ++i) t[i] = min(t0 + from + i * WAVES, p.T - 1);
+            choose<PER_LANE, TOKENS>(p, t, lane, expert, weight);
+#pragma unroll
+            for (int i = 0; i < TOKENS; ++i) keep(from + i * WAVES, expert[i], weight[i]);
+        }
     }
     __syncthreads();
     if constexpr (!ALONE) {
-        for (int e = threadIdx.x; e < p.pitch; e += 64 * ROUTE_WAVES) {
+        for (int e = threadIdx.x; e < p.pitch; e += 64 * WAVES) {
             const uint64_t m = e < p.E ? mask[e] : 0;
             if (e < p.E) p.masks[(int64_t)blockIdx.x * p.E + e] = m;
             p.counts[(int64_t)blockIdx.x * p.pitch + e] = (uint8_t)__popcll(m);
@@ -151,12 +230,7 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES) void route_select_kernel(const Ro
 #pragma unroll
             for (int j = 0; j < PER_LANE; ++j) {
                 const int e = j * 64 + lane, n = __popcll(mask[e]);
-                int sum = n;
-#pragma unroll
-                for (int d = 1; d < 64; d *= 2) {
-                    const int up = __shfl_up(sum, d);
-                    if (lane >= d) sum += up;
-                }
+                const int sum = wave_scan(n);
                 first_row[e] = before + sum - n;
                 if (e <= p.E) p.offsets[e] = before + sum - n;
                 before += __builtin_amdgcn_readlane(sum, 63);
@@ -164,7 +238,7 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES) void route_select_kernel(const Ro
             if (p.E == PER_LANE * 64 && lane == 0) p.offsets[p.E] = before;
         }
         __syncthreads();
-        for (int c = threadIdx.x; c < tokens * p.k; c += 64 * ROUTE_WAVES) {
+        for (int c = threadIdx.x; c < tokens * p.k; c += 64 * WAVES) {
             const int i = c / p.k, e = p.experts[c];
             const int row = first_row[e] + __popcll(mask[e] & ((1ull << i) - 1));
             p.rows[row] = i;
@@ -176,42 +250,68 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES) void route_select_kernel(const Ro
 constexpr int PLACE_THREADS = 512;
 
 __global__ __launch_bounds__(PLACE_THREADS) void route_place_kernel(const RouteParams p) {
-    extern __shared__ int32_t sums[];                  // [pitch] choices of all blocks, then [pitch] of the blocks before this one
-    int32_t *const total = sums, *const before = sums + p.pitch;
-    for (int e = threadIdx.x; e < 2 * p.pitch; e += PLACE_THREADS) sums[e] = 0;
-    __syncthreads();
-    // A thread adds up 16 experts' counts of every `step`-th block.
-    const int chunks = p.pitch / 16, step = PLACE_THREADS / chunks;
-    if ((int)threadIdx.x < step * chunks) {
-        const int c = threadIdx.x % chunks, b0 = threadIdx.x / chunks;
-        int all[16] = {}, early[16] = {};
-        for (int b = b0; b < p.blocks; b += step) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(p.counts + (int64_t)b * p.pitch + c * 16);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    __shared__ int32_t total[kMaxGroups], before[kMaxGroups];      // choices of all blocks; of the blocks before this one, then first rows
+    __shared__ int32_t part[2][PLACE_THREADS * 4];
+    const int t0 = blockIdx.x * ROUTE_TOKENS, tokens = min(ROUTE_TOKENS, p.T - t0);
+    const int64_t first = (int64_t)t0 * p.k;
+    const uint64_t *const masks = p.masks + (int64_t)blockIdx.x * p.E;
+    // The thread's first choice is on its way while the counts are added up.
+    int e = 0;
+    uint64_t m = 0;
+    if ((int)threadIdx.x < tokens * p.k) {
+        e = p.experts[first + threadIdx.x];
+        m = masks[e];
+    }
+    // A thread adds up four experts' counts of every `step`-th block, two of them to a register (up to 32 a block: 2047 blocks do not overflow 16 bits).
+    const int quads = p.pitch / 4, step = PLACE_THREADS / quads;
+    if ((int)threadIdx.x < step * quads) {
+        const int c = threadIdx.x % quads, own = threadIdx.x / quads;
+        const uint32_t *const counts = reinterpret_cast<const uint32_t *>(p.counts) + c;
+        int all[4] = {}, early[4] = {};
+        for (int from = own; from < p.blocks; from += 1000 * step) {
+            uint32_t even[2] = {0, 0}, odd[2] = {0, 0};            // [earlier blocks, others]
+            const int until = min(p.blocks, from + 1000 * step);
+            for (int b0 = from; b0 < until; b0 += 8 * step) {
+                uint32_t v[8];                                     // loads that do not wait for each other
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int n = (w[i >> 2] >> (8 * (i & 3))) & 0xff;
-                all[i] += n;
-                early[i] += b < (int)blockIdx.x ? n : 0;
+                for (int i = 0; i < 8; ++i) v[i] = b0 + i * step < until ? counts[(int64_t)(b0 + i * step) * quads] : 0u;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const bool ahead = b0 + i * step < (int)blockIdx.x;
+                    even[0] += ahead ? v[i] & 0x00ff00ffu : 0u;
+                    odd[0] += ahead ? (v[i] >> 8) & 0x00ff00ffu : 0u;
+                    even[1] += v[i] & 0x00ff00ffu;
+                    odd[1] += (v[i] >> 8) & 0x00ff00ffu;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                early[i] += ((i & 1 ? odd[0] : even[0]) >> (i & 2 ? 16 : 0)) & 0xffffu;
+                all[i] += ((i & 1 ? odd[1] : even[1]) >> (i & 2 ? 16 : 0)) & 0xffffu;
             }
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            if (all[i]) atomicAdd(&total[c * 16 + i], all[i]);
-            if (early[i]) atomicAdd(&before[c * 16 + i], early[i]);
+        for (int i = 0; i < 4; ++i) {
+            part[0][own * p.pitch + c * 4 + i] = all[i];
+            part[1][own * p.pitch + c * 4 + i] = early[i];
         }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < p.pitch; e += PLACE_THREADS) {
+        int a = 0, b = 0;
+        for (int i = 0; i < step; ++i) {
+            a += part[0][i * p.pitch + e];
+            b += part[1][i * p.pitch + e];
+        }
+        total[e] = a;
+        before[e] = b;
     }
     __syncthreads();
     if (threadIdx.x < 64) {                            // first rows: a scan over the experts
         int ahead = 0;
         for (int e = threadIdx.x; e - (int)threadIdx.x < p.pitch; e += 64) {
             const int n = e < p.pitch ? total[e] : 0;
-            int sum = n;
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const int up = __shfl_up(sum, d);
-                if ((int)threadIdx.x >= d) sum += up;
-            }
+            const int sum = wave_scan(n);
             if (blockIdx.x == 0 && e < p.E) p.offsets[e] = ahead + sum - n;
             if (e < p.pitch) before[e] += ahead + sum - n;
             ahead += __builtin_amdgcn_readlane(sum, 63);
@@ -219,14 +319,14 @@ __global__ __launch_bounds__(PLACE_THREADS) void route_place_kernel(const RouteP
         if (blockIdx.x == 0 && threadIdx.x == 0) p.offsets[p.E] = ahead;
     }
     __syncthreads();
-    const int t0 = blockIdx.x * ROUTE_TOKENS, tokens = min(ROUTE_TOKENS, p.T - t0);
     for (int c = threadIdx.x; c < tokens * p.k; c += PLACE_THREADS) {
-        const int i = c / p.k;
-        const int64_t at = (int64_t)t0 * p.k + c;
-        const int e = p.experts[at];
-        const int row = before[e] + __popcll(p.masks[(int64_t)blockIdx.x * p.E + e] & ((1ull << i) - 1));
+        if (c >= PLACE_THREADS) {
+            e = p.experts[first + c];
+            m = masks[e];
+        }
+        const int i = c / p.k, row = before[e] + __popcll(m & ((1ull << i) - 1));
         p.rows[row] = t0 + i;
-        p.slots[at] = row;
+        p.slots[first + c] = row;
     }
 }
 
@@ -235,7 +335,7 @@ inline int route_pitch(int E) { return (E + 15) & ~15; }
 
 template <bool ALONE>
 void launch_select(const RouteParams &p, hipStream_t s) {
-    const dim3 grid((unsigned)(ALONE ? 1 : p.blocks)), block(64 * ROUTE_WAVES);
+    const dim3 grid((unsigned)(ALONE ? 1 : p.blocks)), block(64 * (ALONE ? ROUTE_ALONE : ROUTE_TOKENS) / TOKENS_PER_WAVE);
     if (p.E <= 64) hipLaunchKernelGGL((route_select_kernel<1, ALONE>), grid, block, 0, s, p);
     else if (p.E <= 128) hipLaunchKernelGGL((route_select_kernel<2, ALONE>), grid, block, 0, s, p);
     else if (p.E <= 256) hipLaunchKernelGGL((route_select_kernel<4, ALONE>), grid, block, 0, s, p);
@@ -245,14 +345,14 @@ void launch_select(const RouteParams &p, hipStream_t s) {
 }  // namespace
 
 size_t route_topk_workspace(int T, int E) {
-    if (T <= ROUTE_TOKENS) return 0;
+    if (T <= ROUTE_ALONE) return 0;
     return (size_t)route_blocks(T) * ((size_t)E * 8 + (size_t)route_pitch(E));
 }
 
 hipError_t launch_route_topk(const void *logits, int64_t ldl, int dtype, int T, int E, int k, int renormalize, int32_t *experts, float *weights,
                              int32_t *offsets, int32_t *rows, int32_t *slots, void *workspace, hipStream_t s) {
     RouteParams p{logits, ldl, dtype, T, E, k, renormalize, experts, weights, offsets, rows, slots, nullptr, nullptr, route_pitch(E), route_blocks(T)};
-    if (T <= ROUTE_TOKENS) {
+    if (T <= ROUTE_ALONE) {
         launch_select<true>(p, s);
         return hipGetLastError();
     }
@@ -261,7 +361,7 @@ hipError_t launch_route_topk(const void *logits, int64_t ldl, int dtype, int T, 
     launch_select<false>(p, s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(route_place_kernel, dim3((unsigned)p.blocks), dim3(PLACE_THREADS), 2 * p.pitch * sizeof(int32_t), s, p);
+    hipLaunchKernelGGL(route_place_kernel, dim3((unsigned)p.blocks), dim3(PLACE_THREADS), 0, s, p);
     return hipGetLastError();
 }
 
