@@ -620,7 +620,7 @@ int tbik_route_topk(const void *logits, int64_t ldl, tbik_dtype dtype, int T, in
  *
  *   X        device, x_dtype (TBIK_BF16 or TBIK_F16), [tokens, ldx]
  *   rows     device, int32 [R], or NULL (then tokens >= R); an index outside 0 .. tokens - 1 is taken as the nearest one
- *   W        device, x_dtype, `groups` matrices [K, ldw], weight_stride elements apart (a multiple of 8; 0: the same for all); groups <= 512
+ *   W        device, x_dtype, `groups` matrices [K, ldw], weight_stride elements apart (a multiple of 8; 0: the same for all); groups <= 512, R <= 2^31 - 256
  *   offsets  device, int32 [groups + 1]; not falling and within 0 .. R; values that are not are taken as the largest before them, within 0 .. R
  *   Y        device, y_dtype (TBIK_F32 or x_dtype), [R, ldy]; act likewise, of `dtype`; partials device, fp32, dense [P, R, N]
  *   Everything else as for tbik_gemm, tbik_gemm_swiglu and tbik_gemm_shard_partials; no workspace.  tokens == 0 or groups == 0: nothing is written.
@@ -660,7 +660,8 @@ int tbik_combine_experts(const void *Y, int64_t ldy, tbik_dtype y_dtype, int P, 
  *
  *   X       device, x_dtype (TBIK_BF16 or TBIK_F16), [M, ldx], 16-byte aligned, ldx a multiple of 8
  *   Wq      device, [N, ldwq] bytes, ldwq >= K / 2 a multiple of 16, 16-byte aligned: two elements a byte, the one with the even k in the low four bits
- *   scales  device, x_dtype, [N, lds], lds >= K / group          zeros   device, bytes (the low four bits count), [N, ldz], or NULL
+ *   scales  device, x_dtype, [N, lds], lds >= K / group (bfloat16 without zeros: below 2^124, larger ones count as infinite)
+ *   zeros   device, bytes (the low four bits count), [N, ldz], or NULL
  *   group   a multiple of 32 that divides leaf * k_first; K / (leaf * k_first) / P <= 128
  *   Y       device, y_dtype (TBIK_F32 or x_dtype), [M, ldy], aligned to its type          partials   device, fp32, dense [P, M, N], 16-byte aligned
  *   workspace  tbik_gemm_w4_workspace_bytes(M, N, K, leaf, k_first) bytes, 256-byte aligned, are room for the quickest way to cut the work; less (or NULL) gives

@@ -228,7 +228,7 @@ __global__ __launch_bounds__(256 * KG, MT == 4 ? 1 : 2) void gemm_w4_tiled_kerne
 #pragma unroll
                 for (int r = 0; r < 4; ++r) patch[(q * 16 + 4 * quarter + r) * 32 + b * 16 + l16] = acc.t[2 * a + q][b][r];
         if (p.partials || p.y_f32) {
-            float *const out = p.partials ? p.partials + ((int64_t)blockIdx.z * p.M + m0) * p.N + n0 : reinterpret_cast<float *>(p.Y) + (int64_t)m0 * p.ldy + n0;
+            float *const out = p.partials ? p.partials + blockIdx.z * p.plane + (int64_t)m0 * p.N + n0 : reinterpret_cast<float *>(p.Y) + (int64_t)m0 * p.ldy + n0;
             const int64_t ld = p.partials ? p.N : p.ldy;
 #pragma unroll
             for (int it = 0; it < 4; ++it) {
@@ -424,8 +424,9 @@ hipError_t launch_slice_rows(const W4Params &all, int shards, hipStream_t s) {
         }
     }
     if (p.M > 8) return launch_slice<UNIT, F16, ZEROS, S, 16, S == 1 ? 4 : 2>(p, shards, s);
-    if (S == 1 || ((int64_t)p.N + 31) / 32 * shards <= 256) return launch_slice<UNIT, F16, ZEROS, S, 8, S == 1 ? 6 : 3>(p, shards, s);
-    return launch_slice<UNIT, F16, ZEROS, S, 8, 2>(p, shards, s);
+    if constexpr (S == 1) return launch_slice<UNIT, F16, ZEROS, 1, 8, 6>(p, shards, s);
+    else if (((int64_t)p.N + 31) / 32 * shards <= 256) return launch_slice<UNIT, F16, ZEROS, S, 8, 3>(p, shards, s);
+    else return launch_slice<UNIT, F16, ZEROS, S, 8, 2>(p, shards, s);
 }
 template <int UNIT, bool F16, bool ZEROS, int S>
 hipError_t launch_tile_rows(const W4Params &p, int shards, hipStream_t s) {
@@ -449,13 +450,12 @@ hipError_t launch_unit(const W4Args &a, const W4Params &all, hipStream_t s) {
     }
     if (kernel == W4_SLICES) return launch_slice_rows<UNIT, F16, ZEROS, 2>(p, a.P, s);
     if (kernel == W4_TILES) return launch_tile_rows<UNIT, F16, ZEROS, 2>(p, a.P, s);
-    if (p.leaves_per_wave > 16) return hipErrorInvalidValue;
     for (int64_t m0 = 0; m0 < a.M; m0 += 32 * 4096) {  // 4096 row tiles a launch
         W4Params q = p;
         q.M = (int)(a.M - m0 < 32 * 4096 ? a.M - m0 : 32 * 4096);
         q.X += m0 * a.ldx;
-        if (q.Y) q.Y = static_cast<char *>(q.Y) + m0 * a.ldy * (p.y_f32 ? 4 : 2);
-        if (q.partials && a.M > 32 * 4096) return hipErrorInvalidValue;          // planes of all rows
+        if (q.partials) q.partials += m0 * a.N;
+        else q.Y = static_cast<char *>(q.Y) + m0 * a.ldy * (p.y_f32 ? 4 : 2);
         hipLaunchKernelGGL((gemm_w4_kernel<UNIT, F16, ZEROS>), dim3((unsigned)((a.N + 31) / 32), (unsigned)((q.M + 31) / 32), (unsigned)a.P), dim3(64 * W4_WAVES), 0, s, q);
     }
     return hipGetLastError();
@@ -484,6 +484,7 @@ hipError_t launch_gemm_w4(const W4Args &a, hipStream_t s) {
     p.partials = a.partials; p.Y = a.Y;
     p.ldx = a.ldx; p.ldw = a.ldw; p.lds = a.lds; p.ldz = a.ldz; p.ldy = a.ldy;
     p.M = a.M; p.N = a.N;
+    p.plane = (int64_t)a.M * a.N;
     p.y_f32 = a.y_dtype == TBIK_F32;
     p.superleaf = a.superleaf; p.groups_per_leaf = a.superleaf / a.group;
     p.leaves_per_shard = a.ns / a.P;

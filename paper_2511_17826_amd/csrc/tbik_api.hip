@@ -1278,7 +1278,7 @@ static int gemm_grouped(tbik_dtype x_dtype, const void *X, int64_t ldx, int toke
     if (x_dtype != TBIK_BF16 && x_dtype != TBIK_F16) return TBIK_ERR_DTYPE;
     if (!partials && !legal_y_dtype((int)y_dtype, (int)x_dtype)) return TBIK_ERR_DTYPE;
     if (tokens < 0 || groups < 0 || (!rows && tokens < R)) return TBIK_ERR_SHAPE;
-    if (groups > kMaxGroups) return TBIK_ERR_UNSUPPORTED;
+    if (groups > kMaxGroups || R > 0x7fffff00) return TBIK_ERR_UNSUPPORTED;      // row tiles are counted in 32 bits
     if (R == 0 || N == 0 || groups == 0 || tokens == 0) return TBIK_OK;
     rc = check_operands((int)x_dtype, X, ldx, W, ldw, N, K);
     if (rc != TBIK_OK) return rc;
@@ -1365,8 +1365,7 @@ int tbik_rmsnorm_residual_rmsnorm(const void *y, int64_t ldy, const float *parti
 
 // Parts that K is split into where the tiles of a 4-bit product leave compute units idle: until there is a workgroup for each (and a tile
 // walks at most 16 superleaves).  Up to 16 rows are slices, which split K among their wavefronts.
-static int w4_split(int M, int N, int K, int ns) {
-    (void)K;
+static int w4_split(int M, int N, int ns) {
     if (M <= 16) return 1;
     const int rows = M <= 32 ? 32 : M <= 64 ? 64 : 128;
     const int64_t tiles = ((int64_t)N + 127) / 128 * (((int64_t)M + rows - 1) / rows);
@@ -1402,7 +1401,7 @@ static int gemm_w4(tbik_dtype x_dtype, const void *X, int64_t ldx, const void *W
     hipStream_t s = (hipStream_t)hip_stream;
     if (workspace && !aligned(workspace, 256)) return TBIK_ERR_ALIGN;
     hipError_t e;
-    int split = partials ? 1 : w4_split(M, N, K, ns);
+    int split = partials ? 1 : w4_split(M, N, ns);
     while (split > 1 && split_planes_bytes(M, N, split) > (workspace ? workspace_bytes : 0)) split /= 2;      // less room: the same bits with less of a split
     if (split > 1 && w4_kernel(a) != W4_SLICES) {
         a.partials = reinterpret_cast<float *>(workspace);
@@ -1419,7 +1418,7 @@ static int gemm_w4(tbik_dtype x_dtype, const void *X, int64_t ldx, const void *W
 size_t tbik_gemm_w4_workspace_bytes(int M, int N, int K, int leaf, int k_first) {
     int sl, ns;
     if (check_tree(M, N, K, leaf, k_first, 1, &sl, &ns) != TBIK_OK) return 0;
-    return split_planes_bytes(M, N, w4_split(M, N, K, ns));
+    return split_planes_bytes(M, N, w4_split(M, N, ns));
 }
 
 int tbik_gemm_w4(const void *X, int64_t ldx, const void *Wq, int64_t ldwq, const void *scales, int64_t lds, const void *zeros, int64_t ldz, int group,

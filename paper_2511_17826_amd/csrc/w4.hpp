@@ -19,6 +19,7 @@ struct W4Params {
     float *partials;
     void *Y;
     int64_t ldx, ldw, lds, ldz, ldy;
+    int64_t plane;                         // floats of a shard's partial sums
     int M, N;
     int y_f32;
     int superleaf, groups_per_leaf;
@@ -385,7 +386,7 @@ struct W4Multiplier {
 
 template <bool F16>
 __device__ __forceinline__ void w4_store(const W4Params &p, int shard, int row, int col, float v) {
-    if (p.partials) p.partials[((int64_t)shard * p.M + row) * p.N + col] = v;
+    if (p.partials) p.partials[shard * p.plane + (int64_t)row * p.N + col] = v;
     else if (p.y_f32) reinterpret_cast<float *>(p.Y)[(int64_t)row * p.ldy + col] = v;
     else reinterpret_cast<uint16_t *>(p.Y)[(int64_t)row * p.ldy + col] = (uint16_t)f32_to_16_bits<F16>(v);
 }

@@ -51,7 +51,7 @@ def test_route_workspace(L):
 @pytest.mark.parametrize("changes,status", [
     (dict(R=-1), SHAPE), (dict(N=-1), SHAPE), (dict(K=500), SHAPE), (dict(leaf=8), SHAPE), (dict(tokens=-1), SHAPE), (dict(groups=-1), SHAPE),
     (dict(rows=None), SHAPE),                   # 10 tokens, 20 rows
-    (dict(ldx=504), SHAPE), (dict(ldw=248), SHAPE), (dict(ldy=255), SHAPE), (dict(stride=-8), SHAPE), (dict(groups=513), UNSUPPORTED),
+    (dict(ldx=504), SHAPE), (dict(ldw=248), SHAPE), (dict(ldy=255), SHAPE), (dict(stride=-8), SHAPE), (dict(groups=513), UNSUPPORTED), (dict(R=0x7fffff01), UNSUPPORTED),
     (dict(x_dtype=F32, y_dtype=F32), DTYPE), (dict(x_dtype=5), DTYPE), (dict(y_dtype=F16), DTYPE), (dict(X=None), NULL), (dict(W=None), NULL), (dict(offsets=None), NULL),
     (dict(Y=None), NULL), (dict(X=A + 8), ALIGN), (dict(W=A + 8), ALIGN), (dict(ldx=516), ALIGN), (dict(ldw=260), ALIGN), (dict(stride=512 * 256 + 4), ALIGN),
     (dict(offsets=A + 2), ALIGN), (dict(rows=A + 2), ALIGN), (dict(Y=A + 1), ALIGN), (dict(Y=A + 2, y_dtype=F32), ALIGN),
