@@ -655,8 +655,8 @@ int tbik_combine_experts(const void *Y, int64_t ldy, tbik_dtype y_dtype, int P, 
  *   W[k][n] = scales[n][k / group] (q[n][k] - zeros[n][k / group])         zeros NULL: 8 everywhere
  * Per output element and superleaf: for the groups in ascending k, acc = fma(scale, S, acc) in fp32 from +0, S the group's products x (q - zero) accumulated
  * in fp32 from +0 (q - zero is exact in 16 bits, so the weight is never rounded); the superleaf sums are combined by T, the result is rounded once.  (The 32
- * products of one matrix instruction are added in that instruction's own fixed order, as for the other formats; of each 128 consecutive k -- 64 or 32, where 128
- * does not divide the group -- instruction i takes 8 i .. 8 i + 7 of each quarter.)  The determinism contract is that of tbik_gemm, P included.
+ * products of one matrix instruction are added in that instruction's own fixed order, as for the other formats; of each 128 consecutive k -- 64 where
+ * the group is 64, 32 where 128 does not divide it else -- instruction i takes 8 i .. 8 i + 7 of each quarter.)  The determinism contract is that of tbik_gemm, P included.
  *
  *   X       device, x_dtype (TBIK_BF16 or TBIK_F16), [M, ldx], 16-byte aligned, ldx a multiple of 8
  *   Wq      device, [N, ldwq] bytes, ldwq >= K / 2 a multiple of 16, 16-byte aligned: two elements a byte, the one with the even k in the low four bits

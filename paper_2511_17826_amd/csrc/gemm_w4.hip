@@ -5,17 +5,22 @@
 // q - zero is a whole number of -15 .. 15 and exact in either 16-bit format, so the weight is never rounded: the scale multiplies a
 // group's fp32 sum, once per group, row and channel.  How an element becomes a 16-bit float is at widened_levels.
 //
-// An instruction (16x16x32: of 16 rows and channels) multiplies 32 k; which 32 of a unit of 128 (or 64, or 32, the largest that divides the group) it takes is
-// chosen so that a lane's elements of the whole unit are 16 (8, 4) consecutive bytes: a quarter of the lanes takes a quarter of the unit.  The
+// An instruction (16x16x32: of 16 rows and channels) multiplies 32 k; which 32 of a unit of 128 (64 in groups of 64, 32 where 128 does not divide the group else) it
+// takes is chosen so that a lane's elements of the whole unit are 16 (8, 4) consecutive bytes: a quarter of the lanes takes a quarter of the unit.  The
 // kernels share that map, the chains and the tree, so they give the same bits:
-//   slices   up to 16 rows in one launch: a workgroup takes 32 channels and all of a shard's K, its eight wavefronts consecutive superleaves each (whole and in
+//   slices   16 rows: a workgroup takes 32 or 16 channels and all of a shard's K, its up to eight wavefronts consecutive superleaves each (whole and in
 //            order: Sec. 4.2, App. D.1); each streams its part of the weight, of the rows and of the scales through a ring of stages in
 //            LDS of its own (direct global->LDS loads, no barrier until the sums are there), and the upper levels of the tree run over their sums (App. C)
-//   tiles    more rows: a workgroup takes 128 channels and 32, 64 or 128 rows, which its wavefronts share; few tiles split K (fp32 planes, combined by
-//            the same tree), which the rows' traffic decides: a slice would read all of X for every 32 channels
+//   tiles    a workgroup takes 128 channels and 32, 64 or 128 rows, which its wavefronts share; few tiles split K (fp32 planes, combined by
+//            the same tree)
 //   general  any legal shape, operands straight from memory to registers
-// What bounds slices and low tiles is the vector unit: 14 instructions of four cycles widen 8 elements of a lane (one token, K = 4096, N = 12288: without the loads
-// 5.4 us, without the widening and the products 3.6, an empty kernel of that grid 3.8).
+// Slices read the weight once every 16 rows, tiles leave compute units idle where there are few of them: up to 16 rows are slices, and more where there would be
+// up to W4_FEW_TILES tiles (shards counted).  Tiles / slices, us, without room for a split, bf16: K 12288 x N 4096, groups of 128, 32 rows (32 tiles) 49.8 / 19.9,
+// 128 rows 135 / 64, 256 rows (64 tiles) 135 / 124; 2 shards, 256 rows (128 tiles) 71 / 102; K 5120 x N 5120 2 shards, 32 rows (80 tiles) 14.5 / 15.0; 8 shards of
+// K 12288 x N 4096, 17 rows 10.8 / 34.6, 16 rows 10.4 / 10.6, one row 10.1 / 8.3.
+// What bounds slices and low tiles is the latency of a stage, not a rate: LDS reads, 13 to 19 instructions to widen 8 elements of a lane, products that wait for
+// them, with two wavefronts on a vector unit (27 rows, K 12288 x N 4096, fp16, groups of 64 with zero points: 13.5 us of a tile, without its loads 12.9 before
+// the last steps, without widening and products 9.5, the empty kernel 5.2).
 // This file holds the bf16 kernels, and gemm_w4_f16.hip those of fp16.
 #include "w4.hpp"
 
@@ -33,90 +38,87 @@ __device__ __forceinline__ void w4_last_stages(int stages, Consume &consume) {
     if constexpr (REST > 0) w4_last_stages<REST - 1>(stages, consume);
 }
 
-// XR: rows of X in a stage, 8 or 16; or 1: the one row's part of the wavefront's k lies behind its ring from the start, and a slice is 16 channels (NB == 1),
-// which divides the channels among the compute units more evenly.  LEVELS: of the tree in a wavefront.
-template <int UNIT, bool F16, bool ZEROS, int S, int XR, int RING, int LEVELS>
+// XR: rows of X in a stage, 8 or 16; or 1: the one row's part of the wavefront's k lies behind its ring from the start (K 4096 x N 12288 8.1 us instead of 8.4).
+// LEVELS: of the tree in a wavefront.  blockIdx.y: 16 rows each.
+template <int UNIT, bool WHOLE, bool F16, bool ZEROS, int S, int NB, int XR, int RING, int LEVELS>
 __global__ __launch_bounds__(64 * W4_WAVES, XR == 1 ? (LEVELS == 1 && RING == 2 ? 6 : 4) : RING == 2 ? 4 : 2) void gemm_w4_slice_kernel(const W4Params p) {
     constexpr bool ONE = XR == 1;
-    constexpr int NB = ONE ? 1 : 2;
     using Stream = W4Stream<ZEROS, S, NB>;
     constexpr int X_LOADS = ONE ? 0 : XR * S / 8, X_BYTES = X_LOADS * 1024, STAGE = X_BYTES + Stream::BYTES, LOADS = X_LOADS + Stream::LOADS;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n0 = blockIdx.x * (16 * NB);
+    const int n0 = blockIdx.x * (16 * NB), m0 = blockIdx.y * 16;
     W4Sums<1, NB> acc;
-    if (wave < p.active_waves) {
-        const int first_leaf = blockIdx.z * p.leaves_per_shard + wave * p.leaves_per_wave, stages = p.leaves_per_wave * p.stages_per_leaf;
-        const int row_at = RING * STAGE, groups_at = row_at + (ONE ? p.row_bytes : 0), wave_bytes = groups_at + p.group_bytes;
-        const unsigned ring = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem + wave * wave_bytes;
-        const unsigned char *const mine = smem + wave * wave_bytes;
-        Stream stream(p, n0, first_leaf, p.leaves_per_wave, lane, ring + groups_at, mine + groups_at);
-        stream.issue_groups(0, lane);
-        const char *x_ptr = uniform_pointer(reinterpret_cast<const char *>(p.X + (int64_t)first_leaf * p.superleaf));
-        unsigned x_off[ONE ? 1 : X_LOADS];
+    const int first_leaf = blockIdx.z * p.leaves_per_shard + wave * p.leaves_per_wave, stages = p.leaves_per_wave * p.stages_per_leaf;
+    const int row_at = RING * STAGE, groups_at = row_at + (ONE ? p.row_bytes : 0), wave_bytes = groups_at + p.group_bytes;
+    const unsigned ring = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem + wave * wave_bytes;
+    const unsigned char *const mine = smem + wave * wave_bytes;
+    Stream stream(p, n0, first_leaf, p.leaves_per_wave, lane, ring + groups_at, mine + groups_at);
+    stream.issue_groups(0, lane);
+    const char *x_ptr = uniform_pointer(reinterpret_cast<const char *>(p.X + (int64_t)m0 * p.ldx + (int64_t)first_leaf * p.superleaf));
+    unsigned x_off[ONE ? 1 : X_LOADS];
 #pragma unroll
-        for (int j = 0; j < X_LOADS; ++j) {            // rows behind the last one read it once more; they are not stored
-            const int r = j * (8 / S) + lane / (8 * S), c = (lane % (8 * S)) ^ x_swizzle<S>(r);
-            x_off[j] = (unsigned)(min(r, p.M - 1) * (int)p.ldx + c * 8) * 2u;
-        }
-        if constexpr (ONE) {                           // 512 k a load; behind the part's end its last chunk
-            for (int j = 0; j * 1024 < p.row_bytes; ++j)
-                load_16B_per_lane_to_lds<0, true>(x_ptr, (unsigned)min(j * 1024 + lane * 16, stages * (128 * S) - 16), ring + row_at + j * 1024);
-        }
-        auto issue = [&](int slot) __attribute__((always_inline)) {
-            const unsigned at = ring + slot * STAGE;
-#pragma unroll
-            for (int j = 0; j < X_LOADS; ++j) load_16B_per_lane_to_lds<0, true>(x_ptr, x_off[j], at + j * 1024);
-            x_ptr += 128 * S;
-            stream.issue(at + X_BYTES, true);
-        };
-#pragma unroll
-        for (int i = 0; i < RING; ++i)
-            if (i < stages) issue(i);
-        const int xr = lane & 15 & (XR - 1), x_sw = ONE ? 0 : x_swizzle<S>(xr);
-        const unsigned char *row = mine + row_at;
-        W4Multiplier<UNIT, F16, ZEROS, S, 1, NB> multiplier(p, stream, lane);
-        W4Stash<1, NB, LEVELS> stash;
-        int left = p.stages_per_leaf, leaf = 0, slot = 0;
-        acc.clear();
-        auto consume = [&](auto rest, auto again) __attribute__((always_inline)) {
-            w4_wait_loads<decltype(rest)::value * LOADS>();
-            multiplier.prefetch_groups(stream, lane);
-            const unsigned char *const st = mine + slot * STAGE;
-            const unsigned char *const x_rows[1] = {ONE ? row : st + xr * (128 * S)};
-            row += 128 * S;
-            multiplier.stage(stream, st + X_BYTES, x_rows, x_sw, acc);
-            if constexpr (decltype(again)::value) {    // the stage's bytes are in registers before its slot is filled again
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                issue(slot);
-            }
-            slot = slot + 1 == RING ? 0 : slot + 1;
-            if (--left == 0) {                         // a superleaf ends
-                left = p.stages_per_leaf;
-                stash.push(acc, leaf, leaf + 1 < p.leaves_per_wave);
-                ++leaf;
-            }
-        };
-        for (int s = RING; s < stages; ++s) consume(std::integral_constant<int, RING - 1>{}, std::true_type{});
-        w4_last_stages<RING - 1>(stages, consume);
+    for (int j = 0; j < X_LOADS; ++j) {            // rows behind the last one read it once more; they are not stored
+        const int r = j * (8 / S) + lane / (8 * S), c = (lane % (8 * S)) ^ x_swizzle<S>(r);
+        x_off[j] = (unsigned)(min(r, p.M - 1 - m0) * (int)p.ldx + c * 8) * 2u;
     }
+    if constexpr (ONE) {                           // 512 k a load; behind the part's end its last chunk
+        for (int j = 0; j * 1024 < p.row_bytes; ++j)
+            load_16B_per_lane_to_lds<0, true>(x_ptr, (unsigned)min(j * 1024 + lane * 16, stages * (128 * S) - 16), ring + row_at + j * 1024);
+    }
+    auto issue = [&](int slot) __attribute__((always_inline)) {
+        const unsigned at = ring + slot * STAGE;
+#pragma unroll
+        for (int j = 0; j < X_LOADS; ++j) load_16B_per_lane_to_lds<0, true>(x_ptr, x_off[j], at + j * 1024);
+        x_ptr += 128 * S;
+        stream.issue(at + X_BYTES, true);
+    };
+#pragma unroll
+    for (int i = 0; i < RING; ++i)
+        if (i < stages) issue(i);
+    const int xr = lane & 15 & (XR - 1), x_sw = ONE ? 0 : x_swizzle<S>(xr);
+    const unsigned char *row = mine + row_at;
+    W4Multiplier<UNIT, WHOLE, F16, ZEROS, S, 1, NB> multiplier(p, stream, lane);
+    W4Stash<1, NB, LEVELS> stash;
+    int left = p.stages_per_leaf, leaf = 0, slot = 0;
+    acc.clear();
+    auto consume = [&](auto rest, auto again) __attribute__((always_inline)) {
+        w4_wait_loads<decltype(rest)::value * LOADS>();
+        multiplier.prefetch_groups(stream, lane);
+        const unsigned char *const st = mine + slot * STAGE;
+        const unsigned char *const x_rows[1] = {ONE ? row : st + xr * (128 * S)};
+        row += 128 * S;
+        multiplier.stage(stream, st + X_BYTES, x_rows, x_sw, acc);
+        if constexpr (decltype(again)::value) {    // the stage's bytes are in registers before its slot is filled again
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            issue(slot);
+        }
+        slot = slot + 1 == RING ? 0 : slot + 1;
+        if (--left == 0) {                         // a superleaf ends
+            left = p.stages_per_leaf;
+            stash.push(acc, leaf, leaf + 1 < p.leaves_per_wave);
+            ++leaf;
+        }
+    };
+    for (int s = RING; s < stages; ++s) consume(std::integral_constant<int, RING - 1>{}, std::true_type{});
+    w4_last_stages<RING - 1>(stages, consume);
     __syncthreads();                                   // the rings have been read: the sums take their place
     float *const red = reinterpret_cast<float *>(smem);
-    if (wave < p.active_waves) {
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) red[wave * 512 + (4 * (lane >> 4) + r) * 32 + b * 16 + (lane & 15)] = acc.t[0][b][r];
-    }
+        for (int r = 0; r < 4; ++r) red[wave * 512 + (4 * (lane >> 4) + r) * 32 + b * 16 + (lane & 15)] = acc.t[0][b][r];
     __syncthreads();
-    const int row = threadIdx.x / 32, channel = threadIdx.x % 32;                  // 16 rows of 32
-    if (row < p.M && channel < 16 * NB && n0 + channel < p.N) w4_store<F16>(p, blockIdx.z, row, n0 + channel, tree_of_waves<512>(red, p.active_waves, threadIdx.x));
+    for (int at = threadIdx.x; at < 512; at += 64 * p.active_waves) {              // 16 rows of 32
+        const int row = m0 + at / 32, channel = at % 32;
+        if (row < p.M && channel < 16 * NB && n0 + channel < p.N) w4_store<F16>(p, blockIdx.z, row, n0 + channel, tree_of_waves<512>(red, p.active_waves, at));
+    }
 }
 
 // 32 MT rows times 128 channels; four wavefronts share the rows of X in LDS.  blockIdx.z: the shard or the part of a split K.
 // KG: groups of four wavefronts that halve the part's superleaves among them, the upper half's sums joined in LDS: with few rows a wavefront's conversions
 // and its matrix instructions take turns, and a second one on its vector unit fills the gaps.
-template <int UNIT, bool F16, bool ZEROS, int S, int MT, int RING, int KG>
+template <int UNIT, bool WHOLE, bool F16, bool ZEROS, int S, int MT, int RING, int KG>
 __global__ __launch_bounds__(256 * KG, MT == 4 ? 1 : 2) void gemm_w4_tiled_kernel(const W4Params p) {
     using Stream = W4Stream<ZEROS, S>;
     constexpr int MR = 2 * MT;
@@ -159,7 +161,7 @@ __global__ __launch_bounds__(256 * KG, MT == 4 ? 1 : 2) void gemm_w4_tiled_kerne
     }
     const int x_sw = x_swizzle<S>(l16);                // of every one of the lane's rows
     int cur = 0;
-    W4Multiplier<UNIT, F16, ZEROS, S, MR> multiplier(p, stream, lane);
+    W4Multiplier<UNIT, WHOLE, F16, ZEROS, S, MR> multiplier(p, stream, lane);
     W4Sums<MR> acc;
     // A part has up to 16 superleaves, its halves up to 8; undivided parts of up to 64 rows are single superleaves (launch_tile_rows).
     constexpr int LEVELS = KG == 2 ? 3 : MT == 4 ? 4 : 0;
@@ -371,33 +373,33 @@ constexpr int most_group_bytes(int channels, bool zeros) {
     return 2 * (w4_chunk_bytes(channels, (2 * W4_CHUNK + 5) / 4) + (zeros ? w4_chunk_bytes(channels, (W4_CHUNK + 6) / 4) : 0));
 }
 
-template <int UNIT, bool F16, bool ZEROS, int S, int XR, int RING, int LEVELS>
+template <int UNIT, bool WHOLE, bool F16, bool ZEROS, int S, int NB, int XR, int RING, int LEVELS>
 hipError_t launch_slice_of(const W4Params &all, int shards, hipStream_t s) {
-    constexpr int NB = XR == 1 ? 1 : 2, row = XR == 1 ? 8192 : 0;
+    constexpr int row = XR == 1 ? 8192 : 0;
     constexpr int ring = RING * ((XR == 1 ? 0 : XR * S * 128) + W4Stream<ZEROS, S, NB>::BYTES), most = W4_WAVES * (ring + row + most_group_bytes(16 * NB, ZEROS));
     static_assert(most <= 160 * 1024 && ring >= 2048, "LDS of a compute unit; room for the sums");
     W4Params p = all;
     chunks_of(p, 16 * NB, p.leaves_per_wave, ZEROS);
-    const int lds = W4_WAVES * (ring + (XR == 1 ? p.row_bytes : 0) + p.group_bytes);
-    auto k = gemm_w4_slice_kernel<UNIT, F16, ZEROS, S, XR, RING, LEVELS>;
+    const int lds = p.active_waves * (ring + (XR == 1 ? p.row_bytes : 0) + p.group_bytes);
+    auto k = gemm_w4_slice_kernel<UNIT, WHOLE, F16, ZEROS, S, NB, XR, RING, LEVELS>;
     static std::atomic<unsigned> allowed{0};
     const hipError_t e = allow_lds(k, most, allowed);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k, dim3((unsigned)((p.N + 16 * NB - 1) / (16 * NB)), 1, (unsigned)shards), dim3(64 * W4_WAVES), lds, s, p);
+    hipLaunchKernelGGL(k, dim3((unsigned)((p.N + 16 * NB - 1) / (16 * NB)), (unsigned)((p.M + 15) / 16), (unsigned)shards), dim3(64 * p.active_waves), lds, s, p);
     return hipGetLastError();
 }
-template <int UNIT, bool F16, bool ZEROS, int S, int XR, int RING>
+template <int UNIT, bool WHOLE, bool F16, bool ZEROS, int S, int NB, int XR, int RING>
 hipError_t launch_slice(const W4Params &p, int shards, hipStream_t s) {
-    return p.leaves_per_wave <= 2 ? launch_slice_of<UNIT, F16, ZEROS, S, XR, RING, 1>(p, shards, s) : launch_slice_of<UNIT, F16, ZEROS, S, XR, RING, 4>(p, shards, s);
+    return p.leaves_per_wave <= 2 ? launch_slice_of<UNIT, WHOLE, F16, ZEROS, S, NB, XR, RING, 1>(p, shards, s) : launch_slice_of<UNIT, WHOLE, F16, ZEROS, S, NB, XR, RING, 4>(p, shards, s);
 }
-template <int UNIT, bool F16, bool ZEROS, int S, int MT, int RING, int KG = 1>
+template <int UNIT, bool WHOLE, bool F16, bool ZEROS, int S, int MT, int RING, int KG = 1>
 hipError_t launch_tile(const W4Params &all, int shards, hipStream_t s) {
     constexpr int rings = KG * RING * 4 * (MT * S * 1024 + W4Stream<ZEROS, S>::BYTES), most = rings + 4 * KG * most_group_bytes(32, ZEROS);
     static_assert(most <= 160 * 1024 && rings >= 4 * MT * 4096, "LDS of a compute unit; room for the sums and the patches");
     W4Params p = all;
     chunks_of(p, 32, p.leaves_per_shard / KG, ZEROS);
     const int lds = rings + 4 * KG * p.group_bytes;
-    auto k = gemm_w4_tiled_kernel<UNIT, F16, ZEROS, S, MT, RING, KG>;
+    auto k = gemm_w4_tiled_kernel<UNIT, WHOLE, F16, ZEROS, S, MT, RING, KG>;
     static std::atomic<unsigned> allowed{0};
     const hipError_t e = allow_lds(k, most, allowed);
     if (e != hipSuccess) return e;
@@ -406,36 +408,42 @@ hipError_t launch_tile(const W4Params &all, int shards, hipStream_t s) {
 }
 
 // Stages in flight: three while every workgroup has a compute unit to itself; with more workgroups than compute units two, which lets
-// more of them share one (16 rows are too large for that either way).
-template <int UNIT, bool F16, bool ZEROS, int S>
+// more of them share one (16 rows are too large for that either way).  16 channels a slice where 32 leave half of the compute units idle (8 rows, K 12288 x
+// N 4096 13.7 -> 9.8 us, 16 rows 15.2 -> 12.0), for one row, and where there are so many that three workgroups share a compute unit (8 rows, K 4096 x N 12288
+// 10.2 -> 9.5; with 16 rows, where two do not fit, 12.9 would become 14.4; of 160 slices, 5120 x 5120, 8.1 either way with 8 rows and 8.1 -> 11 with 16).
+template <int UNIT, bool WHOLE, bool F16, bool ZEROS, int S>
 hipError_t launch_row(const W4Params &p, int shards, hipStream_t s) {
-    if (((int64_t)p.N + 15) / 16 * shards <= 256) return launch_slice<UNIT, F16, ZEROS, S, 1, 3>(p, shards, s);
-    return launch_slice<UNIT, F16, ZEROS, S, 1, 2>(p, shards, s);
+    if (((int64_t)p.N + 15) / 16 * shards <= 256) return launch_slice<UNIT, WHOLE, F16, ZEROS, S, 1, 1, 3>(p, shards, s);
+    return launch_slice<UNIT, WHOLE, F16, ZEROS, S, 1, 1, 2>(p, shards, s);
 }
-template <int UNIT, bool F16, bool ZEROS, int S>
+template <int UNIT, bool WHOLE, bool F16, bool ZEROS, int S>
 hipError_t launch_slice_rows(const W4Params &all, int shards, hipStream_t s) {
     W4Params p = all;
     p.row_bytes = (p.leaves_per_wave * p.superleaf * 2 + 1023) & ~1023;
     if constexpr (S == 2) {
         if (p.M == 1 && p.row_bytes <= 8192) {
-            if (p.superleaf % 256 != 0) return launch_row<UNIT, F16, ZEROS, 2>(p, shards, s);
+            if (p.superleaf % 256 != 0) return launch_row<UNIT, WHOLE, F16, ZEROS, 2>(p, shards, s);
             p.stages_per_leaf = p.superleaf / 256;
-            return launch_row<UNIT, F16, ZEROS, 4>(p, shards, s);
+            return launch_row<UNIT, WHOLE, F16, ZEROS, 4>(p, shards, s);
         }
     }
-    if (p.M > 8) return launch_slice<UNIT, F16, ZEROS, S, 16, S == 1 ? 4 : 2>(p, shards, s);
-    if constexpr (S == 1) return launch_slice<UNIT, F16, ZEROS, 1, 8, 6>(p, shards, s);
-    else if (((int64_t)p.N + 31) / 32 * shards <= 256) return launch_slice<UNIT, F16, ZEROS, S, 8, 3>(p, shards, s);
-    else return launch_slice<UNIT, F16, ZEROS, S, 8, 2>(p, shards, s);
+    if constexpr (S == 1) return p.M > 8 ? launch_slice<UNIT, WHOLE, F16, ZEROS, 1, 2, 16, 4>(p, shards, s) : launch_slice<UNIT, WHOLE, F16, ZEROS, 1, 2, 8, 6>(p, shards, s);
+    else {
+        const int64_t slices = ((int64_t)p.N + 31) / 32 * shards;
+        if (slices <= 128) return p.M > 8 ? launch_slice<UNIT, WHOLE, F16, ZEROS, S, 1, 16, 3>(p, shards, s) : launch_slice<UNIT, WHOLE, F16, ZEROS, S, 1, 8, 3>(p, shards, s);
+        if (p.M > 8) return launch_slice<UNIT, WHOLE, F16, ZEROS, S, 2, 16, 2>(p, shards, s);
+        if (slices <= 256) return launch_slice<UNIT, WHOLE, F16, ZEROS, S, 2, 8, 3>(p, shards, s);
+        return launch_slice<UNIT, WHOLE, F16, ZEROS, S, 1, 8, 2>(p, shards, s);
+    }
 }
-template <int UNIT, bool F16, bool ZEROS, int S>
+template <int UNIT, bool WHOLE, bool F16, bool ZEROS, int S>
 hipError_t launch_tile_rows(const W4Params &p, int shards, hipStream_t s) {
     const bool halves = p.leaves_per_shard % 2 == 0;   // a power of two: or one
-    if (p.M <= 32) return halves ? launch_tile<UNIT, F16, ZEROS, S, 1, S == 1 ? 6 : 3, 2>(p, shards, s) : launch_tile<UNIT, F16, ZEROS, S, 1, S == 1 ? 6 : 4>(p, shards, s);
-    if (p.M <= 64) return halves ? launch_tile<UNIT, F16, ZEROS, S, 2, S == 1 ? 4 : 2, 2>(p, shards, s) : launch_tile<UNIT, F16, ZEROS, S, 2, S == 1 ? 5 : 3>(p, shards, s);
-    return launch_tile<UNIT, F16, ZEROS, S, 4, S == 1 ? 6 : 3>(p, shards, s);
+    if (p.M <= 32) return halves ? launch_tile<UNIT, WHOLE, F16, ZEROS, S, 1, S == 1 ? 6 : 3, 2>(p, shards, s) : launch_tile<UNIT, WHOLE, F16, ZEROS, S, 1, S == 1 ? 6 : 4>(p, shards, s);
+    if (p.M <= 64) return halves ? launch_tile<UNIT, WHOLE, F16, ZEROS, S, 2, S == 1 ? 4 : 2, 2>(p, shards, s) : launch_tile<UNIT, WHOLE, F16, ZEROS, S, 2, S == 1 ? 5 : 3>(p, shards, s);
+    return launch_tile<UNIT, WHOLE, F16, ZEROS, S, 4, S == 1 ? 6 : 3>(p, shards, s);
 }
-template <int UNIT, bool F16, bool ZEROS>
+template <int UNIT, bool WHOLE, bool F16, bool ZEROS>
 hipError_t launch_unit(const W4Args &a, const W4Params &all, hipStream_t s) {
     W4Params p = all;
     const int ns = a.ns / a.P, kernel = w4_kernel(a);  // ns: superleaves of a shard
@@ -445,11 +453,11 @@ hipError_t launch_unit(const W4Args &a, const W4Params &all, hipStream_t s) {
     p.leaves_per_wave = ns > W4_WAVES ? ns / W4_WAVES : 1;
     p.active_waves = ns > W4_WAVES ? W4_WAVES : ns;
     if constexpr (UNIT < 128) {
-        if (kernel == W4_SLICES && !two) return launch_slice_rows<UNIT, F16, ZEROS, 1>(p, a.P, s);
-        if (kernel == W4_TILES && !two) return launch_tile_rows<UNIT, F16, ZEROS, 1>(p, a.P, s);
+        if (kernel == W4_SLICES && !two) return launch_slice_rows<UNIT, WHOLE, F16, ZEROS, 1>(p, a.P, s);
+        if (kernel == W4_TILES && !two) return launch_tile_rows<UNIT, WHOLE, F16, ZEROS, 1>(p, a.P, s);
     }
-    if (kernel == W4_SLICES) return launch_slice_rows<UNIT, F16, ZEROS, 2>(p, a.P, s);
-    if (kernel == W4_TILES) return launch_tile_rows<UNIT, F16, ZEROS, 2>(p, a.P, s);
+    if (kernel == W4_SLICES) return launch_slice_rows<UNIT, WHOLE, F16, ZEROS, 2>(p, a.P, s);
+    if (kernel == W4_TILES) return launch_tile_rows<UNIT, WHOLE, F16, ZEROS, 2>(p, a.P, s);
     for (int64_t m0 = 0; m0 < a.M; m0 += 32 * 4096) {  // 4096 row tiles a launch
         W4Params q = p;
         q.M = (int)(a.M - m0 < 32 * 4096 ? a.M - m0 : 32 * 4096);
@@ -459,6 +467,11 @@ hipError_t launch_unit(const W4Args &a, const W4Params &all, hipStream_t s) {
         hipLaunchKernelGGL((gemm_w4_kernel<UNIT, F16, ZEROS>), dim3((unsigned)((a.N + 31) / 32), (unsigned)((q.M + 31) / 32), (unsigned)a.P), dim3(64 * W4_WAVES), 0, s, q);
     }
     return hipGetLastError();
+}
+
+template <int UNIT, bool WHOLE, bool F16>
+hipError_t launch_zeros(const W4Args &a, const W4Params &p, hipStream_t s) {
+    return a.zeros ? launch_unit<UNIT, WHOLE, F16, true>(a, p, s) : launch_unit<UNIT, WHOLE, F16, false>(a, p, s);
 }
 
 }  // namespace
@@ -471,7 +484,7 @@ int w4_kernel(const W4Args &a) {
     const int ns = a.ns / a.P;
     const bool ring = a.superleaf % 64 == 0 && a.ldx < (1 << 22) && a.ldw < (1 << 22) && a.lds < (1 << 22) && a.ldz < (1 << 22);      // 32-bit lane offsets
     if (!ring) return W4_GENERAL;
-    if (a.M <= 16) return W4_SLICES;
+    if (a.M <= 16 || w4_tiles(a.M, a.N) * a.P <= W4_FEW_TILES) return W4_SLICES;
     return ns <= 16 && (int64_t)a.M <= 32 * 65535 ? W4_TILES : W4_GENERAL;
 }
 
@@ -493,10 +506,11 @@ hipError_t launch_gemm_w4(const W4Args &a, hipStream_t s) {
     p.vector_stores = (reinterpret_cast<uintptr_t>(out) & 15) == 0 && ld_bytes % 16 == 0;
     if (a.x_dtype == TBIK_F16) return launch_gemm_w4_f16(a, p, s);
 #endif
-    const bool zeros = a.zeros != nullptr;
-    if (a.group % 128 == 0) return zeros ? launch_unit<128, TBIK_W4_F16, true>(a, p, s) : launch_unit<128, TBIK_W4_F16, false>(a, p, s);
-    if (a.group % 64 == 0) return zeros ? launch_unit<64, TBIK_W4_F16, true>(a, p, s) : launch_unit<64, TBIK_W4_F16, false>(a, p, s);
-    return zeros ? launch_unit<32, TBIK_W4_F16, true>(a, p, s) : launch_unit<32, TBIK_W4_F16, false>(a, p, s);
+    if (a.group == 128) return launch_zeros<128, true, TBIK_W4_F16>(a, p, s);
+    if (a.group == 64) return launch_zeros<64, true, TBIK_W4_F16>(a, p, s);
+    if (a.group == 32) return launch_zeros<32, true, TBIK_W4_F16>(a, p, s);
+    if (a.group % 128 == 0) return launch_zeros<128, false, TBIK_W4_F16>(a, p, s);
+    return launch_zeros<32, false, TBIK_W4_F16>(a, p, s);
 }
 
 }  // namespace tbik

@@ -96,7 +96,7 @@ int internal_split(int M, int N, int K, int ns) {
         return best;
     }
     if (tiles >= 128) return split;             // at least half of the 256 compute units already have a tile
-    while (split < ns && split < 16 && tiles * split < 256) split *= 2;
+    while (split < ns && split < 16 && tiles * split * 2 <= 256) split *= 2;
     return split;
 }
 
@@ -182,7 +182,7 @@ int mxfp6_split(int M, int N, int ns) {
     int split = 1;
     while (ns > 16 * split && split < TBIK_MAX_SHARDS) split *= 2;     // the tiled kernel walks at most 16 superleaves per shard
     if (tiles >= 128) return split;
-    while (split < ns && split < 16 && tiles * split < 256) split *= 2;
+    while (split < ns && split < 16 && tiles * split * 2 <= 256) split *= 2;
     return split;
 }
 
@@ -1363,16 +1363,16 @@ int tbik_rmsnorm_residual_rmsnorm(const void *y, int64_t ldy, const float *parti
     return e == hipSuccess ? TBIK_OK : hip_fail(e);
 }
 
-// Parts that K is split into where the tiles of a 4-bit product leave compute units idle: until there is a workgroup for each (and a tile
-// walks at most 16 superleaves).  Up to 16 rows are slices, which split K among their wavefronts.
+// Parts that K is split into where the tiles of a 4-bit product leave compute units idle: while there are no more workgroups than compute units (and until a tile
+// walks at most 16 superleaves; a second, partly filled round costs more: 27 rows, K 4096 x N 12288, 96 tiles, split 4 19.2 us, split 2 15.7).  Slices split K among
+// their wavefronts.
 static int w4_split(int M, int N, int ns) {
     if (M <= 16) return 1;
-    const int rows = M <= 32 ? 32 : M <= 64 ? 64 : 128;
-    const int64_t tiles = ((int64_t)N + 127) / 128 * (((int64_t)M + rows - 1) / rows);
+    const int64_t tiles = w4_tiles(M, N);
     int split = 1;
     while (ns > 16 * split) split *= 2;
-    while (split < ns && split < 16 && tiles * split < 256) split *= 2;
-    return split;
+    while (split < ns && split < 16 && tiles * split * 2 <= 256) split *= 2;
+    return tiles * split <= W4_FEW_TILES ? 1 : split;
 }
 
 static int gemm_w4(tbik_dtype x_dtype, const void *X, int64_t ldx, const void *Wq, int64_t ldwq, const void *scales, int64_t lds, const void *zeros, int64_t ldz,
@@ -1403,12 +1403,13 @@ static int gemm_w4(tbik_dtype x_dtype, const void *X, int64_t ldx, const void *W
     hipError_t e;
     int split = partials ? 1 : w4_split(M, N, ns);
     while (split > 1 && split_planes_bytes(M, N, split) > (workspace ? workspace_bytes : 0)) split /= 2;      // less room: the same bits with less of a split
-    if (split > 1 && w4_kernel(a) != W4_SLICES) {
-        a.partials = reinterpret_cast<float *>(workspace);
-        a.Y = nullptr;
-        a.P = split;
-        e = launch_gemm_w4(a, s);
-        if (e == hipSuccess) e = launch_tree_combine(a.partials, split, Y, ldy, (int)y_dtype, M, N, s);
+    W4Args parts = a;
+    parts.partials = reinterpret_cast<float *>(workspace);
+    parts.Y = nullptr;
+    parts.P = split;
+    if (split > 1 && w4_kernel(parts) != W4_SLICES) {
+        e = launch_gemm_w4(parts, s);
+        if (e == hipSuccess) e = launch_tree_combine(parts.partials, split, Y, ldy, (int)y_dtype, M, N, s);
     } else {
         e = launch_gemm_w4(a, s);
     }

@@ -190,6 +190,11 @@ struct W4Args : GemmArgs {
 };
 enum { W4_GENERAL, W4_SLICES, W4_TILES };
 int w4_kernel(const W4Args &a);            // what a call launches
+constexpr int W4_FEW_TILES = 64;           // up to so many (shards and parts of a split K included) slices are quicker: see gemm_w4.hip
+inline int64_t w4_tiles(int M, int N) {
+    const int rows = M <= 32 ? 32 : M <= 64 ? 64 : 128;
+    return ((int64_t)N + 127) / 128 * (((int64_t)M + rows - 1) / rows);
+}
 hipError_t launch_gemm_w4(const W4Args &a, hipStream_t s);
 
 // Y = T(partials[0..P)) elementwise + one rounding.

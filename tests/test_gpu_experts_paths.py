@@ -89,8 +89,8 @@ def test_on_the_current_stream(name):
 
 def test_graphs_with_workspaces_of_their_own():
     """4-bit products whose K is split: two graphs, a larger eager call between their replays."""
-    ops = [(rnd((m, 4096), seed=m), whole((N, 2048), 256), rnd((N, 32)).abs(), 256, 1) for m in (40, 24)]
-    assert all(tb.lib().tbik_gemm_w4_workspace_bytes(o[0].shape[0], N, 4096, 256, 1) > 0 for o in ops)
+    ops = [(rnd((m, 4096), seed=m), whole((1160, 2048), 256), rnd((1160, 32)).abs(), 256, 1) for m in (40, 24)]
+    assert all(tb.lib().tbik_gemm_w4_workspace_bytes(o[0].shape[0], 1160, 4096, 256, 1) > 0 for o in ops)
     want = [tb.tbik_gemm_w4(*o) for o in ops]
     graphs, outs = [], []
     side = torch.cuda.Stream()

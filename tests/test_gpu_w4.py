@@ -41,7 +41,13 @@ def check(y, X, W, K):
 
 
 SHAPES = [(1, 32, 64, 64, 1, 64), (1, 4096, 512, 64, 1, 64), (3, 72, 512, 64, 1, 32), (33, 200, 1024, 128, 1, 128), (32, 33, 1536, 64, 3, 96), (70, 40, 640, 128, 5, 128),
-          (5, 1, 2048, 256, 1, 64), (16, 129, 4096, 32, 1, 32), (2, 64, 5120, 128, 5, 128), (130, 130, 256, 256, 1, 256), (300, 96, 512, 64, 1, 64)]
+          (5, 1, 2048, 256, 1, 64), (16, 129, 4096, 32, 1, 32), (2, 64, 5120, 128, 5, 128), (130, 130, 256, 256, 1, 256), (300, 96, 512, 64, 1, 64),
+          # Slices of 32 channels, and of 16 where there are very many; groups of more than one unit.
+          (4, 4136, 512, 64, 1, 64), (12, 4136, 1024, 64, 1, 32), (6, 8232, 512, 128, 1, 128), (16, 8232, 2048, 64, 1, 64), (1, 8232, 512, 64, 1, 32), (7, 4200, 768, 64, 3, 192),
+          (40, 100, 2048, 256, 1, 256), (9, 100, 1536, 64, 3, 192), (1, 72, 4096, 512, 1, 256), (90, 136, 1280, 64, 5, 160),
+          # Tiles of 32, 64 and 128 rows, of one superleaf and of many, K divided or not.
+          (20, 8264, 128, 128, 1, 64), (50, 8264, 256, 256, 1, 128), (20, 8264, 256, 64, 1, 32), (33, 1160, 1024, 128, 1, 128), (70, 2088, 640, 128, 5, 128), (27, 1160, 2048, 64, 1, 64),
+          (130, 1160, 1024, 64, 1, 64), (300, 1160, 512, 64, 1, 64), (200, 4136, 768, 64, 3, 192), (61, 1160, 8192, 256, 1, 256)]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
@@ -80,7 +86,7 @@ def test_high_bits_of_a_zero_do_not_count():
 @pytest.mark.parametrize("zeros", [False, True])
 @pytest.mark.parametrize("K,leaf,k_first,group", [(4096, 256, 1, 128), (2048, 128, 1, 32), (1536, 64, 3, 64), (5120, 128, 5, 128)])
 def test_batch_and_shards(K, leaf, k_first, group, dtype, zeros):
-    X, Wq, scales, z = operands(200, 136, K, group, dtype, zeros, K)
+    X, Wq, scales, z = operands(200, 1160, K, group, dtype, zeros, K)
     want = tb.tbik_gemm_w4(X, Wq, scales, leaf, k_first, zeros=z, out_dtype=torch.float32)
     for lo, hi in ((0, 1), (7, 9), (100, 117), (40, 73), (5, 70), (64, 200)):
         assert torch.equal(bits(tb.tbik_gemm_w4(X[lo:hi], Wq, scales, leaf, k_first, zeros=z, out_dtype=torch.float32)), bits(want[lo:hi]))
@@ -89,7 +95,7 @@ def test_batch_and_shards(K, leaf, k_first, group, dtype, zeros):
     while P <= min(ns, 16):
         for rows in (X, X[:5]):
             parts = tb.tbik_gemm_shard_partials_w4(rows, Wq, scales, leaf, k_first, P, zeros=z)
-            assert parts.shape == (P, rows.shape[0], 136)
+            assert parts.shape == (P, rows.shape[0], 1160)
             assert torch.equal(bits(tb.tbik_tree_combine(parts, out_dtype=torch.float32)), bits(want[:rows.shape[0]]))
         P *= 2
     # A real rank's own part of the operands: whole groups, its own bytes.
@@ -102,13 +108,13 @@ def test_batch_and_shards(K, leaf, k_first, group, dtype, zeros):
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("zeros", [False, True])
-@pytest.mark.parametrize("K,leaf,k_first,group", [(12288, 256, 3, 32), (8192, 64, 1, 32), (6144, 64, 3, 96), (14336, 256, 7, 64)])
+@pytest.mark.parametrize("K,leaf,k_first,group", [(12288, 256, 3, 32), (8192, 64, 1, 32), (6144, 64, 3, 96), (14336, 256, 7, 64), (16384, 256, 1, 256), (12288, 64, 3, 192)])
 def test_more_groups_than_a_chunk_of_scales(K, leaf, k_first, group, dtype, zeros):
     """Every wavefront walks more groups than are held at once; scales and zero points at odd addresses; one row to many, one shard."""
-    X, Wq, scales, z = operands(150, 40, K, group, dtype, zeros, K + group)
-    sw = torch.zeros((40, K // group + 3), dtype=dtype, device=DEV)
+    X, Wq, scales, z = operands(150, 1160, K, group, dtype, zeros, K + group)
+    sw = torch.zeros((1160, K // group + 3), dtype=dtype, device=DEV)
     sw[:, 1:-2] = scales
-    zw = torch.zeros((40, K // group + 6), dtype=torch.uint8, device=DEV)
+    zw = torch.zeros((1160, K // group + 6), dtype=torch.uint8, device=DEV)
     if zeros:
         zw[:, 3:-3] = z
         z = zw[:, 3:-3]
@@ -122,9 +128,9 @@ def test_more_groups_than_a_chunk_of_scales(K, leaf, k_first, group, dtype, zero
 
 def test_less_workspace_and_the_general_kernel():
     """The split of K follows the room; operands too far apart for the kernels with direct loads go another way: the same bits."""
-    X, Wq, scales, z = operands(40, 256, 4096, 64, torch.bfloat16, True, 7)
+    X, Wq, scales, z = operands(40, 1160, 4096, 64, torch.bfloat16, True, 7)
     want = tb.tbik_gemm_w4(X, Wq, scales, 256, 1, zeros=z)
-    need = tb.lib().tbik_gemm_w4_workspace_bytes(40, 256, 4096, 256, 1)
+    need = tb.lib().tbik_gemm_w4_workspace_bytes(40, 1160, 4096, 256, 1)
     assert need > 0
     for room in (0, 256, need // 2, need // 4 + 1, need):
         assert torch.equal(bits(tb.tbik_gemm_w4(X, Wq, scales, 256, 1, zeros=z, workspace=torch.empty(room, dtype=torch.uint8, device=DEV))), bits(want))
