@@ -10,9 +10,11 @@
 namespace tbik {
 
 constexpr int kGroupsPerLane = kMaxGroups / 64;
+constexpr int GROUP_PANEL = 8;             // row tiles
 
 struct GroupRows {
     int group, first, end;                 // rows first .. end - 1 of this tile's group, from the tile on
+    int row, high;                         // which of the group's row tiles it is, of how many
 };
 
 template <int TILE_ROWS>
@@ -54,7 +56,7 @@ struct GroupMap {
 
     // Row tile `tile` (uniform, below `tiles`).
     __device__ __forceinline__ GroupRows at(int tile) const {
-        GroupRows g{0, 0, 0};
+        GroupRows g{0, 0, 0, 0, 1};
         bool found = false;
 #pragma unroll
         for (int j = 0; j < kGroupsPerLane; ++j) {
@@ -64,9 +66,38 @@ struct GroupMap {
                 const int l = __builtin_ctzll(behind);
                 const int b = __builtin_amdgcn_readlane(begin[j], l), n = __builtin_amdgcn_readlane(end[j], l);
                 const int last = __builtin_amdgcn_readlane(tiles_end[j], l);
-                g = {j * 64 + l, b + (tile - (last - (n - b + TILE_ROWS - 1) / TILE_ROWS)) * TILE_ROWS, n};
+                const int high = (n - b + TILE_ROWS - 1) / TILE_ROWS, row = tile - (last - high);
+                g = {j * 64 + l, b + row * TILE_ROWS, n, row, high};
             }
         }
+        return g;
+    }
+
+    // Tile `t` (uniform, below tiles * columns) of a product whose rows have `columns` tiles each: a group's tiles follow those of the group before, row tile by row
+    // tile, or (`panels`) in panels of up to GROUP_PANEL of its row tiles, column by column in a panel, so that consecutive tiles share rows of X and columns of the
+    // weight.  A division is some 30 instructions, ahead of which the next tile's loads cannot start: the common case takes two.
+    __device__ __forceinline__ GroupRows at(int t, int columns, bool panels, int &column) const {
+        const int row_tile = t / columns;
+        GroupRows g = at(row_tile);
+        if (!panels) {
+            column = t - row_tile * columns;
+            return g;
+        }
+        return in_panels(g, t, columns, row_tile, column);
+    }
+
+private:
+    __device__ __forceinline__ GroupRows in_panels(GroupRows g, int t, int columns, int row_tile, int &column) const {
+        int row = g.row, rows = g.high, first = 0;                               // of the panel: how many, the first one
+        int v = (t - row_tile * columns) + row * columns;                        // the tile's number in its group
+        if (rows > GROUP_PANEL) {                                                // panels of about the same height
+            const int n = (rows + GROUP_PANEL - 1) / GROUP_PANEL, most = (rows + n - 1) / n, k = v / (most * columns);
+            first = k * most;
+            v -= first * columns;
+            rows = min(most, rows - first);
+        }
+        column = v / rows;
+        g.first += (first + v - column * rows - row) * TILE_ROWS;
         return g;
     }
 };

@@ -146,6 +146,25 @@ def test_bits_do_not_depend_on_the_kernel(sizes):
         assert torch.equal(bits(tb.tbik_gemm_grouped_shard_partials(X, W, offsets, 128, 1, 4, rows=rows)), bits(want_parts)), variant
 
 
+@pytest.mark.parametrize("sizes", [[1153, 5, 0, 2570, 128], [129, 0, 1], [1025], [300] * 9], ids=str)
+def test_groups_of_several_tiles(sizes):
+    """Tiles of 128 rows: panels of up to eight, rounds that do not fill the card, shards."""
+    X, W, offsets, rows = operands(sizes, 256, 384, torch.bfloat16, 5, tokens=700)
+    tb.tbik_set_gemm_variant(tb.VARIANT_T128)
+    y = tb.tbik_gemm_grouped(X, W, offsets, 64, 1, rows=rows)
+    odd = tb.tbik_gemm_grouped(X, W[:, :, :328], offsets, 64, 1, rows=rows)
+    act = tb.tbik_gemm_grouped_swiglu(X, W, offsets, 64, 1, rows=rows)
+    parts = tb.tbik_gemm_grouped_shard_partials(X, W, offsets, 64, 1, 4, rows=rows)
+    tb.tbik_set_gemm_variant(0)
+    for span, (want, want_act, want_parts) in each_group(
+            lambda x, w: (tb.tbik_gemm(x, w, 64, 1, out_dtype=torch.bfloat16), tb.tbik_gemm_swiglu(x, w, 64, 1), tb.tbik_gemm_shard_partials(x, w, 64, 1, 4)),
+            X, W, offsets, rows):
+        assert torch.equal(bits(y[span]), bits(want))
+        assert torch.equal(bits(odd[span]), bits(want[:, :328]))
+        assert torch.equal(bits(act[span]), bits(want_act))
+        assert torch.equal(bits(parts[:, span]), bits(want_parts))
+
+
 def test_most_groups_and_no_rows():
     sizes = [(i * 7) % 5 for i in range(512)]
     X, W, offsets, rows = operands(sizes, 128, 40, torch.bfloat16, 10, tokens=64)
