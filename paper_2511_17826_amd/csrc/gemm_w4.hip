@@ -11,7 +11,7 @@
 //   slices   16 rows: a workgroup takes 32 or 16 channels and all of a shard's K, its up to eight wavefronts consecutive superleaves each (whole and in
 //            order: Sec. 4.2, App. D.1); each streams its part of the weight, of the rows and of the scales through a ring of stages in
 //            LDS of its own (direct global->LDS loads, no barrier until the sums are there), and the upper levels of the tree run over their sums (App. C)
-//   tiles    a workgroup takes 128 channels and 32, 64 or 128 rows, which its wavefronts share; few tiles split K (fp32 planes, combined by
+//   tiles    a workgroup takes 128 channels and 32 or 64 rows, which its wavefronts share; few tiles split K (fp32 planes, combined by
 //            the same tree)
 //   general  any legal shape, operands straight from memory to registers
 // Slices read the weight once every 16 rows, tiles leave compute units idle where there are few of them: up to 16 rows are slices, and more where there would be
@@ -115,11 +115,12 @@ __global__ __launch_bounds__(64 * W4_WAVES, XR == 1 ? (LEVELS == 1 && RING == 2 
     }
 }
 
-// 32 MT rows times 128 channels; four wavefronts share the rows of X in LDS.  blockIdx.z: the shard or the part of a split K.
+// 32 MT rows (MT 1 or 2) times 128 channels; four wavefronts share the rows of X in LDS.  blockIdx.z: the shard or the part of a split K.
 // KG: groups of four wavefronts that halve the part's superleaves among them, the upper half's sums joined in LDS: with few rows a wavefront's conversions
-// and its matrix instructions take turns, and a second one on its vector unit fills the gaps.
+// and its matrix instructions take turns, and a second one on its vector unit fills the gaps.  That is why there are no tiles of 128 rows, whose registers leave room
+// for one: K 4096 x N 12288, 128 rows 33.8 us (64: 25.7), 256 rows 52.6 (49.2); K 5120 x N 5120, 192 rows 42.7 (25.6).  More stages in flight than these change nothing.
 template <int UNIT, bool WHOLE, bool F16, bool ZEROS, int S, int MT, int RING, int KG>
-__global__ __launch_bounds__(256 * KG, MT == 4 ? 1 : 2) void gemm_w4_tiled_kernel(const W4Params p) {
+__global__ __launch_bounds__(256 * KG, 2) void gemm_w4_tiled_kernel(const W4Params p) {
     using Stream = W4Stream<ZEROS, S>;
     constexpr int MR = 2 * MT;
     constexpr int X_LOADS = MT * S, REGION = X_LOADS * 1024 + Stream::BYTES, STAGE = 4 * REGION, LOADS = X_LOADS + Stream::LOADS;      // a region is what one wavefront loads
@@ -163,8 +164,8 @@ __global__ __launch_bounds__(256 * KG, MT == 4 ? 1 : 2) void gemm_w4_tiled_kerne
     int cur = 0;
     W4Multiplier<UNIT, WHOLE, F16, ZEROS, S, MR> multiplier(p, stream, lane);
     W4Sums<MR> acc;
-    // A part has up to 16 superleaves, its halves up to 8; undivided parts of up to 64 rows are single superleaves (launch_tile_rows).
-    constexpr int LEVELS = KG == 2 ? 3 : MT == 4 ? 4 : 0;
+    // A part has up to 16 superleaves, its halves up to 8; undivided parts are single superleaves (launch_tile_rows).
+    constexpr int LEVELS = KG == 2 ? 3 : 0;
     W4Sums<MR> slots[LEVELS > 0 ? LEVELS : 1];
     auto superleaf = [&](W4Sums<MR> &acc) __attribute__((always_inline)) {
         acc.clear();
@@ -439,9 +440,8 @@ hipError_t launch_slice_rows(const W4Params &all, int shards, hipStream_t s) {
 template <int UNIT, bool WHOLE, bool F16, bool ZEROS, int S>
 hipError_t launch_tile_rows(const W4Params &p, int shards, hipStream_t s) {
     const bool halves = p.leaves_per_shard % 2 == 0;   // a power of two: or one
-    if (p.M <= 32) return halves ? launch_tile<UNIT, WHOLE, F16, ZEROS, S, 1, S == 1 ? 6 : 3, 2>(p, shards, s) : launch_tile<UNIT, WHOLE, F16, ZEROS, S, 1, S == 1 ? 6 : 4>(p, shards, s);
-    if (p.M <= 64) return halves ? launch_tile<UNIT, WHOLE, F16, ZEROS, S, 2, S == 1 ? 4 : 2, 2>(p, shards, s) : launch_tile<UNIT, WHOLE, F16, ZEROS, S, 2, S == 1 ? 5 : 3>(p, shards, s);
-    return launch_tile<UNIT, WHOLE, F16, ZEROS, S, 4, S == 1 ? 6 : 3>(p, shards, s);
+    if (w4_tile_rows(p.M) == 32) return halves ? launch_tile<UNIT, WHOLE, F16, ZEROS, S, 1, S == 1 ? 6 : 3, 2>(p, shards, s) : launch_tile<UNIT, WHOLE, F16, ZEROS, S, 1, S == 1 ? 6 : 4>(p, shards, s);
+    return halves ? launch_tile<UNIT, WHOLE, F16, ZEROS, S, 2, S == 1 ? 4 : 2, 2>(p, shards, s) : launch_tile<UNIT, WHOLE, F16, ZEROS, S, 2, S == 1 ? 5 : 3>(p, shards, s);
 }
 template <int UNIT, bool WHOLE, bool F16, bool ZEROS>
 hipError_t launch_unit(const W4Args &a, const W4Params &all, hipStream_t s) {

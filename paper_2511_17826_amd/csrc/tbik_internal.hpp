@@ -191,8 +191,9 @@ struct W4Args : GemmArgs {
 enum { W4_GENERAL, W4_SLICES, W4_TILES };
 int w4_kernel(const W4Args &a);            // what a call launches
 constexpr int W4_FEW_TILES = 64;           // up to so many (shards and parts of a split K included) slices are quicker: see gemm_w4.hip
+inline int w4_tile_rows(int M) { return M <= 32 ? 32 : 64; }
 inline int64_t w4_tiles(int M, int N) {
-    const int rows = M <= 32 ? 32 : M <= 64 ? 64 : 128;
+    const int rows = w4_tile_rows(M);
     return ((int64_t)N + 127) / 128 * (((int64_t)M + rows - 1) / rows);
 }
 hipError_t launch_gemm_w4(const W4Args &a, hipStream_t s);

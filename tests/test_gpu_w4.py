@@ -45,7 +45,7 @@ SHAPES = [(1, 32, 64, 64, 1, 64), (1, 4096, 512, 64, 1, 64), (3, 72, 512, 64, 1,
           # Slices of 32 channels, and of 16 where there are very many; groups of more than one unit.
           (4, 4136, 512, 64, 1, 64), (12, 4136, 1024, 64, 1, 32), (6, 8232, 512, 128, 1, 128), (16, 8232, 2048, 64, 1, 64), (1, 8232, 512, 64, 1, 32), (7, 4200, 768, 64, 3, 192),
           (40, 100, 2048, 256, 1, 256), (9, 100, 1536, 64, 3, 192), (1, 72, 4096, 512, 1, 256), (90, 136, 1280, 64, 5, 160),
-          # Tiles of 32, 64 and 128 rows, of one superleaf and of many, K divided or not.
+          # Tiles of 32 and 64 rows, of one superleaf and of many, K divided or not.
           (20, 8264, 128, 128, 1, 64), (50, 8264, 256, 256, 1, 128), (20, 8264, 256, 64, 1, 32), (33, 1160, 1024, 128, 1, 128), (70, 2088, 640, 128, 5, 128), (27, 1160, 2048, 64, 1, 64),
           (130, 1160, 1024, 64, 1, 64), (300, 1160, 512, 64, 1, 64), (200, 4136, 768, 64, 3, 192), (61, 1160, 8192, 256, 1, 256)]
 
