@@ -7,6 +7,8 @@
 // Bound by HBM: k rows read and one written per token, the reads gathered but whole rows.  A thread holds 8 consecutive columns and
 // has the rows of up to 8 choices on their way before it adds the first (fp32 sums of P shards: 8 / P choices); slots and weights are
 // the workgroup's (one token), in scalar registers.
+#include <algorithm>
+
 #include "tbik_device.hpp"
 #include "tbik_internal.hpp"
 
@@ -65,8 +67,8 @@ struct Piece<0> {
 template <int P, bool F16, bool WIDE>
 __global__ __launch_bounds__(256) void experts_sum_kernel(const SumParams p) {
     const int64_t t = blockIdx.y;
+    if ((blockIdx.x * 256u + threadIdx.x) * 8u >= (unsigned)p.H) return;       // up to 2^31 + 2047: not an int
     const int col = (blockIdx.x * 256 + threadIdx.x) * 8;
-    if (col >= p.H) return;
     constexpr int AHEAD = P <= 1 ? 8 : P == 2 ? 4 : P == 4 ? 2 : 1;
     const int32_t *const slots = p.slots + t * p.k;
     const float *const weights = p.weights + t * p.k;
@@ -132,8 +134,8 @@ __device__ __forceinline__ float element_16(const void *p, int64_t i) {
 template <int P, bool F16, bool WIDE>
 __global__ __launch_bounds__(256) void experts_sum_element_kernel(const SumParams p) {
     const int64_t t = blockIdx.y;
+    if (blockIdx.x * 256u + threadIdx.x >= (unsigned)p.H) return;
     const int col = blockIdx.x * 256 + threadIdx.x;
-    if (col >= p.H) return;
     float acc = 0.0f;
     for (int j = 0; j < p.k; ++j) {
         const int slot = p.slots[t * p.k + j];
@@ -157,17 +159,17 @@ __global__ __launch_bounds__(256) void experts_sum_element_kernel(const SumParam
 
 template <int P, bool F16, bool WIDE>
 void launch_sum(const SumParams &p, int T, bool vector, hipStream_t s) {
-    const int per_block = vector ? 2048 : 256;
-    const int launches = (int)(((int64_t)T + 16383) / 16384);
-    for (int i = 0; i < launches; ++i) {               // 16384 tokens each: a grid has fewer than 2^32 threads
+    const int64_t blocks = ((int64_t)p.H + (vector ? 2047 : 255)) / (vector ? 2048 : 256);
+    // A grid has fewer than 2^32 threads: 16384 tokens a launch, fewer of rows of more than 2^18 columns (2^21 of eight a thread).
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(16384, (1 << 24) / blocks - 1));
+    for (int64_t t0 = 0; t0 < T; t0 += most) {
         SumParams q = p;
-        const int64_t t0 = (int64_t)i * 16384;
-        const int tokens = (int)(T - t0 < 16384 ? T - t0 : 16384);
+        const int tokens = (int)std::min(T - t0, most);
         q.slots += t0 * p.k;
         q.weights += t0 * p.k;
         if (q.residual) q.residual = static_cast<const char *>(q.residual) + t0 * p.ldr * (WIDE ? 4 : 2);
         q.out = static_cast<char *>(q.out) + t0 * p.ldo * (WIDE ? 4 : 2);
-        const dim3 grid((unsigned)((p.H + per_block - 1) / per_block), (unsigned)tokens);
+        const dim3 grid((unsigned)blocks, (unsigned)tokens);
         if (vector) hipLaunchKernelGGL((experts_sum_kernel<P, F16, WIDE>), grid, dim3(256), 0, s, q);
         else hipLaunchKernelGGL((experts_sum_element_kernel<P, F16, WIDE>), grid, dim3(256), 0, s, q);
     }

@@ -15,9 +15,9 @@
 //            the same tree)
 //   general  any legal shape, operands straight from memory to registers
 // Slices read the weight once every 16 rows, tiles leave compute units idle where there are few of them: up to 16 rows are slices, and more where there would be
-// up to W4_FEW_TILES tiles (shards counted).  Tiles / slices, us, without room for a split, bf16: K 12288 x N 4096, groups of 128, 32 rows (32 tiles) 49.8 / 19.9,
-// 128 rows 135 / 64, 256 rows (64 tiles) 135 / 124; 2 shards, 256 rows (128 tiles) 71 / 102; K 5120 x N 5120 2 shards, 32 rows (80 tiles) 14.5 / 15.0; 8 shards of
-// K 12288 x N 4096, 17 rows 10.8 / 34.6, 16 rows 10.4 / 10.6, one row 10.1 / 8.3.
+// up to W4_FEW_TILES tiles (shards counted).  Tiles / slices, us, without room for a split, bf16: K 12288 x N 4096, groups of 128, 32 rows (32 tiles) 48.0 / 19.0,
+// 64 rows (32) 64.7 / 34.4, 128 rows (64) 64.9 / 64.0, 256 rows (128) 65 / 124; 2 shards, 64 rows (64) 33.8 / 27.1, 256 rows (256) 37 / 102; K 5120 x N 5120, 32
+// rows (40) 21.7 / 12.1, 2 shards (80) 12.6 / 15.0; 8 shards of K 12288 x N 4096, 17 rows 10.0 / 34.6, 16 rows 10.4 / 10.6, one row 10.1 / 8.3.
 // What bounds slices and low tiles is the latency of a stage, not a rate: LDS reads, 13 to 19 instructions to widen 8 elements of a lane, products that wait for
 // them, with two wavefronts on a vector unit (27 rows, K 12288 x N 4096, fp16, groups of 64 with zero points: 13.5 us of a tile, without its loads 12.9 before
 // the last steps, without widening and products 9.5, the empty kernel 5.2).

@@ -147,7 +147,7 @@ struct W4Stash {
 };
 
 // T over 2^levels superleaves, levels <= L: a nest of loops, each of two trips or (above `levels`) one, whose first trip parks its subtree's sum in a slot of
-// its own.  (With the stash above, whose slot is chosen when it is used, tiles of 64 and 128 rows spill.)
+// its own.  (With the stash above, whose slot is chosen when it is used, tiles of 64 rows spill.)
 template <int L>
 struct W4Walk {
     template <class Leaf, int MR, int SLOTS>
@@ -297,7 +297,7 @@ struct W4Stream {
 // Multiplies a stage: rows x_rows[a] (the lane's row of X of block a in the stage, in LDS) times the stage's weight at st.  sum: the running group's; a group that ends
 // goes through its scale into acc.  lane % 16: the row of X and the channel of a block; quarter: lane / 16.
 // WHOLE: a group is one unit, so nothing branches within a stage, and its scales and zero points are read ahead of everything that waits for LDS instead of at
-// the group's end (27 rows, K 12288 x N 4096, groups of 64 with zero points 17.4 -> 15.8 us with its combination; 256 rows 62.3 -> 54.7).
+// the group's end (27 rows, K 12288 x N 4096, groups of 64 with zero points 17.4 -> 15.8 us with its combination).
 template <int UNIT, bool WHOLE, bool F16, bool ZEROS, int S, int MR, int NB = 2>
 struct W4Multiplier {
     using Stream = W4Stream<ZEROS, S, NB>;

@@ -94,6 +94,18 @@ def test_more_tokens_than_a_launch():
     check(tb.tbik_combine_experts(Y, slots, weights), Y, slots, weights, None)
 
 
+def test_rows_of_millions_of_columns_are_several_launches():
+    """Element by element: a grid has fewer than 2^32 threads.  One choice of weight 1: the chosen row itself."""
+    T, H = 2050, (1 << 21) + 1
+    Y = torch.randn((3, H), generator=torch.Generator(device=DEV).manual_seed(6), device=DEV).to(torch.bfloat16)
+    slots = (torch.arange(T, device=DEV, dtype=torch.int32) * 7 % 3).reshape(T, 1)
+    out = torch.full((T, H), 9.0, dtype=torch.bfloat16, device=DEV)
+    tb.tbik_combine_experts(Y, slots, torch.ones((T, 1), device=DEV), out=out)
+    for t in range(0, T, 205):
+        assert torch.equal(out[t:t + 205], Y[slots[t:t + 205, 0].long()])
+    assert torch.equal(out[-1], Y[slots[-1, 0].long()])
+
+
 def test_refusals():
     Y, slots, weights, residual = inputs(5, 4, 20, 64, torch.bfloat16, 4)
     for kw in (dict(slots=slots.long()), dict(weights=weights.half()), dict(weights=weights[:, :3]), dict(residual=residual.float(), out_dtype=torch.bfloat16), dict(residual=residual[:4]),
