@@ -102,7 +102,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_grouped_slice_kernel(const
             load_16B_per_lane_to_lds<0, true>(w_ptr, woff[0], m0v);
             load_16B_per_lane_to_lds<1024, false>(w_ptr, woff[1], m0v);
             load_16B_per_lane_to_lds<2048, false>(w_ptr, woff[2], m0v);
-            load_16B_per_lane_to_lds<3072, false>(w_ptr, woff[3], m0v);
+            load_16B_per_lane_to_lds<3 * 1024, false>(w_ptr, woff[3], m0v);
             load_16B_per_lane_to_lds<-2048, false>(x_ptr, xoff[0], m0v);
             load_16B_per_lane_to_lds<-1024, false>(x_ptr, xoff[1], m0v);
             x_ptr += STEP_K * 2;
