@@ -80,7 +80,8 @@ int tile_rows(int M, int N) {
 // M = 512 218 -> 189 us, M = 128 78 -> 64 us).  The price of a split is the partials' round trip, the second launch and
 // a pipeline fill per item; at K <= 12288 splitting for rounds measured slower (o_proj M = 768: 31 -> 46 us), so this rule
 // applies only the first two reasons there (the time model below may still split).
-int internal_split(int M, int N, int K, int ns) {
+// `one_round`: no more work items than compute units, half as many as otherwise unless the tiles divide 256 (swiglu_split).
+int internal_split(int M, int N, int K, int ns, bool one_round = false) {
     const int bm = tile_rows(M, N);
     const int64_t tiles = (bm == 32 ? ((int64_t)M + 31) >> 5 : bm == 64 ? ((int64_t)M + 63) >> 6 : ((int64_t)M + 127) >> 7) * (((int64_t)N + 127) / 128);
     int split = 1;
@@ -96,7 +97,7 @@ int internal_split(int M, int N, int K, int ns) {
         return best;
     }
     if (tiles >= 128) return split;             // at least half of the 256 compute units already have a tile
-    while (split < ns && split < 16 && tiles * split * 2 <= 256) split *= 2;
+    while (split < ns && split < 16 && (one_round ? tiles * split * 2 <= 256 : tiles * split < 256)) split *= 2;
     return split;
 }
 
@@ -182,7 +183,7 @@ int mxfp6_split(int M, int N, int ns) {
     int split = 1;
     while (ns > 16 * split && split < TBIK_MAX_SHARDS) split *= 2;     // the tiled kernel walks at most 16 superleaves per shard
     if (tiles >= 128) return split;
-    while (split < ns && split < 16 && tiles * split * 2 <= 256) split *= 2;
+    while (split < ns && split < 16 && tiles * split < 256) split *= 2;
     return split;
 }
 
@@ -1061,10 +1062,17 @@ int tbik_gemm_reference_mxfp6(const void *X, int64_t ldx, const void *Xs, int64_
 // How tbik_gemm_swiglu runs a shape (pure): the K split of the [M, 2 I] GEMM, and whether the unsplit case can end in
 // the 128 x 128 tile's activation epilogue or has to pass gate and up through a 16-bit staging buffer.
 enum { SWIGLU_FUSED = 0, SWIGLU_SPLIT = 1, SWIGLU_STAGED = 2 };
+// The split of the gate/up product, which no time model looks at: a second, partly filled round of work items saves nothing and doubles the
+// planes.  Over 126 shapes (K = 2048, 4096, 8192; nine I of 2112 .. 8128, whose tiles do not divide 256; 1 .. 128 rows; bf16) one round takes of the
+// other rule's time, from HBM / from the cache, 0.896 / 0.889 in the geometric mean, 0.82 .. 1.01 / 0.75 .. 1.03 (one row, K = 4096, I =
+// 2560: 14.8 -> 13.7 / 13.3 -> 12.1 us; 128 rows 23.8 -> 19.8 / 21.0 -> 17.0).  Plans that the model chooses keep the other rule: there one round takes
+// up to 1.11 from the cache (160 rows of 4096 x 6144 in bf16 19.0 -> 20.9 us), and in fp32, whose 32-row tiles share a compute unit, 1.07
+// from HBM (16 rows of 4096 x 6144 25.8 -> 27.6).
+static int swiglu_split(int M, int N, int K, int ns) { return internal_split(M, N, K, ns, true); }
 static int swiglu_route(int dtype, int M, int I, int K, int sl, int ns, int *split) {
     const int N = 2 * I;
     GemmArgs probe{nullptr, K, nullptr, N, nullptr, nullptr, I, dtype, M, N, K, sl, ns, 1, dtype, 0};
-    probe.P = *split = internal_split(M, N, K, ns);
+    probe.P = *split = swiglu_split(M, N, K, ns);
     if (*split > 1) return pick_variant(probe, tile_rows(M, N)) != VARIANT_REFERENCE ? SWIGLU_SPLIT : SWIGLU_STAGED;
     probe.swiglu = 1;
     return (tile_rows(M, N) == 128 && g_forced_variant.load() == VARIANT_AUTO && gemm_tiled_supports(probe, VARIANT_T128))
@@ -1077,7 +1085,7 @@ size_t tbik_gemm_swiglu_workspace_bytes(int M, int I, int K, int leaf, int k_fir
     switch (swiglu_route(TBIK_BF16, M, I, K, sl, ns, &split)) {
         case SWIGLU_FUSED: return 0;
         case SWIGLU_SPLIT: return (size_t)split * (size_t)M * (size_t)(2 * I) * sizeof(float);
-        default: return (((size_t)M * (size_t)(2 * I) * 2 + 255) & ~(size_t)255) + split_planes_bytes(M, 2 * I, internal_split(M, 2 * I, K, ns));
+        default: return (((size_t)M * (size_t)(2 * I) * 2 + 255) & ~(size_t)255) + split_planes_bytes(M, 2 * I, swiglu_split(M, 2 * I, K, ns));
     }
 }
 
