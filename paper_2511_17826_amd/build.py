@@ -112,6 +112,7 @@ def build(save_temps: bool = True, jobs: int = 8, defines=(), lib_path: str = LI
             check_generated_code(os.path.join(BUILD, unit + "-hip-amdgcn-amd-amdhsa-gfx950.s"), "gemm_fp8_tiled_kernel")
         check_generated_code(os.path.join(BUILD, "attention-hip-amdgcn-amd-amdhsa-gfx950.s"), "attention_")
         check_generated_code(os.path.join(BUILD, "rmsnorm_8bit-hip-amdgcn-amd-amdhsa-gfx950.s"), "rmsnorm_8bit_kernel")   # a row stays in registers
+        check_generated_code(os.path.join(BUILD, "rmsnorm_join-hip-amdgcn-amd-amdhsa-gfx950.s"), "rmsnorm_join_kernel")   # likewise
         check_generated_code(os.path.join(BUILD, "gemm_f32-hip-amdgcn-amd-amdhsa-gfx950.s"), "gemm_f32_tiled_kernel")
         check_generated_code(os.path.join(BUILD, "gemm_fp8-hip-amdgcn-amd-amdhsa-gfx950.s"), "gemm_fp8_tiled_kernel")
         check_generated_code(os.path.join(BUILD, "gemm_mxfp4-hip-amdgcn-amd-amdhsa-gfx950.s"), "gemm_mxfp4_tiled_kernel")

@@ -60,16 +60,18 @@ __global__ __launch_bounds__(64 * WAVES) void rmsnorm_join_kernel(const JoinPara
             if constexpr (P == 0) y[i] = *reinterpret_cast<const uint4 *>(p.y + row * p.ldy + c * 8);
             else {
                 const float *src = p.partials + row * p.ldy + c * 8;
-                // Sixteen planes of eight columns are 128 registers, all that a thread of 1024 has: eight planes at a time, half of the tree each.
-                constexpr int AT_ONCE = P > 8 ? 8 : P;
-                float v[8];
+                // Sixteen planes of eight columns are 128 registers, all that a thread of 1024 has, and eight segments of y and of the residual are 64: eight
+                // planes at a time, four beside eight segments, a half or a quarter of the tree each.  (Eight beside eight segments spill: 256 rows of 65536
+                // columns, 16 planes 239 us, so 213, 8 planes 137 and 123; one row of 40000, 16 planes 36.6 and 35.2, 8 planes 21.5 and 22.3.)
+                constexpr int AT_ONCE = P > 4 && PER_WAVE >= 8 ? 4 : P > 8 ? 8 : P, PARTS = P / AT_ONCE;
+                float v[8], third[8];
 #pragma unroll
-                for (int first = 0; first < P; first += AT_ONCE) {
+                for (int part = 0; part < PARTS; ++part) {
                     f32x4 lo[AT_ONCE], hi[AT_ONCE];
 #pragma unroll
                     for (int q = 0; q < AT_ONCE; ++q) {
-                        lo[q] = *reinterpret_cast<const f32x4 *>(src + (first + q) * p.plane);
-                        hi[q] = *reinterpret_cast<const f32x4 *>(src + (first + q) * p.plane + 4);
+                        lo[q] = *reinterpret_cast<const f32x4 *>(src + (part * AT_ONCE + q) * p.plane);
+                        hi[q] = *reinterpret_cast<const f32x4 *>(src + (part * AT_ONCE + q) * p.plane + 4);
                     }
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
@@ -77,7 +79,9 @@ __global__ __launch_bounds__(64 * WAVES) void rmsnorm_join_kernel(const JoinPara
 #pragma unroll
                         for (int q = 0; q < AT_ONCE; ++q) u[q] = e < 4 ? lo[q][e & 3] : hi[q][e & 3];
                         const float t = tree_of<AT_ONCE>(u);
-                        v[e] = first == 0 ? t : v[e] + t;
+                        if (part == 0) v[e] = t;
+                        else if (PARTS == 4 && part == 2) third[e] = t;
+                        else v[e] = v[e] + (part == 3 ? third[e] + t : t);
                     }
                 }
                 y[i] = make_uint4(pack_16x2<F16>(v[0], v[1]), pack_16x2<F16>(v[2], v[3]), pack_16x2<F16>(v[4], v[5]), pack_16x2<F16>(v[6], v[7]));
