@@ -11,4 +11,6 @@ from .binding import (  # noqa: F401
     tbik_set_gemm_variant, tbik_tree_combine, variant_names,
     tbik_combine_residual_rmsnorm_fp8, tbik_combine_residual_rmsnorm_mxfp8, tbik_gemm_epilogue, tbik_gemm_fp8_epilogue, tbik_gemm_mxfp8_epilogue,
     tbik_rmsnorm_fp8, tbik_rmsnorm_mxfp8, tbik_silu_mul_fp8, tbik_silu_mul_mxfp8, tbik_tree_combine_epilogue,
+    tbik_combine_experts, tbik_gemm_grouped, tbik_gemm_grouped_shard_partials, tbik_gemm_grouped_swiglu, tbik_gemm_shard_partials_w4, tbik_gemm_w4,
+    tbik_rmsnorm_residual_rmsnorm, tbik_route_topk,
 )
