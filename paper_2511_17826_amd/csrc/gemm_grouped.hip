@@ -1,12 +1,9 @@
-// Products grouped by expert (16-bit operands): the reference kernel, and the kernel for few rows per expert.
+// Products grouped by expert (16-bit operands): the reference kernel, which takes what the slices and tiles do not (grouped_kernel in tbik_api.hip).
 //
 //   Y[i] = X[rows[i]] W[e]   for the rows i of group e          each row's sum in the order of tbik_gemm (Sec. 4.2, App. D.1)
 //
 // The bits of a row are those of tbik_gemm on that row and its expert's weight: the same matrix instruction over the same k, the
 // same chains, the same tree.
-#include <atomic>
-#include <type_traits>
-
 #include "grouped.hpp"
 
 namespace tbik {

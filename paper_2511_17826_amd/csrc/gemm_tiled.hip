@@ -93,7 +93,8 @@ using TiledParamsOf = std::conditional_t<EPI, TiledEpilogueParams, std::conditio
 // EPI: the output passes through an epilogue (epilogue.hpp); P == 1 then, and no gated activation.
 // GROUP: products grouped by expert (grouped.hpp).  A row tile belongs to one group and its number of rows is what the group leaves
 // it; which tiles there are every workgroup works out from the offsets, in registers.  A tile's rows of X are gathered by the
-// lanes' offsets; reading their indexes waits for the loads in flight once a tile.
+// lanes' offsets.  Reading their indexes waits for the loads in flight, once a tile for each of a wavefront's loads of X (four in 128 rows), which is not
+// seen in the time: gate/up 4096 x 4096 of 6000 rows on 16 experts 293.3 us gathered, 294.2 of rows in order (without the activation 287.6, 288.2).
 template <int LEVELS, int WM, int WN, int MT, int NT, int RING, bool F16, bool EPI, bool GROUP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
 void gemm_tiled_kernel(const TiledParamsOf<EPI, GROUP> p) {

@@ -177,6 +177,12 @@ hipError_t launch_join(const JoinParams &p, int M, hipStream_t s) {
     hipLaunchKernelGGL((rmsnorm_join_kernel<P, WAVES, PER_WAVE, F16>), dim3((unsigned)M), dim3(64 * WAVES), 0, s, p);
     return hipGetLastError();
 }
+// One segment a wavefront while a row has up to ten, which is the quickest for few rows; two in eight wavefronts up to sixteen, which is that for many rows; beyond, sixteen
+// wavefronts.  us, bf16, wavefronts x segments of each; rows 64 / 8191:
+//   1024 columns  4 x 1 2.71 / 18.6, 8 x 1 2.69 / 25.7, 2 x 1 2.67 / 16.8       2048   4 x 1 2.90 / 27.3, 8 x 1 2.82 / 28.9, 2 x 2 3.53 / 27.7
+//   4096          8 x 1 3.56 / 47.6, 8 x 2 3.99 / 49.0, 4 x 2 4.39 / 50.6       5120  10 x 1 3.91 / 67.4, 8 x 2 4.31 / 61.7, 16 x 1 3.88 / 68.8
+//   6144          8 x 2 4.39 / 72.3, 12 x 1 3.96 / 78.6, 16 x 1 3.90 / 79.1     8192   8 x 2 4.77 / 98.7, 16 x 1 4.31 / 101.5, 4 x 4 6.21 / 104.3
+//   16384        16 x 2 6.88 / 191, 8 x 4 7.54 / 196                           32768  16 x 4 11.1 / 404, 8 x 8 14.1 / 406
 template <int P, bool F16>
 hipError_t launch_join_rows(const JoinParams &p, int M, hipStream_t s) {
     if (p.segments <= 4) return launch_join<P, 4, 1, F16>(p, M, s);

@@ -11,7 +11,8 @@
 // two launches, a block of 32 tokens each (select), then every block adds up the blocks' counts (a byte per expert and block) for itself (place); what that
 // reads grows with the square of the tokens, so above ROUTE_MANY blocks the counts are summed over chunks of blocks and the chunks scanned first (sum, scan).
 // Measured, kernels: one token of 128 experts, 8 chosen, 3.0 us; 8191 tokens 8.7 us (select) and 4.5 (place).  Whole calls with and without the two extra
-// launches: 16384 tokens of 128 experts 21.7 / 18.9 us, 32768 30.4 / 34.9 (of 8 experts 29.0 / 23.6); with them 65536 47 us, 1048576 537.
+// launches: 16384 tokens of 128 experts 21.7 / 18.9 us, 32768 30.4 / 34.9 (of 8 experts 29.0 / 23.6); with them 65536 47 us, 1048576 537.  Of so many the
+// instructions of the rounds are the bound (their bytes take some 130 us): a maximum over 64 lanes for each choice of each token.
 #include "tbik_device.hpp"
 #include "tbik_internal.hpp"
 
